@@ -390,6 +390,7 @@ cascade_prefix_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
             // S_a(t) complete: so is every earlier MMA of the tile, in
             // particular P.V_a(t-1), so O is stable and P's columns are free
             wait_phase(s_full(a), (uint32_t)t & 1u, c.err, dead);
+            __syncwarp();
             tc_fence_after();
             // The row's maximum (scores read twice: 128 in registers spilled,
             // 96.7 -> 123.5 us on the step above).  m_ref, the reference of o,
@@ -408,8 +409,12 @@ cascade_prefix_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
                     for (int i = 0; i < 64; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(v[i >> 5][i & 31]));
                 }
             const float cmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
-            if (cmax > m_run + 8.f) {
-                const float al = fast_exp2(m_run - cmax);  // 0 when nothing came before
+            // The lanes of a warp read and write TMEM together (tcgen05.ld and .st
+            // must not run in part of a warp: they may not come back), so every
+            // row of the warp is scaled when one asks for it, the others by 1.
+            const bool rise = cmax > m_run + 8.f;
+            if (__any_sync(0xffffffffu, rise)) {
+                const float al = rise ? fast_exp2(m_run - cmax) : 1.f;  // 0 when nothing came before
                 l_run *= al;
                 if (t >= 1) {  // O holds earlier tiles
                     uint32_t o[32];
@@ -422,7 +427,8 @@ cascade_prefix_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
                         tmem_st32(trow + O_COL + cb * 32, o);
                     }
                 }
-                m_run = cmax;
+                if (rise) m_run = cmax;
+                __syncwarp();
             }
             // p = 2^(s * scale - m_ref) as bf16 pairs over the first columns
             // of S (the A operand of P.V), one 64-key half at a time: the MMA
@@ -455,6 +461,7 @@ cascade_prefix_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_con
         }
         // ---- this CTA's record per (sharer, KV head) ----
         wait_phase(o_done(a), (uint32_t)(nt - 1) & 1u, c.err, dead);
+        __syncwarp();
         tc_fence_after();
         float *rec = row_ok && !dead
                          ? c.ws_pre + (((int64_t)ks * c.S + __ldcg(members + mrow)) * c.Hkv + g) * MF
