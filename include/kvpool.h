@@ -179,6 +179,35 @@ int kv_pool_get_base(const kv_pool *pool, void **base);
  */
 int kv_pool_trim(kv_pool *pool, uint64_t *released_bytes);
 
+/*
+ * Move live blocks together so that kv_pool_trim can give memory back: the
+ * least full superpages (of a VMM pool: chunks) are emptied into free blocks
+ * of fuller ones, each block copied on the device on `stream` and every entry
+ * of the pool's open sequence tables that names it changed (sync them before
+ * the next call that reads their device copies).  A superpage or chunk is
+ * emptied whole or not at all, with at most max_moves blocks moved in all;
+ * one that holds a block with a reference that is no entry of an open table
+ * (kv_alloc_blocks, kv_block_ref) stays.  *n_moves (may be null) receives the
+ * number of blocks moved.  A block moved away is free at once, so work on
+ * other streams that still reads it has to be ordered before `stream`; no
+ * other thread may use the pool's tables during the call.  Errors:
+ * KV_ERR_INVALID_ARG, KV_ERR_CUDA (nothing changed), KV_ERR_OUT_OF_BLOCKS (no
+ * host memory for the plan; nothing changed).
+ */
+int kv_pool_compact(kv_pool *pool, int max_moves, void *stream, int *n_moves);
+
+/*
+ * Copy the first tokens[i] rows (every head's K and V; tokens null: the whole
+ * block) of block src[i] to block dst[i], for i < n (host arrays), on
+ * `stream`.  The copies run side by side.  Checked before anything is
+ * launched, else KV_ERR_INVALID_ARG: every id names a live block of `layout`,
+ * no destination appears twice or is also a source, 0 <= tokens[i] <= bs.
+ * The triples travel as kernel parameters (1360 a launch): the arrays may
+ * change right after the call.
+ */
+int kv_copy_blocks(kv_pool *pool, int layout, int n, const int32_t *src, const int32_t *dst, const int32_t *tokens,
+                   void *stream);
+
 /* A physical-memory budget shared by VMM pools (e.g. M_total - M_res of the
  * node, §III-C).  Destroy it after every pool that uses it. */
 int kv_budget_create(uint64_t limit_bytes, kv_budget **out);
@@ -306,6 +335,33 @@ int kv_seq_release(kv_seqtab *t, int s);
 
 /* Drop slot s's reserved blocks beyond ceil(length / bs) (end of a stage). */
 int kv_seq_trim(kv_seqtab *t, int s);
+
+/*
+ * Give up slot s's blocks that a sliding window of `window` tokens with the
+ * first `sinks` tokens kept no longer reaches: those whose tokens all lie in
+ * [sinks, length - window), which no query at position length - 1 or later
+ * sees (paged_decode_attn_window, paged_prompt_attn).  One reference each is
+ * dropped, the entries become -1, and the slot's reach (its length, where its
+ * next block goes) stays.  The sliding-window calls never look at such
+ * entries; the whole-context calls (paged_decode_attn and its forms) must not
+ * be given the slot any more, and kv_seq_share_prefix over such an entry is
+ * KV_ERR_INVALID_ARG.  *n_freed (may be null) receives the number of blocks
+ * given up.  window < 1 or sinks < 0 is KV_ERR_INVALID_ARG.
+ */
+int kv_seq_evict(kv_seqtab *t, int s, int window, int sinks, int32_t *n_freed);
+
+/*
+ * Fork: each of n distinct empty slots dsts[] takes the length and the
+ * context of slot src, e.g. several agents or samples going on from one
+ * chat.  Blocks that are full are held by reference; a partial last block
+ * becomes each fork's own, its rows copied on the device on `stream`, so that
+ * src and every fork can append.  Blocks that src holds past its length stay
+ * its own; entries it has given up (kv_seq_evict) stay -1.  All-or-nothing:
+ * KV_ERR_OUT_OF_BLOCKS (a block per fork is needed where the length is no
+ * multiple of the block size), KV_ERR_INVALID_ARG (a slot that is not empty,
+ * given twice, or src itself) and KV_ERR_CUDA leave every slot as it was.
+ */
+int kv_seq_fork(kv_seqtab *t, int src, int n, const int32_t *dsts, void *stream);
 
 /*
  * A step's finished sequences replaced by new admissions, in one call: for
@@ -472,6 +528,87 @@ int kv_append(kv_pool *pool, int layout, const uint16_t *k_new, const uint16_t *
               void *stream);
 
 /*
+ * Rotary positions (Su et al., 2021): the pair (x, y) of a head's rotated
+ * columns at position p becomes
+ *     magnitude * (x cos(p f_i) - y sin(p f_i), y cos(p f_i) + x sin(p f_i)),
+ * pair i being columns (i, i + rot_dim/2), or (2i, 2i + 1) where interleaved;
+ * columns from rot_dim on pass through.
+ *
+ * kv_rotary_freqs writes the rot_dim/2 frequencies f_i (radians a position,
+ * host array): base^(-2i/rot_dim), and where a context longer than the
+ * trained one is wanted, scaled by `factor`:
+ *   KV_ROTARY_LINEAR    f / factor (linear position interpolation);
+ *   KV_ROTARY_BY_PARTS  by the turns r = original_len f / 2 pi that a
+ *     frequency makes over the trained context (NTK-by-parts; Peng et al.,
+ *     2023): f / factor up to low_turns, f from high_turns on, between them
+ *     mixed in proportion.  Those authors' magnitude is 0.1 ln(factor) + 1.
+ * A caller with other frequencies fills the array itself.
+ * Errors: KV_ERR_INVALID_ARG (rot_dim odd or not in [2, 512], base <= 1,
+ * factor < 1, high_turns <= low_turns, original_len < 1).
+ *
+ * kv_rotary_steps turns n frequencies into the library's form, turns per
+ * position as 64-bit fixed-point fractions (f / 2 pi in units of 2^-64), in
+ * which position * frequency is exact at any position.  The caller keeps them
+ * in device memory (kv_rotary::steps).
+ */
+enum { KV_ROTARY_PLAIN = 0, KV_ROTARY_LINEAR = 1, KV_ROTARY_BY_PARTS = 2 };
+
+typedef struct kv_rotary_desc {
+    int32_t rot_dim;
+    int32_t scaling;      /* KV_ROTARY_* */
+    double base;          /* e.g. 10000 */
+    double factor;        /* >= 1; read unless KV_ROTARY_PLAIN */
+    double low_turns;     /* KV_ROTARY_BY_PARTS, e.g. 1 */
+    double high_turns;    /* e.g. 32 */
+    int32_t original_len; /* trained context length */
+    int32_t reserved;
+} kv_rotary_desc;
+
+int kv_rotary_freqs(const kv_rotary_desc *desc, double *inv_freq);
+int kv_rotary_steps(const double *inv_freq, int n, uint64_t *steps);
+
+typedef struct kv_rotary {
+    int32_t rot_dim;       /* 0 .. d, a multiple of 16; 0: nothing is rotated */
+    int32_t interleaved;   /* 0: pairs (i, i + rot_dim/2); 1: pairs (2i, 2i + 1) */
+    const uint64_t *steps; /* device uint64[rot_dim/2] (kv_rotary_steps) */
+    float magnitude;
+    int32_t reserved;
+} kv_rotary;
+
+/*
+ * The new tokens' q and k rotated to their positions, and k and v written into
+ * the pool: the append of a decode step or of ragged prompt chunks.
+ *   dev_q_starts  device int32[S + 1], ascending from 0: sequence s's new
+ *                 tokens are rows [starts[s], starts[s + 1]) of q, k and v,
+ *                 T = starts[S] rows in all, at the last positions of its
+ *                 context: row r at n - (starts[s + 1] - r) with n =
+ *                 dev_ctx_lens[s] (post-append).  NULL: one token a sequence
+ *                 (T = S, position n - 1).
+ *   positions     device int32[T] or NULL: positions to rotate by, where they
+ *                 are not those (negative ones are fine)
+ *   q             bf16 rows of [Hq][d], row r at q + r * q_stride elements;
+ *                 q_out: bf16 [T][Hq][d].  q == q_out rotates in place
+ *                 (q_stride = Hq * d); otherwise the two do not overlap.  NULL:
+ *                 no queries.
+ *   k, v          bf16 rows of [Hkv][d] at strides k_stride, v_stride (e.g.
+ *                 column ranges of one fused projection), or both NULL: the
+ *                 queries alone.
+ * Pointers 16-byte aligned, strides multiples of 8 elements that hold a row.
+ * Arithmetic: the fraction of a turn exact, cos, sin and the products in
+ * fp32, one rounding to bf16; v and the columns past rot_dim are copied as
+ * they are.  q_out is written for every row; k and v of a sequence with n <= 0
+ * are not, and a row whose position lies before 0, beyond the table, in an
+ * entry outside the pool or past its sequence's end in dev_q_starts is
+ * skipped and sets the error word.  No two sequences may append to one block.
+ * Errors: KV_ERR_INVALID_ARG, KV_ERR_UNSUPPORTED (rot_dim no multiple of 16),
+ * KV_ERR_CUDA.
+ */
+int kv_append_rotary(kv_pool *pool, int layout, const kv_rotary *rot, const uint16_t *q, int64_t q_stride,
+                     uint16_t *q_out, const uint16_t *k, int64_t k_stride, const uint16_t *v, int64_t v_stride,
+                     const int32_t *positions, const int32_t *dev_q_starts, int T, const int32_t *dev_table,
+                     const int32_t *dev_ctx_lens, int max_blocks, int S, int Hq, void *stream);
+
+/*
  * Bytes of device workspace paged_decode_attn needs for these sizes and this
  * num_splits: a run table, two int32 per (sequence, KV head) run that say
  * where its records are, followed by fp32 split partials, one record of
@@ -532,6 +669,57 @@ int paged_decode_attn_append(kv_pool *pool, int layout, const uint16_t *q, const
                              const uint16_t *v_new, uint16_t *out, const int32_t *dev_table,
                              const int32_t *dev_ctx_lens, int max_blocks, int S, int Hq, float scale,
                              int num_splits, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * paged_decode_attn (k_new, v_new NULL) or paged_decode_attn_append with a
+ * sliding window and sinks: the query at position n - 1 sees token j when
+ *     j >= n - window   or   j < sinks        (j < n).
+ * window = 0 is the whole context (and sinks says nothing then).  Blocks whose
+ * tokens are all unseen are never looked at: their table entries may be -1
+ * (kv_seq_evict) or anything else.  Whatever the unseen tokens' rows hold, NaN
+ * and infinities too, does not reach the output.  Everything else, the
+ * workspace (kv_workspace_bytes), the work split, the arithmetic, step overlap
+ * and n == 0, is as there; the tensor-core variant runs (kv_set_attn_variant
+ * does not apply).  KV_ERR_INVALID_ARG also for window < 0 or sinks < 0.
+ */
+int paged_decode_attn_window(kv_pool *pool, int layout, const uint16_t *q, const uint16_t *k_new,
+                             const uint16_t *v_new, uint16_t *out, const int32_t *dev_table,
+                             const int32_t *dev_ctx_lens, int max_blocks, int S, int Hq, float scale, int window,
+                             int sinks, int num_splits, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Causal attention of prompt chunks over the paged pool: sequence s's queries
+ * are rows [starts[s], starts[s + 1]) of q (dev_q_starts as for
+ * kv_append_rotary, which writes their K and V first), at the last positions
+ * of its context, p = n - (starts[s + 1] - r), n = dev_ctx_lens[s].  With KV
+ * head g = floor(h / G):
+ *     out[r][h] = sum_j softmax_j(scale * q[r][h] . K_j) V_j
+ * over the tokens j <= p with j > p - window or j < sinks (window = 0: all
+ * j <= p).  Chunks of one token are fine (a batch may mix decode steps and
+ * prompts), empty ones too.
+ *   q, out      bf16 [T][Hq][d], 16-byte aligned device arrays, T = starts[S];
+ *               max_q: the longest chunk, at least
+ *   dev_q_starts device int32[S + 1]
+ *   workspace   kv_prompt_workspace_bytes, 256-byte aligned; not initialised;
+ *               0 bytes (NULL) where that says so
+ * Rows at p < 0 (n shorter than the chunk) see nothing: zeros, and the error
+ * word is set.  Unseen tokens, and what lies past a sequence's length in its
+ * last block, reach no output, whatever they hold; a NaN or an infinity in a
+ * seen row reaches the outputs of the queries that see it.  Table entries of
+ * blocks that no query of a chunk sees may be -1.
+ * Arithmetic: bf16 products and fp32 sums on the tensor cores, online softmax
+ * in base 2 with fp32 statistics (a score that leaves fp32's range is
+ * infinite), weights rounded to bf16 for P.V, output rounded once to bf16.  The result of a call does not depend on where its
+ * blocks lie.
+ * Errors: those of paged_decode_attn, KV_ERR_INVALID_ARG also for window < 0,
+ * sinks < 0, T < 0, max_q < 0 or max_q > T.
+ */
+int kv_prompt_workspace_bytes(const kv_pool *pool, int layout, int S, int Hq, int T, int max_q, int max_blocks,
+                              int window, int sinks, size_t *out_bytes);
+
+int paged_prompt_attn(kv_pool *pool, int layout, const uint16_t *q, uint16_t *out, const int32_t *dev_q_starts, int T,
+                      int max_q, const int32_t *dev_table, const int32_t *dev_ctx_lens, int max_blocks, int S, int Hq,
+                      float scale, int window, int sinks, void *workspace, size_t ws_bytes, void *stream);
 
 /*
  * kv_seqtab_sync(t, dev_table, dev_ctx_lens, stream) followed by

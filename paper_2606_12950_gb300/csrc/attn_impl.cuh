@@ -193,6 +193,11 @@ struct AttnArgs {
     // grid before it has completed
     const uint64_t *flags;
     uint64_t epoch;
+    // sliding window (WIN kernels): the query at position n - 1 sees tokens
+    // [n - window, n) and [0, sinks); sink_units = ceil(sinks / kUnit)
+    int32_t window;          // 0: the whole context
+    int32_t sinks;
+    int32_t sink_units;
     // fused table sync (paged_decode_attn_seqtab): this step's lengths of
     // rows [0, sync_nlens) and its changed table entries travel here.  The
     // kernel takes the lengths and those entries from here, and the CTAs
@@ -253,6 +258,7 @@ __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 
 // ------------------------------------------------------------ CUDA cores ---
 template <int D, int G>
 struct FmaCompute {
+    static constexpr bool WIN = false;
     static constexpr int kMinBlocks = 1;                     // registers allow one CTA per SM
     static constexpr int LPT = (G * D / 8 <= 64) ? 8 : 16;  // lanes per token
     static constexpr int EPL = D / LPT;                      // elements per lane
@@ -433,8 +439,10 @@ struct FmaCompute {
 };
 
 // ----------------------------------------------------------- tensor cores --
-template <int D, int G>
+// WIN_: units may hold unseen rows between the sinks and the window (hole)
+template <int D, int G, bool WIN_ = false>
 struct MmaCompute {
+    static constexpr bool WIN = WIN_;
     static_assert(G <= 8, "query-head group must fit the n=8 MMA tile");
     static constexpr int kMinBlocks = 2;
     static constexpr int KS = D / 16;
@@ -446,6 +454,19 @@ struct MmaCompute {
     uint32_t pb[NM][2];  // B operand of P.V (P^T fragments)
     float qk_scale;
     int gid, tig, lane_, nv;
+    int h0, h1;          // (WIN) rows [h0, h1) of the unit are unseen
+
+    __device__ __forceinline__ void hole(int lo, int hi)
+    {
+        h0 = lo;
+        h1 = hi;
+    }
+    // some row of the unit is not seen, or past the context
+    __device__ __forceinline__ bool partial() const
+    {
+        return nv < kUnit<D> || (WIN && h0 < h1 && h1 > 0 && h0 < kUnit<D>);
+    }
+    __device__ __forceinline__ bool unseen(int r) const { return r >= nv || (WIN && r >= h0 && r < h1); }
 
     // qrow: the run's G query rows, staged in shared memory
     __device__ __forceinline__ void begin(const uint16_t *qrow, float scale, int lane)
@@ -498,11 +519,11 @@ struct MmaCompute {
         // Rows past the valid tokens of a loaded box may hold anything; a box
         // that was not loaded (16 mt >= nv) holds an earlier unit's rows: both
         // are masked
-        if (nv < kUnit<D>) {
+        if (partial()) {
 #pragma unroll
             for (int mt = 0; mt < NM; ++mt) {
-                if (mt * 16 + gid >= nv) x[mt][0] = x[mt][1] = -INFINITY;
-                if (mt * 16 + gid + 8 >= nv) x[mt][2] = x[mt][3] = -INFINITY;
+                if (unseen(mt * 16 + gid)) x[mt][0] = x[mt][1] = -INFINITY;
+                if (unseen(mt * 16 + gid + 8)) x[mt][2] = x[mt][3] = -INFINITY;
             }
         }
         float t0 = fmaxf(x[0][0], x[0][2]), t1 = fmaxf(x[0][1], x[0][3]);
@@ -557,12 +578,13 @@ struct MmaCompute {
     {
         // rows past the context may hold anything (even NaN bit patterns);
         // P is zero there, but 0 * NaN is NaN inside the MMA, so clear them
-        if (nv < kUnit<D>) {
-            const int nchunk = (kUnit<D> - nv) * (D / 8);
+        if (partial()) {
+            const int first = WIN ? 0 : nv;
+            const int nchunk = (kUnit<D> - first) * (D / 8);
             for (int idx = lane_; idx < nchunk; idx += 32) {
-                const int r = nv + idx / (D / 8);
+                const int r = first + idx / (D / 8);
                 const int c = idx % (D / 8);
-                *reinterpret_cast<uint4 *>(Vs + swz(r, c)) = make_uint4(0u, 0u, 0u, 0u);
+                if (!WIN || unseen(r)) *reinterpret_cast<uint4 *>(Vs + swz(r, c)) = make_uint4(0u, 0u, 0u, 0u);
             }
             __syncwarp();
         }
@@ -709,20 +731,37 @@ __device__ __forceinline__ int find_seq(const int32_t *T, int S, int32_t u)
     return lo;
 }
 
-// units of a run of sequence s
+// With a sliding window (WIN) a run's units are the tiles of the sinks, then
+// those from the window's first token on; SK[s] holds the tiles left out
+// between the two (0 where they meet or overlap).
 template <int D>
+__device__ __forceinline__ int32_t window_gap(const AttnArgs &a, int32_t n)
+{
+    const int32_t w0 = max(0, n - a.window) / kUnit<D>;
+    return max(0, w0 - a.sink_units);
+}
+// tile of a run's unit i
+__device__ __forceinline__ int32_t window_tile(const AttnArgs &a, int32_t gap, int32_t i)
+{
+    return i < a.sink_units ? i : i + gap;
+}
+
+// units of a run of sequence s
+template <int D, bool WIN>
 __device__ __forceinline__ int32_t run_units(const int32_t *T, int S, int s)
 {
+    if constexpr (WIN)
+        return (int32_t)((uint32_t)(seq_len(T, S, s) + kUnit<D> - 1) / (uint32_t)kUnit<D>) - seq_skip(T, S, s);
     return (int32_t)((uint32_t)(seq_len(T, S, s) - seq_skip(T, S, s) + kUnit<D> - 1) / (uint32_t)kUnit<D>);
 }
 
 // the run that holds unit u
-template <int D>
+template <int D, bool WIN>
 __device__ __forceinline__ Run run_of(const AttnArgs &a, const int32_t *T, int32_t u)
 {
     Run r;
     r.s = find_seq(T, a.S, u);
-    r.nt = run_units<D>(T, a.S, r.s);
+    r.nt = run_units<D, WIN>(T, a.S, r.s);
     const int32_t t0 = T[r.s];
     r.g = div_est((uint32_t)(u - t0), (uint32_t)r.nt, inv_of(r.nt));
     r.begin = t0 + r.g * r.nt;
@@ -730,7 +769,7 @@ __device__ __forceinline__ Run run_of(const AttnArgs &a, const int32_t *T, int32
 }
 
 // the run after r (there is one: the caller has units past r)
-template <int D>
+template <int D, bool WIN>
 __device__ __forceinline__ Run next_run(const AttnArgs &a, const int32_t *T, Run r)
 {
     r.begin += r.nt;
@@ -739,7 +778,7 @@ __device__ __forceinline__ Run next_run(const AttnArgs &a, const int32_t *T, Run
         do
             ++r.s;
         while (T[r.s + 1] == T[r.s]);  // sequences without units
-        r.nt = run_units<D>(T, a.S, r.s);
+        r.nt = run_units<D, WIN>(T, a.S, r.s);
     }
     return r;
 }
@@ -758,14 +797,18 @@ __device__ __forceinline__ int32_t table_entry(const AttnArgs &a, int64_t idx)
 
 // Pool row of box j of unit u's K tile (TMA y coordinate; V is Hkv*bs rows
 // further), kRowBad if the block table names a block outside the pool, or
-// kRowNone if the context ends before the box (the table may have no entry).
+// kRowNone if no token of the box is seen (the context ends before it, or a
+// window leaves it out: the table may have no entry).
 constexpr int32_t kRowBad = -1, kRowNone = -2;
-template <int D>
+template <int D, bool WIN>
 __device__ __forceinline__ int32_t unit_row(const AttnArgs &a, const int32_t *T, int32_t u, int j)
 {
-    const Run r = run_of<D>(a, T, u);
-    const int32_t tok0 = seq_skip(T, a.S, r.s) + (u - r.begin) * kUnit<D> + j * kTile;
+    const Run r = run_of<D, WIN>(a, T, u);
+    const int32_t skip = seq_skip(T, a.S, r.s), i = u - r.begin;
+    const int32_t tok0 = (WIN ? window_tile(a, skip, i) * kUnit<D> : skip + i * kUnit<D>) + j * kTile;
     if (j > 0 && tok0 >= seq_len(T, a.S, r.s)) return kRowNone;
+    // (a unit of one box has a seen token: its box is always loaded)
+    if (WIN && kSub<D> > 1 && tok0 >= a.sinks && tok0 + kTile <= seq_len(T, a.S, r.s) - a.window) return kRowNone;
     const int32_t blk = a.bs_shift >= 0 ? tok0 >> a.bs_shift : tok0 / a.bs;
     const int32_t phys = table_entry(a, (int64_t)r.s * a.max_blocks + blk);
     if (phys < 0 || (int64_t)phys + a.pages_per_block > a.pool_pages) return kRowBad;
@@ -833,14 +876,14 @@ template <int D>
 struct UnitRows {
     int32_t y[kSub<D>];
 };
-template <int D>
+template <int D, bool WIN>
 __device__ __forceinline__ UnitRows<D> rows_of(const AttnArgs &a, const int32_t *T, const int32_t *rows, int32_t cu0,
                                                int32_t u)
 {
     UnitRows<D> r;
     const int32_t k = (u - cu0) * kSub<D>;
 #pragma unroll
-    for (int j = 0; j < kSub<D>; ++j) r.y[j] = k + j < a.rows_cap ? rows[k + j] : unit_row<D>(a, T, u, j);
+    for (int j = 0; j < kSub<D>; ++j) r.y[j] = k + j < a.rows_cap ? rows[k + j] : unit_row<D, WIN>(a, T, u, j);
     return r;
 }
 
@@ -884,6 +927,7 @@ __global__ void __launch_bounds__(kThreads, Comp::kMinBlocks)
 paged_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ AttnArgs a)
 {
     constexpr bool MERGE = MODE != kRecWarps, BY_PART = MODE == kRecCtasByPart;
+    constexpr bool WIN = Comp::WIN;  // sliding window and sinks: no shared prefix, SK holds tiles (window_gap)
     constexpr int HALVES = D / 64;
     constexpr int UNIT = kUnit<D>, SUB = kSub<D>;
     static_assert(HALVES == 1 || SUB == 1, "a unit's boxes follow each other in shared memory");
@@ -977,10 +1021,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constan
         for (int s = lo; s < hi; ++s) {
             int32_t raw;
             const int32_t n = load_len(a, s, &raw);
-            const int32_t k = load_skip(a, s, n);
+            const int32_t k = WIN ? window_gap<D>(a, n) : load_skip(a, s, n);
             NL[s] = n | (raw != n ? (int32_t)0x80000000 : 0);
             SK[s] = k;
-            const int32_t ne = n - k;
+            const int32_t ne = WIN ? n - k * UNIT : n - k;
             local += ((ne + UNIT - 1) / UNIT) * Hkv;
         }
         int32_t incl = local;
@@ -1002,7 +1046,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constan
         int32_t run = (warp > 0 ? base : 0) + incl - local;
         for (int s = lo; s < hi; ++s) {  // this thread's own NL / SK entries
             T[s] = run;
-            run += run_units<D>(T, S, s) * Hkv;
+            run += run_units<D, WIN>(T, S, s) * Hkv;
         }
         if (tid == 0) T[S] = tot;
         if (early) {
@@ -1010,7 +1054,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constan
             write_sync();
         }
         for (int s = lo; s < hi; ++s) {  // sequences with no tile: writes after any wait
-            const int32_t n = NL[s] & 0x7fffffff, ne = n - SK[s];
+            const int32_t n = NL[s] & 0x7fffffff, ne = WIN ? n : n - SK[s];
             if (ne != 0 || (s % a.P) != (int)blockIdx.x) continue;
             make_ready();
             // the fused append needs the new token outside a shared prefix
@@ -1073,7 +1117,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constan
     // memory system is idle (later lookups would queue behind the TMA stream)
     {
         const int32_t k0 = (u0 - cu0) * SUB, k1 = min((u1 - cu0) * SUB, a.rows_cap);
-        for (int32_t k = k0 + lane; k < k1; k += 32) rows[k] = unit_row<D>(a, T, cu0 + k / SUB, k % SUB);
+        for (int32_t k = k0 + lane; k < k1; k += 32) rows[k] = unit_row<D, WIN>(a, T, cu0 + k / SUB, k % SUB);
         __syncwarp();
     }
     float *mbuf = reinterpret_cast<float *>(mbufs) + (size_t)warp * MF;
@@ -1088,7 +1132,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constan
 
     const uint32_t el = elect_one();
     for (int st = 0; st < kStages && u0 + st < u1; ++st) {
-        const UnitRows<D> ur = rows_of<D>(a, T, rows, cu0, u0 + st);
+        const UnitRows<D> ur = rows_of<D, WIN>(a, T, rows, cu0, u0 + st);
         issue_half<D>(&tmap, a, ur, 0, smem_u32(k_of(st)), bk_of(st), policy, el);
         issue_half<D>(&tmap, a, ur, 1, smem_u32(k_of(st) + TILE_BYTES), bv_of(st), policy, el);
     }
@@ -1104,7 +1148,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constan
     };
     Run run{};
     if (!MERGE || u0 < u1) {
-        run = run_of<D>(a, T, u0);
+        run = run_of<D, WIN>(a, T, u0);
         stage_q(run);
         cp_async_commit();
     }
@@ -1130,7 +1174,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constan
         }
         Run next = run;
         if (pe < u1) {  // the next piece's q rows
-            next = next_run<D>(a, T, run);
+            next = next_run<D, WIN>(a, T, run);
             stage_q(next);
         }
         cp_async_commit();
@@ -1140,12 +1184,14 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constan
             uint8_t *Ks = k_of(st);
             uint8_t *Vs = Ks + TILE_BYTES;
             const uint32_t bk = bk_of(st), bv = bv_of(st);
-            const int nvalid = min(UNIT, n - skip - (uu - run.begin) * UNIT);
+            const int tok0 = WIN ? window_tile(a, skip, uu - run.begin) * UNIT : skip + (uu - run.begin) * UNIT;
+            const int nvalid = min(UNIT, n - tok0);
+            if constexpr (WIN) comp.hole(a.sinks - tok0, n - a.window - tok0);
             const bool more = uu + kStages < u1;  // the unit this stage takes next
             const bool app = app_run && uu == run_end - 1;
-            const int arow = (n - 1 - skip) % UNIT;
+            const int arow = (WIN ? n - 1 : n - 1 - skip) % UNIT;
             UnitRows<D> ur;
-            if (more) ur = rows_of<D>(a, T, rows, cu0, uu + kStages);
+            if (more) ur = rows_of<D, WIN>(a, T, rows, cu0, uu + kStages);
             wait_phase(bk, par, a.err, dead);
             if (app) {
                 cp_async_wait_all();  // the new K/V rows
@@ -1177,7 +1223,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constan
                 // the tile have completed, and no other unit covers that row
                 const int j = arow / kTile;  // the box that holds the row
                 const int32_t k = (uu - cu0) * SUB + j;
-                const int32_t y = k < a.rows_cap ? rows[k] : unit_row<D>(a, T, uu, j);
+                const int32_t y = k < a.rows_cap ? rows[k] : unit_row<D, WIN>(a, T, uu, j);
                 if (y >= 0 && lane < AB / 16) {
                     const int which = lane / (D / 8), c = lane % (D / 8);
                     const int64_t row = (int64_t)y + arow % kTile + (int64_t)which * Hkv * a.bs;
@@ -1194,7 +1240,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constan
         // ---- end of a piece: the output, or this part's partial ----
         const int32_t r = run.s * Hkv + run.g;
         // a run whose prefix lives in prefix records always leaves a partial
-        const bool split = run.begin < g0 || run_end > g1 || skip > 0;
+        const bool split = run.begin < g0 || run_end > g1 || (!WIN && skip > 0);
         // the run's first part and its last one tell the combine where its
         // records begin and end
         const bool first = run.begin >= g0, last = run_end <= g1;
@@ -1518,7 +1564,10 @@ constexpr int kRowsCap = 2048;
 inline int64_t table_units(const AttnArgs &a, int D)
 {
     const int unit = D == 64 ? kUnit<64> : kUnit<128>;
-    return (int64_t)a.S * a.Hkv * (((int64_t)a.max_blocks * a.bs + unit - 1) / unit);
+    int64_t run = ((int64_t)a.max_blocks * a.bs + unit - 1) / unit;
+    if (a.window > 0)  // no run is longer than the sinks and the window
+        run = std::min(run, (int64_t)a.sink_units + ((int64_t)a.window + unit - 1) / unit + 1);
+    return (int64_t)a.S * a.Hkv * run;
 }
 // fewer than kMergeUnits units a warp (by the table's width)
 inline bool small_batch(const AttnArgs &a, int D, int P, int nwarps)

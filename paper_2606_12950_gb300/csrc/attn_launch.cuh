@@ -243,6 +243,11 @@ int kvp_attn_d64(int variant, int G, const CUtensorMap *tmap, const kvp::AttnArg
                  cudaStream_t st, int what, int *P_out);
 int kvp_attn_d128(int variant, int G, const CUtensorMap *tmap, const kvp::AttnArgs *a, int P_req, int sm_count,
                   cudaStream_t st, int what, int *P_out);
+// the same with a sliding window (a->window > 0), tensor-core MMA
+int kvp_attn_win_d64(int G, const CUtensorMap *tmap, const kvp::AttnArgs *a, int P_req, int sm_count, cudaStream_t st,
+                     int what, int *P_out);
+int kvp_attn_win_d128(int G, const CUtensorMap *tmap, const kvp::AttnArgs *a, int P_req, int sm_count, cudaStream_t st,
+                      int what, int *P_out);
 int kvp_cascade_d64(int G, const CUtensorMap *tmap, const kvp::CascadeArgs *c, int grid, int sm_count,
                     cudaStream_t st, bool launch, int *P_out);
 int kvp_cascade_d128(int G, const CUtensorMap *tmap, const kvp::CascadeArgs *c, int grid, int sm_count,

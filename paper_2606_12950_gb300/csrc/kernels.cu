@@ -15,6 +15,7 @@
 #include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 
+#include "attn_host.h"
 #include "attn_launch.cuh"
 #include "pool_internal.h"
 #include "seqtab_internal.h"
@@ -197,6 +198,9 @@ int attn_shape(const kv_pool *p, int layout, int S, int Hq, int max_blocks, int 
 int dispatch(int variant, int D, int G, const CUtensorMap *tmap, const kvp::AttnArgs *a, int P_req, int sms,
              cudaStream_t st, int what, int *P_out)
 {
+    if (a->window > 0)
+        return D == 64 ? kvp_attn_win_d64(G, tmap, a, P_req, sms, st, what, P_out)
+                       : kvp_attn_win_d128(G, tmap, a, P_req, sms, st, what, P_out);
     if (D == 64) return kvp_attn_d64(variant, G, tmap, a, P_req, sms, st, what, P_out);
     return kvp_attn_d128(variant, G, tmap, a, P_req, sms, st, what, P_out);
 }
@@ -400,6 +404,12 @@ int cascade_dispatch(int D, int G, const CUtensorMap *tmap, const kvp::CascadeAr
 
 }  // namespace
 
+int kvp_attn_shape(const kv_pool *p, int layout, int S, int Hq, int max_blocks, int *G_out)
+{
+    return attn_shape(p, layout, S, Hq, max_blocks, G_out);
+}
+int kvp_ensure_tmap(kv_pool *p, int layout) { return ensure_tmap(p, layout); }
+
 extern "C" {
 
 int kv_append(kv_pool *p, int layout, const uint16_t *k_new, const uint16_t *v_new, const int32_t *dev_table,
@@ -490,10 +500,10 @@ struct CascadePlan {
 int attn_call(kv_pool *p, int layout, const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new,
               uint16_t *out, const int32_t *dev_table, const int32_t *dev_ctx_lens, int max_blocks, int S, int Hq,
               float scale, int num_splits, void *workspace, size_t ws_bytes, void *stream,
-              const CascadePlan *cas = nullptr, const FusedSync *sync = nullptr)
+              const CascadePlan *cas = nullptr, const FusedSync *sync = nullptr, int window = 0, int sinks = 0)
 {
     int G = 0;
-    if (num_splits < 0 || !std::isfinite(scale)) return KV_ERR_INVALID_ARG;
+    if (num_splits < 0 || !std::isfinite(scale) || window < 0 || sinks < 0) return KV_ERR_INVALID_ARG;
     int rc = attn_shape(p, layout, S, Hq, max_blocks, &G);
     if (rc) return rc;
     if (S == 0) return KV_OK;
@@ -519,7 +529,22 @@ int attn_call(kv_pool *p, int layout, const uint16_t *q, const uint16_t *k_new, 
     a.Hkv = L.num_kv_heads;
     a.bs = p->desc.block_size;
     a.qk_scale = scale * 1.4426950408889634f;
+    // a window that no context outgrows is the whole context
+    const int32_t reach = max_blocks * a.bs;
+    if (window > 0 && window < reach) {
+        const int unit = L.head_dim == 64 ? kvp::kUnit<64> : kvp::kUnit<128>;
+        a.window = window;
+        a.sinks = std::min(sinks, reach);
+        a.sink_units = (a.sinks + unit - 1) / unit;
+    }
     int P = 0;
+    if (a.window > 0 && num_splits == 0 && variant == 1) {
+        // the workspace is sized for the pool's variant, with fewer CTAs an SM
+        rc = L.head_dim == 64 ? kvp_attn_d64(variant, G, nullptr, &a, 0, p->sm_count, nullptr, kvp::kLaunchQuery, &P)
+                              : kvp_attn_d128(variant, G, nullptr, &a, 0, p->sm_count, nullptr, kvp::kLaunchQuery, &P);
+        if (rc) return rc;
+        num_splits = P;
+    }
     rc = dispatch(variant, L.head_dim, G, nullptr, &a, num_splits, p->sm_count, nullptr, kvp::kLaunchQuery, &P);
     if (rc) return rc;
     size_t part_off;
@@ -757,6 +782,15 @@ int paged_decode_attn_append(kv_pool *p, int layout, const uint16_t *q, const ui
     if (!k_new || !v_new) return KV_ERR_INVALID_ARG;
     return attn_call(p, layout, q, k_new, v_new, out, dev_table, dev_ctx_lens, max_blocks, S, Hq, scale,
                      num_splits, workspace, ws_bytes, stream);
+}
+
+int paged_decode_attn_window(kv_pool *p, int layout, const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new,
+                             uint16_t *out, const int32_t *dev_table, const int32_t *dev_ctx_lens, int max_blocks,
+                             int S, int Hq, float scale, int window, int sinks, int num_splits, void *workspace,
+                             size_t ws_bytes, void *stream)
+{
+    return attn_call(p, layout, q, k_new, v_new, out, dev_table, dev_ctx_lens, max_blocks, S, Hq, scale, num_splits,
+                     workspace, ws_bytes, stream, nullptr, nullptr, window, sinks);
 }
 
 int paged_decode_attn_seqtab(kv_pool *p, kv_seqtab *t, const uint16_t *q, const uint16_t *k_new,

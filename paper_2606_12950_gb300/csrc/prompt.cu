@@ -1,0 +1,154 @@
+// prompt.cu -- causal attention of prompt chunks over the paged pool
+// (paged_prompt_attn): argument checks, the split of the key range, launches.
+#include <algorithm>
+#include <atomic>
+#include <climits>
+#include <cmath>
+#include <cstdint>
+
+#include <cuda_runtime.h>
+
+#include "attn_host.h"
+#include "pool_internal.h"
+#include "prompt_impl.cuh"
+#include "stream_order.h"
+
+namespace {
+
+// Row tiles the grid needs at most (the chunks' lengths are on the device).
+int64_t row_tiles(int S, int T, int max_q, int TT)
+{
+    return std::min((int64_t)S * ((max_q + TT - 1) / TT), (int64_t)T / TT + S);
+}
+
+// Key splits: CTAs for every SM where the rows are few, each with at least
+// kLeastTiles key tiles.
+constexpr int kLeastTiles = 4;
+int key_splits(int64_t ctas, int sm_count, int64_t reach, int TT, int window, int sinks)
+{
+    int64_t keys = reach;
+    if (window > 0) keys = std::min(keys, (int64_t)window + TT + sinks);
+    const int64_t tiles = (keys + kvp::kPrKeys - 1) / kvp::kPrKeys;
+    const int64_t want = std::min((int64_t)sm_count / std::max<int64_t>(1, ctas), tiles / kLeastTiles);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(want, kvp::kPrMaxSplits));
+}
+
+struct Shape {
+    int G, D, Hkv, TT, KS;
+    int64_t tiles;
+    size_t ws_bytes;
+};
+
+int prompt_shape(const kv_pool *p, int layout, int S, int Hq, int T, int max_q, int max_blocks, int window, int sinks,
+                 Shape *s)
+{
+    const int rc = kvp_attn_shape(p, layout, S, Hq, max_blocks, &s->G);
+    if (rc) return rc;
+    if (T < 0 || max_q < 0 || max_q > T || window < 0 || sinks < 0) return KV_ERR_INVALID_ARG;
+    if (T > 0 && (S == 0 || max_q == 0)) return KV_ERR_INVALID_ARG;
+    const kv_layout &L = p->desc.layouts[layout];
+    s->D = L.head_dim;
+    s->Hkv = L.num_kv_heads;
+    s->TT = kvp::kPrTiles * (kvp::kPrRows / s->G);
+    s->tiles = row_tiles(S, T, max_q, s->TT);
+    if (p->sm_count <= 0) return KV_ERR_CUDA;
+    s->KS = key_splits(s->tiles * s->Hkv, p->sm_count, (int64_t)max_blocks * p->desc.block_size, s->TT, window, sinks);
+    if (s->tiles * s->Hkv * s->KS > INT32_MAX) return KV_ERR_INVALID_ARG;
+    s->ws_bytes = s->KS > 1 ? (size_t)s->KS * T * Hq * (s->D + 4) * sizeof(float) : 0;
+    return KV_OK;
+}
+
+template <int D>
+int prompt_run(const CUtensorMap *tmap, const kvp::PromptArgs &a, cudaStream_t st)
+{
+    static std::atomic<bool> attr_set{false};
+    const size_t smem = kvp::prompt_smem_bytes<D>();
+    if (!attr_set.load()) {
+        if (cudaFuncSetAttribute(kvp::prompt_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
+            cudaSuccess)
+            return KV_ERR_CUDA;
+        attr_set.store(true);
+    }
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.tiles * a.Hkv * a.KS));
+    cfg.blockDim = dim3(kvp::kPrThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kvp::prompt_attn_kernel<D>, *tmap, a) != cudaSuccess) return KV_ERR_CUDA;
+    kvp_note_stream(st, false);
+    if (a.KS == 1) return KV_OK;
+    const int64_t rows = (int64_t)a.T * a.Hkv * a.G;
+    cfg.gridDim = dim3((unsigned)((rows + 7) / 8));
+    cfg.blockDim = dim3(256);
+    cfg.dynamicSmemBytes = 0;
+    if (cudaLaunchKernelEx(&cfg, kvp::prompt_merge_kernel<D>, (const float *)a.ws, a.out, rows, (int)a.KS) !=
+        cudaSuccess)
+        return KV_ERR_CUDA;
+    return KV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int kv_prompt_workspace_bytes(const kv_pool *p, int layout, int S, int Hq, int T, int max_q, int max_blocks, int window,
+                              int sinks, size_t *out_bytes)
+{
+    if (!out_bytes) return KV_ERR_INVALID_ARG;
+    Shape s{};
+    const int rc = prompt_shape(p, layout, S, Hq, T, max_q, max_blocks, window, sinks, &s);
+    if (rc) return rc;
+    *out_bytes = s.ws_bytes;
+    return KV_OK;
+}
+
+int paged_prompt_attn(kv_pool *p, int layout, const uint16_t *q, uint16_t *out, const int32_t *dev_q_starts, int T,
+                      int max_q, const int32_t *dev_table, const int32_t *dev_ctx_lens, int max_blocks, int S, int Hq,
+                      float scale, int window, int sinks, void *workspace, size_t ws_bytes, void *stream)
+{
+    if (!std::isfinite(scale)) return KV_ERR_INVALID_ARG;
+    Shape s{};
+    int rc = prompt_shape(p, layout, S, Hq, T, max_q, max_blocks, window, sinks, &s);
+    if (rc) return rc;
+    if (T == 0) return KV_OK;
+    if (!q || !out || !dev_q_starts || !dev_table || !dev_ctx_lens) return KV_ERR_INVALID_ARG;
+    if (((uintptr_t)q & 15u) || ((uintptr_t)out & 15u)) return KV_ERR_INVALID_ARG;
+    if (s.ws_bytes && (!workspace || ws_bytes < s.ws_bytes || ((uintptr_t)workspace & 255u))) return KV_ERR_WORKSPACE;
+    rc = kvp_ensure_tmap(p, layout);
+    if (rc) return rc;
+    kvp::PromptArgs a{};
+    a.q = q;
+    a.out = out;
+    a.pool = reinterpret_cast<const uint16_t *>(p->desc.device_base);
+    a.starts = dev_q_starts;
+    a.table = dev_table;
+    a.ctx_lens = dev_ctx_lens;
+    a.err = p->desc.device_error;
+    a.ws = reinterpret_cast<float *>(workspace);
+    a.rows_per_page = (int64_t)(p->page_bytes / (2ull * s.D));
+    a.pool_pages = p->n_pages;
+    a.pages_per_block = p->pages_per_block[layout];
+    a.max_blocks = max_blocks;
+    a.S = S;
+    a.Hkv = s.Hkv;
+    a.G = s.G;
+    a.bs = p->desc.block_size;
+    a.T = T;
+    a.tiles = (int32_t)s.tiles;
+    a.KS = s.KS;
+    const int32_t reach = max_blocks * a.bs;
+    a.window = window < reach ? window : 0;  // one that no context outgrows is the whole context
+    a.sinks = a.window > 0 ? std::min(sinks, reach) : 0;
+    a.q_xor = scale < 0.f ? 0x80008000u : 0u;
+    a.q_and = scale == 0.f ? 0u : 0xffffffffu;
+    a.qk_scale = scale == 0.f ? 1.f : std::fabs(scale) * 1.4426950408889634f;
+    const cudaStream_t st = (cudaStream_t)stream;
+    return s.D == 64 ? prompt_run<64>(&p->tmap[layout], a, st) : prompt_run<128>(&p->tmap[layout], a, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,602 @@
+// prompt_impl.cuh -- causal attention of prompt chunks over the paged pool,
+// with a sliding window and sinks, on the fifth-generation tensor cores.
+//
+// A query at position p of its sequence sees the tokens j <= p with
+// j > p - window or j < sinks (window 0: all).  The query heads of a KV head
+// share its K and V, so a Q tile's 128 rows are TQ = floor(128 / G)
+// consecutive tokens x G heads of one (sequence, KV head), and a CTA takes two
+// Q tiles (2 TQ tokens) over their common key range, in 128-key tiles:
+//   S = Q K^T     tcgen05.mma, M = 128 rows, N = 128 keys, fp32 in TMEM
+//   softmax       one thread per row, S read from TMEM, base 2, lazy rescale
+//   O += P V      tcgen05.mma, P (bf16) over S in TMEM, V from shared memory
+// While one Q tile's four warps run the softmax the tensor core works on the
+// other's.  A warp each loads K and V by TMA (16-token boxes, 128-byte
+// swizzle, two stages, released apart), one issues the MMAs.
+//
+// Keys.  A CTA's tiles are those of the sinks, then those from its first
+// query's window on up to its last query; a tile in which some query of the
+// CTA does not see some token (the diagonal, the window's edge, the sinks'
+// edge) is masked element by element, the others are not looked at.
+// 16-token boxes that no query of the CTA sees are not loaded: their table
+// entries may be gone (kv_seq_evict).
+//
+// NaN and infinities.  A weight of 0 times a NaN is NaN in the MMA.  So in
+// masked tiles the rows of V that no query sees are cleared, and rows that some
+// query sees and that hold a NaN or an infinity are cleared too and noted; at
+// the end each row adds the noted tokens that it sees itself.
+//
+// Few rows (KS > 1): a CTA's key tiles are split over KS CTAs, each leaving per
+// row one fp32 record (o, running max, sum) that prompt_merge_kernel merges.
+#pragma once
+
+#include "attn_impl.cuh"
+
+namespace kvp {
+
+constexpr int kPrRows = 128;   // rows of a Q tile: the MMA's M
+constexpr int kPrTiles = 2;    // Q tiles per CTA
+constexpr int kPrKeys = 128;   // keys per tile: S's N, P.V's K
+constexpr int kPrStages = 2;
+constexpr int kPrSoft = kPrTiles * 128;     // softmax threads, one per row
+constexpr int kPrThreads = kPrSoft + 96;    // + K and V load warps, MMA warp
+constexpr int kPrMasked = 16;  // masked tiles of a CTA: 3 on the diagonal, 3 at the window's edge, 2 of sinks at most
+constexpr int kPrMaxSplits = 16;
+// TMEM per Q tile: S [0, 128) fp32, P over S's first 64 columns (bf16 pairs), O [128, 128 + d)
+constexpr uint32_t kPrTmemCols = 256;
+
+struct PromptArgs {
+    const uint16_t *q;
+    uint16_t *out;
+    const uint16_t *pool;
+    const int32_t *starts;
+    const int32_t *table;
+    const int32_t *ctx_lens;
+    int32_t *err;
+    float *ws;             // KS > 1: records [KS][T][Hq], pr_record<D>() floats each
+    int64_t rows_per_page;
+    int64_t pool_pages;
+    int32_t pages_per_block;
+    int32_t max_blocks;
+    int32_t S, Hkv, G, bs, T;
+    int32_t tiles;         // row tiles of the grid, at least those there are
+    int32_t KS;
+    int32_t window, sinks; // window 0: the whole context
+    uint32_t q_xor;        // sign bits flipped in q (a negative scale), and
+    uint32_t q_and;        // 0 where the scale is 0
+    float qk_scale;        // |scale| * log2(e) (1 where the scale is 0)
+};
+
+// a record: o[D] unnormalised, m, l, padded to 16 bytes
+template <int D>
+__host__ __device__ constexpr uint32_t pr_record() { return D + 4; }
+
+// shared memory (offsets from a 1024-byte aligned base)
+template <int D>
+struct PrSmem {
+    static constexpr int HALVES = D / 64;
+    static constexpr uint32_t KV_HALF = kPrKeys * 128;
+    static constexpr uint32_t KV_TILE = HALVES * KV_HALF;
+    static constexpr uint32_t STAGE = 2 * KV_TILE;
+    static constexpr uint32_t Q_HALF = kPrRows * 128;
+    static constexpr uint32_t Q_TILE = HALVES * Q_HALF;
+    static constexpr uint32_t ST_OFF = kPrTiles * Q_TILE;
+    static constexpr uint32_t BAR_OFF = ST_OFF + kPrStages * STAGE;
+    static constexpr int NBARS = 4 * kPrStages + 4 * kPrTiles + 2;
+    static constexpr uint32_t SLOT_OFF = BAR_OFF + NBARS * 8;
+    static constexpr uint32_t NOTE_OFF = SLOT_OFF + 16;  // per masked tile: its first key, 4 words of noted rows
+    static constexpr uint32_t BYTES = NOTE_OFF + kPrMasked * 5 * 4 + 16;
+};
+
+__device__ __forceinline__ uint32_t pr_pack(float lo, float hi)
+{
+    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t *>(&v);
+}
+
+// A CTA's share: tokens [i0, i1) of sequence s, its keys.
+struct PrWork {
+    int32_t s;
+    int32_t row0;      // q row of token i0
+    int32_t ntok;      // tokens of this CTA (0: none)
+    int32_t p0, p1;    // positions of its first and last token
+    int32_t lo;        // first token of the first query's window
+    int32_t head;      // key tiles of the sinks before the window's tiles
+    int32_t gap;       // key tiles left out between the two
+    int32_t nt;        // key tiles in all
+    __device__ __forceinline__ int32_t key0(int32_t i) const { return (i < head ? i : i + gap) * kPrKeys; }
+};
+
+// The work of row tile `tile` (each warp for itself, converged).
+__device__ __forceinline__ PrWork pr_work(const PromptArgs &a, int tile, int TT, int lane)
+{
+    PrWork w{};
+    int before = 0;  // row tiles of the sequences before
+    for (int s0 = 0; s0 < a.S; s0 += 32) {
+        const int s = s0 + lane;
+        int cnt = 0;
+        if (s < a.S) cnt = max(0, a.starts[s + 1] - a.starts[s]);
+        const int nt = (cnt + TT - 1) / TT;
+        int incl = nt;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, off);
+            if (lane >= off) incl += v;
+        }
+        const unsigned hit = __ballot_sync(0xffffffffu, before + incl > tile);
+        if (hit) {
+            const int l = __ffs((int)hit) - 1;
+            const int t0 = before + __shfl_sync(0xffffffffu, incl - nt, l);
+            const int nq = __shfl_sync(0xffffffffu, cnt, l);
+            w.s = s0 + l;
+            const int i0 = (tile - t0) * TT;
+            const int32_t st = a.starts[w.s];
+            w.row0 = st + i0;
+            w.ntok = min(TT, nq - i0);
+            if (st < 0 || (int64_t)st + nq > a.T) {  // a bad array: nothing of it is touched
+                report(a.err, KV_ERR_DEVICE_BOUNDS);
+                w.ntok = 0;
+                return w;
+            }
+            int32_t n = a.ctx_lens[w.s];
+            const int32_t cap = a.max_blocks * a.bs;
+            if (n < nq || n > cap) {
+                report(a.err, KV_ERR_DEVICE_BOUNDS);
+                n = n > cap ? cap : max(n, 0);
+            }
+            w.p0 = n - nq + i0;
+            w.p1 = w.p0 + w.ntok - 1;
+            if (w.p1 < 0) return w;
+            w.lo = a.window > 0 ? max(0, w.p0 - a.window + 1) : 0;
+            const int32_t sk = min(a.sinks, w.lo);  // sinks before the window
+            w.head = (sk + kPrKeys - 1) / kPrKeys;
+            w.gap = max(0, w.lo / kPrKeys - w.head);
+            w.nt = w.p1 / kPrKeys + 1 - w.gap;
+            return w;
+        }
+        before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    return w;
+}
+
+// Pool row of token tok's K for KV head g, or -1 outside the pool.
+__device__ __forceinline__ int32_t pr_pool_row(const PromptArgs &a, int s, int g, int32_t tok)
+{
+    const int32_t blk = tok / a.bs;
+    const int32_t phys = a.table[(int64_t)s * a.max_blocks + blk];
+    if (phys < 0 || (int64_t)phys + a.pages_per_block > a.pool_pages) return -1;
+    return (int32_t)((int64_t)phys * a.rows_per_page + (int64_t)g * a.bs + (tok - blk * a.bs));
+}
+
+template <int D>
+__global__ void __launch_bounds__(kPrThreads, 1)
+prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ PromptArgs a)
+{
+    using L = PrSmem<D>;
+    constexpr int HALVES = L::HALVES;
+    constexpr uint32_t O_COL = kPrKeys;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const uint32_t sbase = smem_u32(smem);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + L::BAR_OFF);
+    uint32_t *tslot = reinterpret_cast<uint32_t *>(smem + L::SLOT_OFF);
+    int32_t *note_key = reinterpret_cast<int32_t *>(smem + L::NOTE_OFF);      // [kPrMasked]
+    uint32_t *note = reinterpret_cast<uint32_t *>(note_key + kPrMasked);      // [kPrMasked][4]
+    int32_t *n_notes = reinterpret_cast<int32_t *>(note + kPrMasked * 4);
+    auto bar = [&](int i) { return smem_u32(&bars[i]); };
+    constexpr int FULL_K = 0, EMPTY_K = kPrStages, FULL_V = 2 * kPrStages, EMPTY_V = 3 * kPrStages;
+    constexpr int QB = 4 * kPrStages, FIN = QB + 4 * kPrTiles, Q_READY = FIN + 1;
+    auto s_full = [&](int t) { return bar(QB + 4 * t); };
+    auto p_full = [&](int t, int half) { return bar(QB + 4 * t + 1 + half); };
+    auto o_done = [&](int t) { return bar(QB + 4 * t + 3); };
+
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    const int G = a.G, Hq = a.Hkv * G, TQ = kPrRows / G, TT = kPrTiles * TQ;
+    int bid = blockIdx.x;
+    const int ks = bid % a.KS;
+    bid /= a.KS;
+    const int g = bid % a.Hkv;
+    const int tile = a.tiles - 1 - bid / a.Hkv;  // the longest key ranges first
+
+    if (tid == 0) {
+        for (int i = 0; i < 4 * kPrStages; ++i) mbar_init(bar(i), 1);
+        for (int t = 0; t < kPrTiles; ++t) {
+            mbar_init(s_full(t), 1);
+            mbar_init(p_full(t, 0), 128);
+            mbar_init(p_full(t, 1), 128);
+            mbar_init(o_done(t), 1);
+        }
+        mbar_init(bar(FIN), 1);
+        mbar_init(bar(Q_READY), kPrSoft);
+        fence_mbar_init();
+    }
+    if (warp == 0) {
+        tmem_alloc(smem_u32(tslot), kPrTiles * kPrTmemCols);
+        tmem_relinquish();
+    }
+    if (tid == 32) prefetch_tensormap(&tmap);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tbase = *tslot;
+    bool dead = false;
+    grid_dependency_wait();
+    grid_launch_dependents();
+
+    const PrWork w = pr_work(a, tile, TT, lane);
+    const int nqt = (w.ntok + TQ - 1) / TQ;  // Q tiles with tokens
+    const int t0 = (int)((int64_t)ks * w.nt / a.KS), t1 = (int)((int64_t)(ks + 1) * w.nt / a.KS);
+    const int nt = t1 - t0;  // this CTA's key tiles
+    auto key0 = [&](int t) { return w.key0(t0 + t); };
+    // some query of the CTA does not see some token of the tile
+    auto masked = [&](int k0) {
+        return k0 + kPrKeys - 1 > w.p0 ||
+               (a.window > 0 && k0 <= w.p1 - a.window && k0 + kPrKeys > a.sinks);
+    };
+    // some query of the CTA sees some token of [tok, tok + n)
+    auto seen_by_any = [&](int tok, int n) { return tok <= w.p1 && (tok + n > w.lo || tok < a.sinks); };
+
+    const int qa = tid / kPrRows, r = tid % kPrRows;  // Q tile and row of a softmax thread
+    const int itok = qa * TQ + r / G;                 // its token in the CTA
+    const bool row_ok = tid < kPrSoft && r < TQ * G && itok < w.ntok;
+    const int64_t qrow_off = ((int64_t)(w.row0 + itok) * Hq + (int64_t)g * G + r % G) * D;
+    constexpr int LOAD_WARP = kPrSoft / 32, MMA_WARP = LOAD_WARP + 2;
+
+    if (nt > 0) {
+        if (tid < kPrSoft) {
+            const uint16_t *qrow = a.q + qrow_off;
+            uint8_t *qdst = smem + qa * L::Q_TILE;
+            uint4 qv[D / 8];
+#pragma unroll
+            for (int ch = 0; ch < D / 8; ++ch)
+                qv[ch] = row_ok ? *reinterpret_cast<const uint4 *>(qrow + ch * 8) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int ch = 0; ch < D / 8; ++ch) {
+                uint4 x = qv[ch];
+                x.x = (x.x ^ a.q_xor) & a.q_and;
+                x.y = (x.y ^ a.q_xor) & a.q_and;
+                x.z = (x.z ^ a.q_xor) & a.q_and;
+                x.w = (x.w ^ a.q_xor) & a.q_and;
+                *reinterpret_cast<uint4 *>(qdst + (ch / 8) * L::Q_HALF + swz(r, ch % 8)) = x;
+            }
+            fence_proxy_async_smem();
+            mbar_arrive(bar(Q_READY));
+        }
+        if (warp == LOAD_WARP || warp == LOAD_WARP + 1) {
+            // ---- TMA producer warps, one of K and one of V: one box per lane ----
+            const bool is_v = warp != LOAD_WARP;
+            const uint64_t pol = l2_policy_evict_normal();
+            constexpr int NBOX = kPrKeys / kTile * HALVES;
+            const int full0 = is_v ? FULL_V : FULL_K, empty0 = is_v ? EMPTY_V : EMPTY_K;
+            const int j = lane / HALVES, h = lane % HALVES;
+            // pool row of this lane's box of tile t: -1 outside the pool, -2 not wanted
+            auto box_row = [&](int t) {
+                const int32_t tok = key0(t) + j * kTile;
+                if (lane >= NBOX || t >= nt || !seen_by_any(tok, kTile)) return -2;
+                const int32_t y = pr_pool_row(a, w.s, g, tok);
+                return y < 0 ? -1 : y + (is_v ? a.Hkv * a.bs : 0);
+            };
+            int32_t y = box_row(0);
+            for (int t = 0; t < nt; ++t) {
+                const int st = t % kPrStages;
+                const int32_t y_next = box_row(t + 1);
+                const bool bad = __any_sync(0xffffffffu, y == -1);
+                const uint32_t n = __popc(__ballot_sync(0xffffffffu, y >= 0));
+                const uint32_t full = bar(full0 + st);
+                if (t >= kPrStages) wait_phase(bar(empty0 + st), (uint32_t)(t / kPrStages - 1) & 1u, a.err, dead);
+                if (lane == 0) {
+                    if (bad || n == 0) {
+                        if (bad) report(a.err, KV_ERR_DEVICE_BOUNDS);
+                        mbar_arrive(full);  // complete the phase without data
+                    } else {
+                        mbar_arrive_expect_tx(full, n * kHalfBytes);
+                    }
+                }
+                __syncwarp();
+                if (!bad && y >= 0)
+                    tma_load_2d(sbase + L::ST_OFF + st * L::STAGE + (is_v ? L::KV_TILE : 0) + h * L::KV_HALF +
+                                    j * (kTile * 128),
+                                &tmap, h * 64, y, full, pol);
+                __syncwarp();
+                y = y_next;
+            }
+            // drain: the last stages' loads have landed
+            if (lane == 0)
+                for (int t = max(0, nt - kPrStages); t < nt; ++t)
+                    wait_phase(bar(full0 + t % kPrStages), (uint32_t)(t / kPrStages) & 1u, a.err, dead);
+        } else if (warp == MMA_WARP) {
+            // ---- MMA issuer: S_0(0) S_1(0) | PV_0(t) S_0(t+1) PV_1(t) S_1(t+1) | ... ; the
+            // pipe runs one thread's MMAs in issue order, so S_a(t+1) overwrites P
+            // only after PV_a(t) has read it ----
+            const uint32_t el = elect_one();
+            constexpr uint32_t ID_S = idesc_bf16_f32(kPrRows, kPrKeys, 0, 0);
+            constexpr uint32_t ID_O = idesc_bf16_f32(kPrRows, D, 0, 1);
+            auto issue_s = [&](int t_, int t) {
+                const uint32_t ka = sbase + L::ST_OFF + (t % kPrStages) * L::STAGE;
+                const uint32_t q_ = sbase + t_ * L::Q_TILE;
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk)
+                    umma_bf16(tbase + t_ * kPrTmemCols, smem_desc_sw128(q_ + (kk / 4) * L::Q_HALF + (kk % 4) * 32, 16, 1024),
+                              smem_desc_sw128(ka + (kk / 4) * L::KV_HALF + (kk % 4) * 32, 16, 1024), ID_S, kk > 0, el);
+                umma_commit(s_full(t_), el);
+            };
+            auto issue_pv = [&](int t_, int t, int half) {
+                const uint32_t va = sbase + L::ST_OFF + (t % kPrStages) * L::STAGE + L::KV_TILE;
+                constexpr int STEPS = kPrKeys / 2 / 16;
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i) {
+                    const int kk = half * STEPS + i;
+                    umma_bf16_tmem_a(tbase + t_ * kPrTmemCols + O_COL, tbase + t_ * kPrTmemCols + kk * 8,
+                                     smem_desc_sw128(va + kk * (16 * 128), L::KV_HALF, 1024), ID_O, t > 0 || kk > 0, el);
+                }
+            };
+            wait_phase(bar(Q_READY), 0u, a.err, dead);
+            wait_phase(bar(FULL_K + 0), 0u, a.err, dead);
+            tc_fence_after();
+            for (int t_ = 0; t_ < nqt; ++t_) issue_s(t_, 0);
+            umma_commit(bar(EMPTY_K + 0), el);
+            for (int t = 0; t < nt; ++t) {
+                const bool next = t + 1 < nt;
+                for (int t_ = 0; t_ < nqt; ++t_) {
+                    if (t_ == 0)
+                        wait_phase(bar(FULL_V + t % kPrStages), (uint32_t)(t / kPrStages) & 1u, a.err, dead);
+                    wait_phase(p_full(t_, 0), (uint32_t)t & 1u, a.err, dead);
+                    tc_fence_after();
+                    issue_pv(t_, t, 0);
+                    wait_phase(p_full(t_, 1), (uint32_t)t & 1u, a.err, dead);
+                    tc_fence_after();
+                    issue_pv(t_, t, 1);
+                    umma_commit(o_done(t_), el);
+                    if (t_ == nqt - 1) umma_commit(bar(EMPTY_V + t % kPrStages), el);
+                    if (next) {
+                        if (t_ == 0)
+                            wait_phase(bar(FULL_K + (t + 1) % kPrStages), (uint32_t)((t + 1) / kPrStages) & 1u, a.err,
+                                       dead);
+                        tc_fence_after();
+                        issue_s(t_, t + 1);
+                        if (t_ == nqt - 1) umma_commit(bar(EMPTY_K + (t + 1) % kPrStages), el);
+                    }
+                }
+            }
+            // every MMA has completed before TMEM is released
+            umma_commit(bar(FIN), el);
+            wait_phase(bar(FIN), 0u, a.err, dead);
+        }
+    }
+    if (tid < kPrSoft && qa < nqt) {
+        const int p = w.p0 + itok;  // this row's position
+        const uint32_t trow = tbase + qa * kPrTmemCols + ((uint32_t)((warp % 4) * 32) << 16);
+        const float scale = a.qk_scale;
+        float m_run = kMaxStart, l_run = 0.f;
+        int n_masked = 0;
+        for (int t = 0; t < nt; ++t) {
+            const int k0 = key0(t);
+            const bool mk = masked(k0);
+            wait_phase(s_full(qa), (uint32_t)t & 1u, a.err, dead);
+            __syncwarp();
+            tc_fence_after();
+            if (mk && qa == 0) {
+                // rows of V that no query sees, or that hold a NaN or an
+                // infinity, are cleared; the latter noted
+                wait_phase(bar(FULL_V + t % kPrStages), (uint32_t)(t / kPrStages) & 1u, a.err, dead);
+                uint8_t *v = smem + L::ST_OFF + (t % kPrStages) * L::STAGE + L::KV_TILE + r * 128;
+                const bool any = seen_by_any(k0 + r, 1);
+                uint32_t odd = 0;
+                if (any) {
+#pragma unroll
+                    for (int c = 0; c < D / 8; ++c) {
+                        const uint4 x = *reinterpret_cast<const uint4 *>(v + (c / 8) * L::KV_HALF + ((c ^ r) & 7) * 16);
+                        constexpr uint32_t E = 0x7F807F80u;
+                        odd |= __vcmpeq2(x.x & E, E) | __vcmpeq2(x.y & E, E) | __vcmpeq2(x.z & E, E) |
+                               __vcmpeq2(x.w & E, E);
+                    }
+                }
+                if (!any || odd)
+#pragma unroll
+                    for (int c = 0; c < D / 8; ++c)
+                        *reinterpret_cast<uint4 *>(v + (c / 8) * L::KV_HALF + ((c ^ r) & 7) * 16) =
+                            make_uint4(0u, 0u, 0u, 0u);
+                __syncwarp();
+                const uint32_t bits = __ballot_sync(0xffffffffu, odd != 0);
+                if (lane == 0) note[n_masked * 4 + warp] = bits;
+                if (tid == 0) note_key[n_masked] = k0;
+                ++n_masked;
+                fence_proxy_async_smem();
+                __syncwarp();
+            }
+            // tokens of the tile that this row sees: [.., hi] and (> wl or < sk)
+            const int hi = p - k0, wl = a.window > 0 ? hi - a.window : -1, sk = a.sinks - k0;
+            auto load = [&](int cp, uint32_t (&v)[2][32]) {
+                tmem_ld32(trow + cp * 64, v[0]);
+                tmem_ld32(trow + cp * 64 + 32, v[1]);
+                tmem_wait_ld();
+                if (mk)
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) {
+                        const int k = cp * 64 + i;
+                        if (k > hi || (k <= wl && k >= sk)) v[i >> 5][i & 31] = 0xff800000u;  // -inf
+                    }
+            };
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            uint32_t v[2][32];
+#pragma unroll
+            for (int cp = 1; cp >= 0; --cp) {
+                load(cp, v);
+#pragma unroll
+                for (int i = 0; i < 64; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(v[i >> 5][i & 31]));
+            }
+            const float cmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+            // (a warp's lanes read and write TMEM together: all rows of a warp are
+            // scaled when one of them asks for it, the others by 1)
+            const bool rise = cmax > m_run + 8.f;
+            if (__any_sync(0xffffffffu, rise)) {
+                const float al = rise ? fast_exp2(m_run - cmax) : 1.f;  // 0 when nothing came before
+                l_run *= al;
+                if (t >= 1) {
+                    uint32_t o[32];
+#pragma unroll
+                    for (int cb = 0; cb < D / 32; ++cb) {
+                        tmem_ld32(trow + O_COL + cb * 32, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * al);
+                        tmem_st32(trow + O_COL + cb * 32, o);
+                    }
+                }
+                if (rise) m_run = cmax;
+                __syncwarp();
+            }
+#pragma unroll
+            for (int cp = 0; cp < 2; ++cp) {
+                if (cp > 0) load(cp, v);  // the first half's scores are still in v
+                uint32_t pw[32];
+                float r4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < 64; i += 2) {
+                    const uint32_t(&x)[32] = v[i >> 5];
+                    const float p0 = fast_exp2(fmaf(__uint_as_float(x[i & 31]), scale, -m_run));
+                    const float p1 = fast_exp2(fmaf(__uint_as_float(x[(i + 1) & 31]), scale, -m_run));
+                    r4[(i >> 1) & 3] += p0 + p1;
+                    pw[i / 2] = pr_pack(p0, p1);
+                }
+                l_run += (r4[0] + r4[1]) + (r4[2] + r4[3]);
+                tmem_st32(trow + cp * 32, pw);
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(p_full(qa, cp));
+            }
+        }
+        // ---- the rows' outputs, or this split's records ----
+        if (nt > 0) wait_phase(o_done(qa), (uint32_t)(nt - 1) & 1u, a.err, dead);
+        __syncwarp();
+        tc_fence_after();
+        if (tid == 0) *n_notes = n_masked;
+        asm volatile("bar.sync 1, %0;" ::"r"(nqt * 128) : "memory");  // Q tile 0's notes
+        const int notes = *n_notes;
+        const bool blind = p < 0;  // the row sees nothing: zeros
+        const float inv = blind || nt == 0 ? 0.f : 1.f / l_run;
+        const bool rec = a.KS > 1;
+        // Through shared memory, 128 bytes of a row at a time, so that eight
+        // lanes write 128 consecutive bytes; the buffer is the stage that the
+        // last key tile did not use.
+        uint8_t *xb = smem + L::ST_OFF + (nt % kPrStages) * L::STAGE + warp * (32 * 128);
+        const int64_t rec_i = ((int64_t)ks * a.T + w.row0 + itok) * Hq + (int64_t)g * G + r % G;
+        float *recp = a.ws + rec_i * pr_record<D>();
+        const unsigned long long orow =
+            !row_ok || dead ? 0ull
+                            : rec ? reinterpret_cast<unsigned long long>(recp)
+                                  : reinterpret_cast<unsigned long long>(a.out + qrow_off);
+        auto chunk = [&](int cb, uint32_t (&o)[32]) {  // columns 32 cb .. 32 cb + 31 of O, noted tokens added
+            if (nt == 0) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = 0u;
+                return;
+            }
+            tmem_ld32(trow + O_COL + cb * 32, o);
+            tmem_wait_ld();
+            for (int b = 0; b < notes; ++b)
+                for (int q4 = 0; q4 < 4; ++q4)
+                    for (uint32_t bits = note[b * 4 + q4]; bits; bits &= bits - 1) {
+                        const int tok = note_key[b] + q4 * 32 + __ffs((int)bits) - 1;
+                        if (!row_ok || tok > p || (a.window > 0 && tok <= p - a.window && tok >= a.sinks)) continue;
+                        const int32_t y = pr_pool_row(a, w.s, g, tok);
+                        if (y < 0) continue;
+                        const uint16_t *kr = a.pool + (int64_t)y * D, *vr = kr + (int64_t)a.Hkv * a.bs * D;
+                        float s = 0.f;
+                        for (int e = 0; e < D; ++e)
+                            s = fmaf(bf_lo((a.q[qrow_off + e] ^ (a.q_xor & 0xffffu)) & a.q_and), bf_lo(kr[e]), s);
+                        const float pj = fast_exp2(fmaf(s, scale, -m_run));
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            o[i] = __float_as_uint(fmaf(pj, bf_lo(vr[cb * 32 + i]), __uint_as_float(o[i])));
+                    }
+            __syncwarp();
+        };
+        auto send = [&](int part, const uint4 (&x)[8]) {  // 128 bytes of each row
+#pragma unroll
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4 *>(xb + lane * 128 + ((i ^ (lane & 7)) * 16)) = x[i];
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int rr = i * 4 + lane / 8, ch = lane % 8;
+                const unsigned long long dst = __shfl_sync(0xffffffffu, orow, rr);
+                const uint4 y = *reinterpret_cast<const uint4 *>(xb + rr * 128 + ((ch ^ (rr & 7)) * 16));
+                if (dst) *reinterpret_cast<uint4 *>(dst + part * 128 + ch * 16) = y;
+            }
+            __syncwarp();
+        };
+        uint32_t o[32];
+        uint4 x[8];
+        if (rec) {
+#pragma unroll
+            for (int cb = 0; cb < D / 32; ++cb) {
+                chunk(cb, o);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                send(cb, x);
+            }
+            if (orow) {
+                recp[D] = blind || nt == 0 ? -INFINITY : m_run;
+                recp[D + 1] = l_run;
+            }
+        } else {
+#pragma unroll
+            for (int cb = 0; cb < D / 32; ++cb) {
+                chunk(cb, o);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float f0 = __uint_as_float(o[8 * i + 2 * e]), f1 = __uint_as_float(o[8 * i + 2 * e + 1]);
+                        y[e] = blind ? 0u : pr_pack(f0 * inv, f1 * inv);
+                    }
+                    x[(cb & 1) * 4 + i] = make_uint4(y[0], y[1], y[2], y[3]);
+                }
+                if (cb & 1) send(cb / 2, x);
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 0) tmem_dealloc(tbase, kPrTiles * kPrTmemCols);
+}
+
+// Merge of the KS records of each (row, query head): a warp each, D / 32
+// columns a lane.  A row without records (no split saw anything) is zero.
+template <int D>
+__global__ void __launch_bounds__(256) prompt_merge_kernel(const float *ws, uint16_t *out, int64_t n_rows, int KS)
+{
+    grid_dependency_wait();
+    grid_launch_dependents();
+    constexpr int C = D / 32;
+    const int64_t i = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+    const int lane = threadIdx.x & 31;
+    if (i >= n_rows) return;
+    float M = -INFINITY, L = 0.f, O[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) O[c] = 0.f;
+    for (int k = 0; k < KS; ++k) {
+        const float *rec = ws + ((int64_t)k * n_rows + i) * pr_record<D>();
+        const float m = rec[D], l = rec[D + 1];
+        if (m == -INFINITY) continue;
+        const float Mn = fmaxf(M, m), sa = fast_exp2(M - Mn), sb = fast_exp2(m - Mn);
+        L = fmaf(L, sa, l * sb);
+#pragma unroll
+        for (int c = 0; c < C; ++c) O[c] = fmaf(O[c], sa, rec[lane * C + c] * sb);
+        M = Mn;
+    }
+    const float inv = M == -INFINITY ? 0.f : 1.f / L;
+    uint32_t y[C / 2];
+#pragma unroll
+    for (int c = 0; c < C / 2; ++c) y[c] = pr_pack(O[2 * c] * inv, O[2 * c + 1] * inv);
+    uint32_t *dst = reinterpret_cast<uint32_t *>(out + i * D + lane * C);
+#pragma unroll
+    for (int c = 0; c < C / 2; ++c) dst[c] = y[c];
+}
+
+template <int D>
+inline size_t prompt_smem_bytes() { return 1024 + (size_t)PrSmem<D>::BYTES; }
+
+}  // namespace kvp

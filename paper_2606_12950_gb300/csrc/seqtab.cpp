@@ -10,6 +10,7 @@
 #include <cstring>
 #include <vector>
 
+#include "pages_internal.h"
 #include "pool_internal.h"
 #include "seqtab_internal.h"
 
@@ -28,7 +29,35 @@ void set_entry(kv_seqtab *t, int s, int i, int32_t v)
     }
 }
 
+// Give up the blocks of entries [lo, hi) of slot s: one reference each, the
+// entries -1.  Entries that kv_seq_evict has given up already are -1 and
+// passed over.  *n_given (may be null) receives how many were not.
+int give_up(kv_seqtab *t, int s, int lo, int hi, int32_t *n_given)
+{
+    const int32_t *row = &t->table[(size_t)s * t->max_blocks];
+    int32_t n = 0;
+    if (std::find(row + lo, row + hi, -1) == row + hi) {
+        int rc = kv_free_blocks(t->pool, t->layout, hi - lo, row + lo);
+        if (rc) return rc;
+        n = hi - lo;
+    } else {
+        std::vector<int32_t> ids;
+        for (int i = lo; i < hi; ++i)
+            if (row[i] >= 0) ids.push_back(row[i]);
+        n = (int32_t)ids.size();
+        int rc = n ? kv_free_blocks(t->pool, t->layout, n, ids.data()) : KV_OK;
+        if (rc) return rc;
+    }
+    for (int i = lo; i < hi; ++i)
+        if (row[i] >= 0) set_entry(t, s, i, -1);
+    t->counters.blocks_held -= n;
+    if (n_given) *n_given = n;
+    return KV_OK;
+}
+
 }  // namespace
+
+void kvp_seqtab_set_entry(kv_seqtab *t, int s, int i, int32_t v) { set_entry(t, s, i, v); }
 
 void kvp_seqtab_detach(kv_seqtab *t) { t->pool = nullptr; }
 
@@ -65,10 +94,8 @@ int kv_seq_release(kv_seqtab *t, int s)
     if (!slot_ok(t, s)) return KV_ERR_INVALID_ARG;
     const int h = t->held[(size_t)s];
     if (h > 0) {
-        int rc = kv_free_blocks(t->pool, t->layout, h, &t->table[(size_t)s * t->max_blocks]);
+        int rc = give_up(t, s, 0, h, nullptr);
         if (rc) return rc;
-        for (int i = 0; i < h; ++i) set_entry(t, s, i, -1);
-        t->counters.blocks_held -= h;
     }
     t->held[(size_t)s] = 0;
     t->lens[(size_t)s] = 0;
@@ -181,12 +208,21 @@ int kv_seq_trim(kv_seqtab *t, int s)
     const int keep = (t->lens[(size_t)s] + t->bs - 1) / t->bs;
     const int h = t->held[(size_t)s];
     if (h <= keep) return KV_OK;
-    int rc = kv_free_blocks(t->pool, t->layout, h - keep, &t->table[(size_t)s * t->max_blocks + keep]);
+    int rc = give_up(t, s, keep, h, nullptr);
     if (rc) return rc;
-    for (int i = keep; i < h; ++i) set_entry(t, s, i, -1);
     t->held[(size_t)s] = keep;
-    t->counters.blocks_held -= h - keep;
     return KV_OK;
+}
+
+int kv_seq_evict(kv_seqtab *t, int s, int window, int sinks, int32_t *n_freed)
+{
+    if (!slot_ok(t, s) || window < 1 || sinks < 0) return KV_ERR_INVALID_ARG;
+    if (n_freed) *n_freed = 0;
+    // tokens in [sinks, len - window) are seen by no query from position len - 1 on
+    const int first = (int)(((int64_t)sinks + t->bs - 1) / t->bs);
+    const int last = (int)std::max<int64_t>(0, ((int64_t)t->lens[(size_t)s] - window) / t->bs);
+    if (first >= last) return KV_OK;
+    return give_up(t, s, first, last, n_freed);
 }
 
 int kv_seq_replace(kv_seqtab *t, int n, const int32_t *slots, const int64_t *reserve_tokens,

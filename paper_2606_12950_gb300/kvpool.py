@@ -144,6 +144,18 @@ class kv_attn_batch(ctypes.Structure):
                 ("ws_bytes", ctypes.c_size_t)]
 
 
+class kv_rotary_desc(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("scaling", ctypes.c_int32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("low_turns", ctypes.c_double), ("high_turns", ctypes.c_double),
+                ("original_len", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class kv_rotary(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("steps", ctypes.c_void_p),
+                ("magnitude", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+KV_ROTARY_PLAIN, KV_ROTARY_LINEAR, KV_ROTARY_BY_PARTS = 0, 1, 2
 KV_ENGINE_IDLE, KV_ENGINE_SLEEPING, KV_ENGINE_SLEEP_PENDING, KV_ENGINE_ACTIVE, KV_ENGINE_COLD = 0, 1, 2, 3, 4
 KV_ACT_SLEEP, KV_ACT_EVICT, KV_ACT_STOP, KV_ACT_PREEMPT, KV_ACT_ABORT = 1, 2, 3, 4, 5
 
@@ -191,6 +203,16 @@ def lib() -> ctypes.CDLL:
             "kv_budget_used": [P, ctypes.POINTER(U64)],
             "paged_decode_attn_cascade": [P, I, P, P, P, P, P, P, I, I, I, F, P, I, P, P, SZ, P],
             "paged_decode_attn_cascade_seqtab": [P, P, P, P, P, P, P, P, I, I, F, P, I, P, P, SZ, P],
+            "kv_pool_compact": [P, I, P, ctypes.POINTER(I)],
+            "kv_copy_blocks": [P, I, I, P, P, P, P],
+            "kv_rotary_freqs": [ctypes.POINTER(kv_rotary_desc), P],
+            "kv_rotary_steps": [P, I, P],
+            "kv_append_rotary": [P, I, P, P, I64, P, P, I64, P, I64, P, P, I, P, P, I, I, I, P],
+            "paged_decode_attn_window": [P, I, P, P, P, P, P, P, I, I, I, F, I, I, I, P, SZ, P],
+            "kv_prompt_workspace_bytes": [P, I, I, I, I, I, I, I, I, ctypes.POINTER(SZ)],
+            "paged_prompt_attn": [P, I, P, P, P, I, I, P, P, I, I, I, F, I, I, P, SZ, P],
+            "kv_seq_evict": [P, I, I, I, ctypes.POINTER(I32)],
+            "kv_seq_fork": [P, I, I, P, P],
             "kv_seqtab_create": [P, I, I, I, ctypes.POINTER(P)],
             "kv_seqtab_destroy": [P],
             "kv_seq_reserve": [P, I, I64],
@@ -319,6 +341,26 @@ def kv_pool_trim(pool) -> int:
     return int(r.value)
 
 
+def kv_pool_compact(pool, max_moves: int = 2**31 - 1, stream=None) -> int:
+    """Move live blocks together so that kv_pool_trim can give memory back;
+    returns the number of blocks moved.  Sync the pool's tables afterwards."""
+    n = ctypes.c_int(0)
+    _check("kv_pool_compact", lib().kv_pool_compact(pool, int(max_moves), _stream(stream), ctypes.byref(n)))
+    return int(n.value)
+
+
+def kv_copy_blocks(pool, layout: int, src, dst, tokens=None, stream=None) -> None:
+    """Copy the first tokens[i] rows (None: all) of block src[i] to block
+    dst[i]; host arrays of one length."""
+    src, dst = _i32(src), _i32(dst)
+    tokens = None if tokens is None else _i32(tokens)
+    if src.ndim != 1 or src.shape != dst.shape or (tokens is not None and tokens.shape != src.shape):
+        raise ValueError("src, dst and tokens must be 1-D and of one length")
+    _check("kv_copy_blocks",
+           lib().kv_copy_blocks(pool, layout, int(src.size), src.ctypes.data, dst.ctypes.data,
+                                None if tokens is None else tokens.ctypes.data, _stream(stream)))
+
+
 def kv_budget_create(limit_bytes: int):
     out = ctypes.c_void_p()
     _check("kv_budget_create", lib().kv_budget_create(int(limit_bytes), ctypes.byref(out)))
@@ -406,6 +448,47 @@ def kv_append(pool, layout: int, k_new, v_new, dev_table, dev_ctx_lens, max_bloc
                                         _addr(dev_ctx_lens), int(max_blocks), int(S), _stream(stream)))
 
 
+def kv_rotary_freqs(rot_dim: int, base: float = 10000.0, scaling: int = KV_ROTARY_PLAIN, factor: float = 1.0,
+                    original_len: int = 0, low_turns: float = 1.0, high_turns: float = 32.0) -> np.ndarray:
+    """Frequencies (radians a position) of the rotated pairs, float64[rot_dim / 2]."""
+    d = kv_rotary_desc(int(rot_dim), int(scaling), float(base), float(factor), float(low_turns), float(high_turns),
+                       int(original_len), 0)
+    out = np.zeros(max(1, int(rot_dim) // 2), dtype=np.float64)
+    _check("kv_rotary_freqs", lib().kv_rotary_freqs(ctypes.byref(d), out.ctypes.data))
+    return out
+
+
+def kv_rotary_steps(inv_freq) -> np.ndarray:
+    """Frequencies as 64-bit fractions of a turn per position, uint64[n]; the
+    caller keeps them on the device for Rotary."""
+    f = np.ascontiguousarray(inv_freq, dtype=np.float64)
+    out = np.zeros(f.size, dtype=np.uint64)
+    _check("kv_rotary_steps", lib().kv_rotary_steps(f.ctypes.data, int(f.size), out.ctypes.data))
+    return out
+
+
+class Rotary:
+    """The rotation of kv_append_rotary, marshalled once: rotated columns,
+    pair layout, device steps (64-bit words of kv_rotary_steps) and magnitude."""
+
+    def __init__(self, rot_dim: int, steps, interleaved: bool = False, magnitude: float = 1.0):
+        self.steps = steps  # kept alive
+        self.struct = kv_rotary(int(rot_dim), int(bool(interleaved)), _addr(steps), float(magnitude), 0)
+        self.address = ctypes.addressof(self.struct)
+
+
+def kv_append_rotary(pool, layout: int, rotary: Rotary, q, q_stride: int, q_out, k, k_stride: int, v, v_stride: int,
+                     positions, q_starts, T: int, dev_table, dev_ctx_lens, max_blocks: int, S: int, Hq: int,
+                     stream=None) -> None:
+    """q and k rotated to their positions, k and v written into the pool
+    (strides in elements; q, or k and v, may be None)."""
+    _check("kv_append_rotary",
+           lib().kv_append_rotary(pool, layout, rotary.address, _addr(q), int(q_stride), _addr(q_out), _addr(k),
+                                  int(k_stride), _addr(v), int(v_stride), _addr(positions), _addr(q_starts), int(T),
+                                  _addr(dev_table), _addr(dev_ctx_lens), int(max_blocks), int(S), int(Hq),
+                                  _stream(stream)))
+
+
 def kv_workspace_bytes(pool, layout: int, S: int, Hq: int, max_blocks: int, num_splits: int = 0) -> int:
     n = ctypes.c_size_t(0)
     _check("kv_workspace_bytes", lib().kv_workspace_bytes(pool, layout, int(S), int(Hq), int(max_blocks),
@@ -435,6 +518,39 @@ def paged_decode_attn_append(pool, layout: int, q, k_new, v_new, out, dev_table,
                                           _addr(dev_table), _addr(dev_ctx_lens), int(max_blocks), int(S),
                                           int(Hq), float(scale), int(num_splits), _addr(workspace),
                                           int(ws_bytes), _stream(stream)))
+
+
+def paged_decode_attn_window(pool, layout: int, q, k_new, v_new, out, dev_table, dev_ctx_lens, max_blocks: int,
+                             S: int, Hq: int, scale: float, window: int, sinks: int, num_splits: int, workspace,
+                             ws_bytes: int, stream=None) -> None:
+    """paged_decode_attn(_append) over the last `window` tokens and the first
+    `sinks` ones (window 0: all); k_new and v_new may be None."""
+    _check("paged_decode_attn_window",
+           lib().paged_decode_attn_window(pool, layout, _addr(q), _addr(k_new), _addr(v_new), _addr(out),
+                                          _addr(dev_table), _addr(dev_ctx_lens), int(max_blocks), int(S), int(Hq),
+                                          float(scale), int(window), int(sinks), int(num_splits), _addr(workspace),
+                                          int(ws_bytes), _stream(stream)))
+
+
+def kv_prompt_workspace_bytes(pool, layout: int, S: int, Hq: int, T: int, max_q: int, max_blocks: int, window: int,
+                              sinks: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check("kv_prompt_workspace_bytes",
+           lib().kv_prompt_workspace_bytes(pool, layout, int(S), int(Hq), int(T), int(max_q), int(max_blocks),
+                                           int(window), int(sinks), ctypes.byref(n)))
+    return int(n.value)
+
+
+def paged_prompt_attn(pool, layout: int, q, out, q_starts, T: int, max_q: int, dev_table, dev_ctx_lens,
+                      max_blocks: int, S: int, Hq: int, scale: float, window: int, sinks: int, workspace,
+                      ws_bytes: int, stream=None) -> None:
+    """Causal attention of ragged prompt chunks over the pool, with a sliding
+    window and sinks (window 0: the whole context)."""
+    _check("paged_prompt_attn",
+           lib().paged_prompt_attn(pool, layout, _addr(q), _addr(out), _addr(q_starts), int(T), int(max_q),
+                                   _addr(dev_table), _addr(dev_ctx_lens), int(max_blocks), int(S), int(Hq),
+                                   float(scale), int(window), int(sinks), _addr(workspace), int(ws_bytes),
+                                   _stream(stream)))
 
 
 def paged_decode_attn_seqtab(pool, seqtab, q, k_new, v_new, out, dev_table, dev_ctx_lens, S: int, Hq: int,
@@ -578,6 +694,19 @@ class SeqTab:
 
     def trim(self, s: int) -> None:
         _check("kv_seq_trim", lib().kv_seq_trim(self.handle, int(s)))
+
+    def evict(self, s: int, window: int, sinks: int) -> int:
+        """Give up slot s's blocks that the window and the sinks no longer
+        reach; returns how many."""
+        n = ctypes.c_int32(0)
+        _check("kv_seq_evict", lib().kv_seq_evict(self.handle, int(s), int(window), int(sinks), ctypes.byref(n)))
+        return int(n.value)
+
+    def fork(self, src: int, dsts, stream=None) -> None:
+        """Each empty slot of dsts takes slot src's context: full blocks by
+        reference, a partial last one as its own copy on `stream`."""
+        a = _i32(dsts)
+        _check("kv_seq_fork", lib().kv_seq_fork(self.handle, int(src), int(a.size), a.ctypes.data, _stream(stream)))
 
     def replace(self, slots, reserve_tokens, lens) -> np.ndarray:
         """Release each listed slot, then reserve and set the length of its
