@@ -67,6 +67,11 @@ int prompt_run(const CUtensorMap *tmap, const kvp::PromptArgs &a, cudaStream_t s
         if (cudaFuncSetAttribute(kvp::prompt_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
             cudaSuccess)
             return KV_ERR_CUDA;
+        // the warpgroups' register shares wait for what the launch holds: no
+        // launch without it
+        cudaFuncAttributes at;
+        if (cudaFuncGetAttributes(&at, kvp::prompt_attn_kernel<D>) != cudaSuccess || at.numRegs != kvp::kPrRegsLaunch)
+            return KV_ERR_CUDA;
         attr_set.store(true);
     }
     cudaLaunchAttribute attr[1];

@@ -38,7 +38,11 @@ constexpr int kPrTiles = 2;    // Q tiles per CTA
 constexpr int kPrKeys = 128;   // keys per tile: S's N, P.V's K
 constexpr int kPrStages = 2;
 constexpr int kPrSoft = kPrTiles * 128;     // softmax threads, one per row
-constexpr int kPrThreads = kPrSoft + 96;    // + K and V load warps, MMA warp
+constexpr int kPrThreads = kPrSoft + 128;   // + K and V load warps, MMA warp, one to fill the warpgroup
+// Registers a thread, by warpgroup: launched with 168; a softmax thread holds a
+// row's 128 scores, the others need few.  2 x 128 x 200 + 128 x 104 = 384 x 168.
+constexpr int kPrRegsLaunch = 168, kPrRegsSoft = 200, kPrRegsOther = 104;
+static_assert(kPrSoft * kPrRegsSoft + 128 * kPrRegsOther <= kPrThreads * kPrRegsLaunch, "what the launch holds");
 constexpr int kPrMasked = 16;  // masked tiles of a CTA: 3 on the diagonal, 3 at the window's edge, 2 of sinks at most
 constexpr int kPrMaxSplits = 16;
 // TMEM per Q tile: S [0, 128) fp32, P over S's first 64 columns (bf16 pairs), O [128, 128 + d)
@@ -167,6 +171,27 @@ __device__ __forceinline__ int32_t pr_pool_row(const PromptArgs &a, int s, int g
     return (int32_t)((int64_t)phys * a.rows_per_page + (int64_t)g * a.bs + (tok - blk * a.bs));
 }
 
+// bits 0 .. n of a word (none for n < 0, all from 31 on)
+__device__ __forceinline__ uint32_t pr_bits(int n) { return n < 0 ? 0u : 0xffffffffu >> (31 - min(n, 31)); }
+// 32 scores of a row: those of unseen tokens to -inf (column k is seen when
+// k <= hi and not wl >= k >= sk).  The columns' bits first, then a select each:
+// what a masked tile executes is fetched anew by every CTA, and with the
+// comparisons per column it took 16000 clocks, 2500 unmasked.
+__device__ __forceinline__ void pr_mask(uint32_t (&x)[32], int hi, int wl, int sk)
+{
+    const uint32_t seen = pr_bits(hi) & ~(pr_bits(wl) & ~pr_bits(sk - 1));
+#pragma unroll
+    for (int k = 0; k < 32; ++k)
+        if (!(seen >> k & 1u)) x[k] = 0xff800000u;
+}
+// and their maximum, in four chains
+__device__ __forceinline__ void pr_max(const uint32_t (&x)[32], float (&mx)[4])
+{
+#pragma unroll
+    for (int k = 0; k < 32; k += 2)
+        mx[(k >> 1) & 3] = fmaxf(fmaxf(mx[(k >> 1) & 3], __uint_as_float(x[k])), __uint_as_float(x[k + 1]));
+}
+
 template <int D>
 __global__ void __launch_bounds__(kPrThreads, 1)
 prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ PromptArgs a)
@@ -242,27 +267,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
     const int64_t qrow_off = ((int64_t)(w.row0 + itok) * Hq + (int64_t)g * G + r % G) * D;
     constexpr int LOAD_WARP = kPrSoft / 32, MMA_WARP = LOAD_WARP + 2;
 
-    if (nt > 0) {
-        if (tid < kPrSoft) {
-            const uint16_t *qrow = a.q + qrow_off;
-            uint8_t *qdst = smem + qa * L::Q_TILE;
-            uint4 qv[D / 8];
-#pragma unroll
-            for (int ch = 0; ch < D / 8; ++ch)
-                qv[ch] = row_ok ? *reinterpret_cast<const uint4 *>(qrow + ch * 8) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-            for (int ch = 0; ch < D / 8; ++ch) {
-                uint4 x = qv[ch];
-                x.x = (x.x ^ a.q_xor) & a.q_and;
-                x.y = (x.y ^ a.q_xor) & a.q_and;
-                x.z = (x.z ^ a.q_xor) & a.q_and;
-                x.w = (x.w ^ a.q_xor) & a.q_and;
-                *reinterpret_cast<uint4 *>(qdst + (ch / 8) * L::Q_HALF + swz(r, ch % 8)) = x;
-            }
-            fence_proxy_async_smem();
-            mbar_arrive(bar(Q_READY));
-        }
-        if (warp == LOAD_WARP || warp == LOAD_WARP + 1) {
+    if (warp >= LOAD_WARP) {
+        reg_dec<kPrRegsOther>();
+        if (nt == 0) {
+            // nothing to load
+        } else if (warp == LOAD_WARP || warp == LOAD_WARP + 1) {
             // ---- TMA producer warps, one of K and one of V: one box per lane ----
             const bool is_v = warp != LOAD_WARP;
             const uint64_t pol = l2_policy_evict_normal();
@@ -362,198 +371,252 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             umma_commit(bar(FIN), el);
             wait_phase(bar(FIN), 0u, a.err, dead);
         }
-    }
-    if (tid < kPrSoft && qa < nqt) {
-        const int p = w.p0 + itok;  // this row's position
-        const uint32_t trow = tbase + qa * kPrTmemCols + ((uint32_t)((warp % 4) * 32) << 16);
-        const float scale = a.qk_scale;
-        float m_run = kMaxStart, l_run = 0.f;
-        int n_masked = 0;
-        for (int t = 0; t < nt; ++t) {
-            const int k0 = key0(t);
-            const bool mk = masked(k0);
-            wait_phase(s_full(qa), (uint32_t)t & 1u, a.err, dead);
+    } else {
+        reg_inc<kPrRegsSoft>();
+        if (nt > 0) {
+            // whole rows per 16-byte load (a lane reading its own row: 4000
+            // clocks more); rows without a token are zero
+            uint8_t *qdst = smem + qa * L::Q_TILE;
+            constexpr int CPR = D / 8, RPI = 32 / CPR;  // chunks of a row, rows a load
+            const int64_t mine = row_ok ? qrow_off : -1;
+#pragma unroll 1
+            for (int i0 = 0; i0 < 32 / RPI; i0 += 8) {
+                uint4 x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int64_t off = __shfl_sync(0xffffffffu, mine, (i0 + i) * RPI + lane / CPR);
+                    x[i] = off >= 0 ? *reinterpret_cast<const uint4 *>(a.q + off + lane % CPR * 8)
+                                    : make_uint4(0u, 0u, 0u, 0u);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int rr = (warp % 4) * 32 + (i0 + i) * RPI + lane / CPR, ch = lane % CPR;
+                    x[i].x = (x[i].x ^ a.q_xor) & a.q_and;
+                    x[i].y = (x[i].y ^ a.q_xor) & a.q_and;
+                    x[i].z = (x[i].z ^ a.q_xor) & a.q_and;
+                    x[i].w = (x[i].w ^ a.q_xor) & a.q_and;
+                    *reinterpret_cast<uint4 *>(qdst + (ch / 8) * L::Q_HALF + swz(rr, ch % 8)) = x[i];
+                }
+            }
+            fence_proxy_async_smem();
+            mbar_arrive(bar(Q_READY));
+        }
+        if (qa < nqt) {
+            const int p = w.p0 + itok;  // this row's position
+            const uint32_t trow = tbase + qa * kPrTmemCols + ((uint32_t)((warp % 4) * 32) << 16);
+            const float scale = a.qk_scale;
+            float m_run = kMaxStart, l_run = 0.f;
+            int n_masked = 0;
+            for (int t = 0; t < nt; ++t) {
+                const int k0 = key0(t);
+                const bool mk = masked(k0);
+                wait_phase(s_full(qa), (uint32_t)t & 1u, a.err, dead);
+                __syncwarp();
+                tc_fence_after();
+                if (mk && qa == 0) {
+                    // rows of V that no query sees, or that hold a NaN or an
+                    // infinity, are cleared; the latter noted
+                    wait_phase(bar(FULL_V + t % kPrStages), (uint32_t)(t / kPrStages) & 1u, a.err, dead);
+                    uint8_t *v = smem + L::ST_OFF + (t % kPrStages) * L::STAGE + L::KV_TILE + r * 128;
+                    const bool any = seen_by_any(k0 + r, 1);
+                    uint32_t odd = 0;  // a half-word with all exponent bits set: one more carries into its sign bit
+                    if (any)
+#pragma unroll 4
+                        for (int c = 0; c < D / 8; ++c) {
+                            const uint4 x = *reinterpret_cast<const uint4 *>(v + (c / 8) * L::KV_HALF + ((c ^ r) & 7) * 16);
+                            odd |= ((x.x & 0x7fff7fffu) + 0x00800080u) | ((x.y & 0x7fff7fffu) + 0x00800080u) |
+                                   ((x.z & 0x7fff7fffu) + 0x00800080u) | ((x.w & 0x7fff7fffu) + 0x00800080u);
+                        }
+                    odd &= 0x80008000u;
+                    if (!any || odd)
+#pragma unroll 1
+                        for (int c = 0; c < D / 8; ++c)
+                            *reinterpret_cast<uint4 *>(v + (c / 8) * L::KV_HALF + ((c ^ r) & 7) * 16) =
+                                make_uint4(0u, 0u, 0u, 0u);
+                    __syncwarp();
+                    const uint32_t bits = __ballot_sync(0xffffffffu, odd != 0);
+                    if (lane == 0) note[n_masked * 4 + warp] = bits;
+                    if (tid == 0) note_key[n_masked] = k0;
+                    ++n_masked;
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                }
+                // tokens of the tile that this row sees: [.., hi] and (> wl or < sk)
+                const int hi = p - k0, wl = a.window > 0 ? hi - a.window : -1, sk = a.sinks - k0;
+                uint32_t v[4][32];  // the row's scores, then its weights
+                tmem_ld32(trow, v[0]);
+                tmem_ld32(trow + 32, v[1]);
+                tmem_wait_ld();
+                tmem_ld32(trow + 64, v[2]);
+                tmem_ld32(trow + 96, v[3]);
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                if (mk) {
+                    pr_mask(v[0], hi, wl, sk);
+                    pr_mask(v[1], hi - 32, wl - 32, sk - 32);
+                }
+                pr_max(v[0], mx);
+                pr_max(v[1], mx);
+                tmem_wait_ld();
+                if (mk) {
+                    pr_mask(v[2], hi - 64, wl - 64, sk - 64);
+                    pr_mask(v[3], hi - 96, wl - 96, sk - 96);
+                }
+                pr_max(v[2], mx);
+                pr_max(v[3], mx);
+                const float cmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+                // (a warp's lanes read and write TMEM together: all rows of a warp are
+                // scaled when one of them asks for it, the others by 1)
+                const bool rise = cmax > m_run + 8.f;
+                if (__any_sync(0xffffffffu, rise)) {
+                    const float al = rise ? fast_exp2(m_run - cmax) : 1.f;  // 0 when nothing came before
+                    l_run *= al;
+                    if (t >= 1) {
+                        uint32_t o[32];
+#pragma unroll
+                        for (int cb = 0; cb < D / 32; ++cb) {
+                            tmem_ld32(trow + O_COL + cb * 32, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * al);
+                            tmem_st32(trow + O_COL + cb * 32, o);
+                        }
+                    }
+                    if (rise) m_run = cmax;
+                    __syncwarp();
+                }
+                // p = 2^(s * scale - m_run), as bf16 pairs over the first columns of S,
+                // handed over in halves
+                const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(-m_run, -m_run);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t pw[16];
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        float2 y = __ffma2_rn(make_float2(__uint_as_float(v[c][i]), __uint_as_float(v[c][i + 1])), sc2, nm2);
+                        y.x = fast_exp2(y.x);
+                        y.y = fast_exp2(y.y);
+                        pw[i / 2] = pr_pack(y.x, y.y);
+                        v[c][i] = __float_as_uint(y.x);
+                        v[c][i + 1] = __float_as_uint(y.y);
+                    }
+                    tmem_st16(trow + c * 16, pw);
+                    if (c & 1) {
+                        tmem_wait_st();
+                        tc_fence_before();
+                        mbar_arrive(p_full(qa, c / 2));
+                    }
+                }
+                // the weights' sum, while the tensor core works on them
+                float2 r2[4] = {};
+#pragma unroll
+                for (int i = 0; i < 128; i += 2)
+                    r2[(i >> 1) & 3] = __fadd2_rn(r2[(i >> 1) & 3], make_float2(__uint_as_float(v[i >> 5][i & 31]),
+                                                                                 __uint_as_float(v[i >> 5][(i & 31) + 1])));
+                const float2 r1 = __fadd2_rn(__fadd2_rn(r2[0], r2[1]), __fadd2_rn(r2[2], r2[3]));
+                l_run += r1.x + r1.y;
+            }
+            // ---- the rows' outputs, or this split's records ----
+            if (nt > 0) wait_phase(o_done(qa), (uint32_t)(nt - 1) & 1u, a.err, dead);
             __syncwarp();
             tc_fence_after();
-            if (mk && qa == 0) {
-                // rows of V that no query sees, or that hold a NaN or an
-                // infinity, are cleared; the latter noted
-                wait_phase(bar(FULL_V + t % kPrStages), (uint32_t)(t / kPrStages) & 1u, a.err, dead);
-                uint8_t *v = smem + L::ST_OFF + (t % kPrStages) * L::STAGE + L::KV_TILE + r * 128;
-                const bool any = seen_by_any(k0 + r, 1);
-                uint32_t odd = 0;
-                if (any) {
-#pragma unroll
-                    for (int c = 0; c < D / 8; ++c) {
-                        const uint4 x = *reinterpret_cast<const uint4 *>(v + (c / 8) * L::KV_HALF + ((c ^ r) & 7) * 16);
-                        constexpr uint32_t E = 0x7F807F80u;
-                        odd |= __vcmpeq2(x.x & E, E) | __vcmpeq2(x.y & E, E) | __vcmpeq2(x.z & E, E) |
-                               __vcmpeq2(x.w & E, E);
-                    }
-                }
-                if (!any || odd)
-#pragma unroll
-                    for (int c = 0; c < D / 8; ++c)
-                        *reinterpret_cast<uint4 *>(v + (c / 8) * L::KV_HALF + ((c ^ r) & 7) * 16) =
-                            make_uint4(0u, 0u, 0u, 0u);
-                __syncwarp();
-                const uint32_t bits = __ballot_sync(0xffffffffu, odd != 0);
-                if (lane == 0) note[n_masked * 4 + warp] = bits;
-                if (tid == 0) note_key[n_masked] = k0;
-                ++n_masked;
-                fence_proxy_async_smem();
-                __syncwarp();
-            }
-            // tokens of the tile that this row sees: [.., hi] and (> wl or < sk)
-            const int hi = p - k0, wl = a.window > 0 ? hi - a.window : -1, sk = a.sinks - k0;
-            auto load = [&](int cp, uint32_t (&v)[2][32]) {
-                tmem_ld32(trow + cp * 64, v[0]);
-                tmem_ld32(trow + cp * 64 + 32, v[1]);
-                tmem_wait_ld();
-                if (mk)
-#pragma unroll
-                    for (int i = 0; i < 64; ++i) {
-                        const int k = cp * 64 + i;
-                        if (k > hi || (k <= wl && k >= sk)) v[i >> 5][i & 31] = 0xff800000u;  // -inf
-                    }
-            };
-            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            uint32_t v[2][32];
-#pragma unroll
-            for (int cp = 1; cp >= 0; --cp) {
-                load(cp, v);
-#pragma unroll
-                for (int i = 0; i < 64; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(v[i >> 5][i & 31]));
-            }
-            const float cmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
-            // (a warp's lanes read and write TMEM together: all rows of a warp are
-            // scaled when one of them asks for it, the others by 1)
-            const bool rise = cmax > m_run + 8.f;
-            if (__any_sync(0xffffffffu, rise)) {
-                const float al = rise ? fast_exp2(m_run - cmax) : 1.f;  // 0 when nothing came before
-                l_run *= al;
-                if (t >= 1) {
+            if (tid == 0) *n_notes = n_masked;
+            asm volatile("bar.sync 1, %0;" ::"r"(nqt * 128) : "memory");  // Q tile 0's notes
+            const int notes = *n_notes;
+            const bool blind = p < 0;  // the row sees nothing: zeros
+            const float inv = blind || nt == 0 ? 0.f : 1.f / l_run;
+            const bool rec = a.KS > 1;
+            // Through shared memory, 128 bytes of a row at a time, so that eight
+            // lanes write 128 consecutive bytes; the buffer is the stage that the
+            // last key tile did not use.
+            uint8_t *xb = smem + L::ST_OFF + (nt % kPrStages) * L::STAGE + warp * (32 * 128);
+            const int64_t rec_i = ((int64_t)ks * a.T + w.row0 + itok) * Hq + (int64_t)g * G + r % G;
+            float *recp = a.ws + rec_i * pr_record<D>();
+            const unsigned long long orow =
+                !row_ok || dead ? 0ull
+                                : rec ? reinterpret_cast<unsigned long long>(recp)
+                                      : reinterpret_cast<unsigned long long>(a.out + qrow_off);
+            // noted tokens that this row sees: added to O in TMEM
+            bool any_note = false;
+            for (int b = lane; b < notes * 4; b += 32) any_note |= note[b] != 0;
+            if (__any_sync(0xffffffffu, any_note)) {
+#pragma unroll 1
+                for (int cb = 0; cb < D / 32; ++cb) {
                     uint32_t o[32];
+                    tmem_ld32(trow + O_COL + cb * 32, o);
+                    tmem_wait_ld();
+#pragma unroll 1
+                    for (int b = 0; b < notes * 4; ++b)
+                        for (uint32_t bits = note[b]; bits; bits &= bits - 1) {
+                            const int tok = note_key[b / 4] + b % 4 * 32 + __ffs((int)bits) - 1;
+                            if (!row_ok || tok > p || (a.window > 0 && tok <= p - a.window && tok >= a.sinks)) continue;
+                            const int32_t y = pr_pool_row(a, w.s, g, tok);
+                            if (y < 0) continue;
+                            const uint16_t *kr = a.pool + (int64_t)y * D, *vr = kr + (int64_t)a.Hkv * a.bs * D;
+                            float s = 0.f;
+#pragma unroll 1
+                            for (int e = 0; e < D; ++e)
+                                s = fmaf(bf_lo((a.q[qrow_off + e] ^ (a.q_xor & 0xffffu)) & a.q_and), bf_lo(kr[e]), s);
+                            const float pj = fast_exp2(fmaf(s, scale, -m_run));
 #pragma unroll
-                    for (int cb = 0; cb < D / 32; ++cb) {
-                        tmem_ld32(trow + O_COL + cb * 32, o);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * al);
-                        tmem_st32(trow + O_COL + cb * 32, o);
-                    }
+                            for (int i = 0; i < 32; ++i)
+                                o[i] = __float_as_uint(fmaf(pj, bf_lo(vr[cb * 32 + i]), __uint_as_float(o[i])));
+                        }
+                    __syncwarp();
+                    tmem_st32(trow + O_COL + cb * 32, o);
+                    tmem_wait_st();
                 }
-                if (rise) m_run = cmax;
+            }
+            auto send = [&](int part, const uint4 (&x)[8]) {  // 128 bytes of each row
+#pragma unroll
+                for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4 *>(xb + lane * 128 + ((i ^ (lane & 7)) * 16)) = x[i];
                 __syncwarp();
-            }
 #pragma unroll
-            for (int cp = 0; cp < 2; ++cp) {
-                if (cp > 0) load(cp, v);  // the first half's scores are still in v
-                uint32_t pw[32];
-                float r4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < 64; i += 2) {
-                    const uint32_t(&x)[32] = v[i >> 5];
-                    const float p0 = fast_exp2(fmaf(__uint_as_float(x[i & 31]), scale, -m_run));
-                    const float p1 = fast_exp2(fmaf(__uint_as_float(x[(i + 1) & 31]), scale, -m_run));
-                    r4[(i >> 1) & 3] += p0 + p1;
-                    pw[i / 2] = pr_pack(p0, p1);
+                for (int i = 0; i < 8; ++i) {
+                    const int rr = i * 4 + lane / 8, ch = lane % 8;
+                    const unsigned long long dst = __shfl_sync(0xffffffffu, orow, rr);
+                    const uint4 y = *reinterpret_cast<const uint4 *>(xb + rr * 128 + ((ch ^ (rr & 7)) * 16));
+                    if (dst) *reinterpret_cast<uint4 *>(dst + part * 128 + ch * 16) = y;
                 }
-                l_run += (r4[0] + r4[1]) + (r4[2] + r4[3]);
-                tmem_st32(trow + cp * 32, pw);
-                tmem_wait_st();
-                tc_fence_before();
-                mbar_arrive(p_full(qa, cp));
-            }
-        }
-        // ---- the rows' outputs, or this split's records ----
-        if (nt > 0) wait_phase(o_done(qa), (uint32_t)(nt - 1) & 1u, a.err, dead);
-        __syncwarp();
-        tc_fence_after();
-        if (tid == 0) *n_notes = n_masked;
-        asm volatile("bar.sync 1, %0;" ::"r"(nqt * 128) : "memory");  // Q tile 0's notes
-        const int notes = *n_notes;
-        const bool blind = p < 0;  // the row sees nothing: zeros
-        const float inv = blind || nt == 0 ? 0.f : 1.f / l_run;
-        const bool rec = a.KS > 1;
-        // Through shared memory, 128 bytes of a row at a time, so that eight
-        // lanes write 128 consecutive bytes; the buffer is the stage that the
-        // last key tile did not use.
-        uint8_t *xb = smem + L::ST_OFF + (nt % kPrStages) * L::STAGE + warp * (32 * 128);
-        const int64_t rec_i = ((int64_t)ks * a.T + w.row0 + itok) * Hq + (int64_t)g * G + r % G;
-        float *recp = a.ws + rec_i * pr_record<D>();
-        const unsigned long long orow =
-            !row_ok || dead ? 0ull
-                            : rec ? reinterpret_cast<unsigned long long>(recp)
-                                  : reinterpret_cast<unsigned long long>(a.out + qrow_off);
-        auto chunk = [&](int cb, uint32_t (&o)[32]) {  // columns 32 cb .. 32 cb + 31 of O, noted tokens added
-            if (nt == 0) {
+                __syncwarp();
+            };
+            // (rolled: each CTA fetches this code anew)
+            if (rec) {
+#pragma unroll 1
+                for (int cb = 0; cb < D / 32 && nt > 0; ++cb) {
+                    uint32_t o[32];
+                    tmem_ld32(trow + O_COL + cb * 32, o);
+                    tmem_wait_ld();
+                    uint4 x[8];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = 0u;
-                return;
-            }
-            tmem_ld32(trow + O_COL + cb * 32, o);
-            tmem_wait_ld();
-            for (int b = 0; b < notes; ++b)
-                for (int q4 = 0; q4 < 4; ++q4)
-                    for (uint32_t bits = note[b * 4 + q4]; bits; bits &= bits - 1) {
-                        const int tok = note_key[b] + q4 * 32 + __ffs((int)bits) - 1;
-                        if (!row_ok || tok > p || (a.window > 0 && tok <= p - a.window && tok >= a.sinks)) continue;
-                        const int32_t y = pr_pool_row(a, w.s, g, tok);
-                        if (y < 0) continue;
-                        const uint16_t *kr = a.pool + (int64_t)y * D, *vr = kr + (int64_t)a.Hkv * a.bs * D;
-                        float s = 0.f;
-                        for (int e = 0; e < D; ++e)
-                            s = fmaf(bf_lo((a.q[qrow_off + e] ^ (a.q_xor & 0xffffu)) & a.q_and), bf_lo(kr[e]), s);
-                        const float pj = fast_exp2(fmaf(s, scale, -m_run));
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            o[i] = __float_as_uint(fmaf(pj, bf_lo(vr[cb * 32 + i]), __uint_as_float(o[i])));
-                    }
-            __syncwarp();
-        };
-        auto send = [&](int part, const uint4 (&x)[8]) {  // 128 bytes of each row
-#pragma unroll
-            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4 *>(xb + lane * 128 + ((i ^ (lane & 7)) * 16)) = x[i];
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int rr = i * 4 + lane / 8, ch = lane % 8;
-                const unsigned long long dst = __shfl_sync(0xffffffffu, orow, rr);
-                const uint4 y = *reinterpret_cast<const uint4 *>(xb + rr * 128 + ((ch ^ (rr & 7)) * 16));
-                if (dst) *reinterpret_cast<uint4 *>(dst + part * 128 + ch * 16) = y;
-            }
-            __syncwarp();
-        };
-        uint32_t o[32];
-        uint4 x[8];
-        if (rec) {
-#pragma unroll
-            for (int cb = 0; cb < D / 32; ++cb) {
-                chunk(cb, o);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-                send(cb, x);
-            }
-            if (orow) {
-                recp[D] = blind || nt == 0 ? -INFINITY : m_run;
-                recp[D + 1] = l_run;
-            }
-        } else {
-#pragma unroll
-            for (int cb = 0; cb < D / 32; ++cb) {
-                chunk(cb, o);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t y[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float f0 = __uint_as_float(o[8 * i + 2 * e]), f1 = __uint_as_float(o[8 * i + 2 * e + 1]);
-                        y[e] = blind ? 0u : pr_pack(f0 * inv, f1 * inv);
-                    }
-                    x[(cb & 1) * 4 + i] = make_uint4(y[0], y[1], y[2], y[3]);
+                    for (int i = 0; i < 8; ++i) x[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                    send(cb, x);
                 }
-                if (cb & 1) send(cb / 2, x);
+                if (orow) {
+                    recp[D] = blind || nt == 0 ? -INFINITY : m_run;
+                    recp[D + 1] = l_run;
+                }
+            } else {
+#pragma unroll 1
+                for (int cb = 0; cb < D / 64; ++cb) {
+                    uint32_t o[2][32] = {};
+                    if (nt > 0) {
+                        tmem_ld32(trow + O_COL + cb * 64, o[0]);
+                        tmem_ld32(trow + O_COL + cb * 64 + 32, o[1]);
+                        tmem_wait_ld();
+                    }
+                    uint4 x[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        uint32_t y[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int k = 8 * (i % 4) + 2 * e;
+                            y[e] = pr_pack(__uint_as_float(o[i / 4][k]) * inv, __uint_as_float(o[i / 4][k + 1]) * inv);
+                        }
+                        x[i] = blind ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(y[0], y[1], y[2], y[3]);
+                    }
+                    send(cb, x);
+                }
             }
         }
     }

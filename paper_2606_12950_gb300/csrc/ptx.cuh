@@ -162,6 +162,19 @@ __device__ __forceinline__ uint64_t ld_acquire_gpu(const uint64_t *p)
     return v;
 }
 
+// More or fewer registers for every warp of this warpgroup, out of those the
+// block was launched with.
+template <int N>
+__device__ __forceinline__ void reg_inc()
+{
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void reg_dec()
+{
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
 // 2^x (hardware approximation, flush-to-zero).
 __device__ __forceinline__ float fast_exp2(float x)
 {
