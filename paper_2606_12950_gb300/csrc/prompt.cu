@@ -59,7 +59,8 @@ int prompt_shape(const kv_pool *p, int layout, int S, int Hq, int T, int max_q, 
 }
 
 template <int D>
-int prompt_run(const CUtensorMap *tmap, const kvp::PromptArgs &a, cudaStream_t st)
+int prompt_run(const CUtensorMap *tmap, const CUtensorMap &qmap, const kvp::PromptArgs &a, int sm_count,
+               cudaStream_t st)
 {
     static std::atomic<bool> attr_set{false};
     const size_t smem = kvp::prompt_smem_bytes<D>();
@@ -78,13 +79,13 @@ int prompt_run(const CUtensorMap *tmap, const kvp::PromptArgs &a, cudaStream_t s
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.tiles * a.Hkv * a.KS));
+    cfg.gridDim = dim3((unsigned)std::min(a.n_items, sm_count));  // a CTA an SM: its TMEM
     cfg.blockDim = dim3(kvp::kPrThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, kvp::prompt_attn_kernel<D>, *tmap, a) != cudaSuccess) return KV_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, kvp::prompt_attn_kernel<D>, *tmap, qmap, a) != cudaSuccess) return KV_ERR_CUDA;
     kvp_note_stream(st, false);
     if (a.KS == 1) return KV_OK;
     const int64_t rows = (int64_t)a.T * a.Hkv * a.G;
@@ -149,11 +150,16 @@ int paged_prompt_attn(kv_pool *p, int layout, const uint16_t *q, uint16_t *out, 
     const int32_t reach = max_blocks * a.bs;
     a.window = window < reach ? window : 0;  // one that no context outgrows is the whole context
     a.sinks = a.window > 0 ? std::min(sinks, reach) : 0;
-    a.q_xor = scale < 0.f ? 0x80008000u : 0u;
-    a.q_and = scale == 0.f ? 0u : 0xffffffffu;
+    a.n_items = (int32_t)(s.tiles * s.Hkv * s.KS);
+    a.sign = scale > 0.f ? 1.f : scale < 0.f ? -1.f : 0.f;
     a.qk_scale = scale == 0.f ? 1.f : std::fabs(scale) * 1.4426950408889634f;
     const cudaStream_t st = (cudaStream_t)stream;
-    return s.D == 64 ? prompt_run<64>(&p->tmap[layout], a, st) : prompt_run<128>(&p->tmap[layout], a, st);
+    // q as [T][Hq][d]: a box is half the columns of TQ tokens x G heads
+    CUtensorMap qmap;
+    rc = kvp_tmap_3d(&qmap, q, s.D, Hq, T, 64, s.G, kvp::kPrRows / s.G);
+    if (rc) return rc;
+    return s.D == 64 ? prompt_run<64>(&p->tmap[layout], qmap, a, p->sm_count, st)
+                     : prompt_run<128>(&p->tmap[layout], qmap, a, p->sm_count, st);
 }
 
 }  // extern "C"

@@ -4,20 +4,26 @@
 // A query at position p of its sequence sees the tokens j <= p with
 // j > p - window or j < sinks (window 0: all).  The query heads of a KV head
 // share its K and V, so a Q tile's 128 rows are TQ = floor(128 / G)
-// consecutive tokens x G heads of one (sequence, KV head), and a CTA takes two
-// Q tiles (2 TQ tokens) over their common key range, in 128-key tiles:
+// consecutive tokens x G heads of one (sequence, KV head), and an item, the
+// unit of work, is two Q tiles (2 TQ tokens) over their common key range, in
+// 128-key tiles:
 //   S = Q K^T     tcgen05.mma, M = 128 rows, N = 128 keys, fp32 in TMEM
 //   softmax       one thread per row, S read from TMEM, base 2, lazy rescale
 //   O += P V      tcgen05.mma, P (bf16) over S in TMEM, V from shared memory
 // While one Q tile's four warps run the softmax the tensor core works on the
-// other's.  A warp each loads K and V by TMA (16-token boxes, 128-byte
-// swizzle, two stages, released apart), one issues the MMAs.
+// other's.
 //
-// Keys.  A CTA's tiles are those of the sinks, then those from its first
+// CTAs stay and take one item after another, so that the next item's K and V
+// (a warp each, TMA, 16-token boxes, 128-byte swizzle, two stages, released
+// apart) and Q load while the last tiles of the one before are worked on and
+// its output is written.  One warp issues the MMAs; one looks up the next
+// item, loads Q and checks V (below).
+//
+// Keys.  An item's tiles are those of the sinks, then those from its first
 // query's window on up to its last query; a tile in which some query of the
-// CTA does not see some token (the diagonal, the window's edge, the sinks'
+// item does not see some token (the diagonal, the window's edge, the sinks'
 // edge) is masked element by element, the others are not looked at.
-// 16-token boxes that no query of the CTA sees are not loaded: their table
+// 16-token boxes that no query of the item sees are not loaded: their table
 // entries may be gone (kv_seq_evict).
 //
 // NaN and infinities.  A weight of 0 times a NaN is NaN in the MMA.  So in
@@ -25,8 +31,8 @@
 // query sees and that hold a NaN or an infinity are cleared too and noted; at
 // the end each row adds the noted tokens that it sees itself.
 //
-// Few rows (KS > 1): a CTA's key tiles are split over KS CTAs, each leaving per
-// row one fp32 record (o, running max, sum) that prompt_merge_kernel merges.
+// Few rows (KS > 1): an item's key tiles are split over KS items, each leaving
+// per row one fp32 record (o, running max, sum) that prompt_merge_kernel merges.
 #pragma once
 
 #include "attn_impl.cuh"
@@ -34,16 +40,16 @@
 namespace kvp {
 
 constexpr int kPrRows = 128;   // rows of a Q tile: the MMA's M
-constexpr int kPrTiles = 2;    // Q tiles per CTA
+constexpr int kPrTiles = 2;    // Q tiles per item
 constexpr int kPrKeys = 128;   // keys per tile: S's N, P.V's K
 constexpr int kPrStages = 2;
 constexpr int kPrSoft = kPrTiles * 128;     // softmax threads, one per row
-constexpr int kPrThreads = kPrSoft + 128;   // + K and V load warps, MMA warp, one to fill the warpgroup
+constexpr int kPrThreads = kPrSoft + 128;   // + K and V load warps, MMA warp, scheduling warp
 // Registers a thread, by warpgroup: launched with 168; a softmax thread holds a
-// row's 128 scores, the others need few.  2 x 128 x 200 + 128 x 104 = 384 x 168.
-constexpr int kPrRegsLaunch = 168, kPrRegsSoft = 200, kPrRegsOther = 104;
+// row's 128 scores, the others need fewer.  2 x 128 x 216 + 128 x 72 = 384 x 168.
+constexpr int kPrRegsLaunch = 168, kPrRegsSoft = 216, kPrRegsOther = 72;
 static_assert(kPrSoft * kPrRegsSoft + 128 * kPrRegsOther <= kPrThreads * kPrRegsLaunch, "what the launch holds");
-constexpr int kPrMasked = 16;  // masked tiles of a CTA: 3 on the diagonal, 3 at the window's edge, 2 of sinks at most
+constexpr int kPrMasked = 16;  // masked tiles of an item: 3 on the diagonal, 3 at the window's edge, 2 of sinks at most
 constexpr int kPrMaxSplits = 16;
 // TMEM per Q tile: S [0, 128) fp32, P over S's first 64 columns (bf16 pairs), O [128, 128 + d)
 constexpr uint32_t kPrTmemCols = 256;
@@ -62,17 +68,46 @@ struct PromptArgs {
     int32_t pages_per_block;
     int32_t max_blocks;
     int32_t S, Hkv, G, bs, T;
-    int32_t tiles;         // row tiles of the grid, at least those there are
+    int32_t tiles;         // row tiles, at least those there are
+    int32_t n_items;       // tiles * Hkv * KS
     int32_t KS;
     int32_t window, sinks; // window 0: the whole context
-    uint32_t q_xor;        // sign bits flipped in q (a negative scale), and
-    uint32_t q_and;        // 0 where the scale is 0
+    float sign;            // 1, or what the scores are multiplied by first: -1 or 0 with the scale's sign
     float qk_scale;        // |scale| * log2(e) (1 where the scale is 0)
 };
 
 // a record: o[D] unnormalised, m, l, padded to 16 bytes
 template <int D>
 __host__ __device__ constexpr uint32_t pr_record() { return D + 4; }
+
+// An item: tokens [row0, row0 + ntok) of q, positions p0 .. p1 of sequence s,
+// KV head g, and its key tiles.
+struct PrItem {
+    int32_t s;         // -1: no more items
+    int32_t row0;      // q row of its first token
+    int32_t ntok;
+    int32_t p0, p1;    // positions of its first and last token
+    int32_t lo;        // first token of the first query's window
+    int32_t head;      // key tiles of the sinks before the window's tiles
+    int32_t gap;       // key tiles left out between the two
+    int32_t t0, nt;    // the tiles of this split: the first one, how many
+    int32_t g, ks;
+    __device__ __forceinline__ int32_t key0(int32_t t) const
+    {
+        const int32_t i = t0 + t;
+        return (i < head ? i : i + gap) * kPrKeys;
+    }
+    // some query does not see some token of the tile at k0
+    __device__ __forceinline__ bool masked(const PromptArgs &a, int32_t k0) const
+    {
+        return k0 + kPrKeys - 1 > p0 || (a.window > 0 && k0 <= p1 - a.window && k0 + kPrKeys > a.sinks);
+    }
+    // some query sees some token of [tok, tok + n)
+    __device__ __forceinline__ bool sees(const PromptArgs &a, int32_t tok, int32_t n) const
+    {
+        return tok <= p1 && (tok + n > lo || tok < a.sinks);
+    }
+};
 
 // shared memory (offsets from a 1024-byte aligned base)
 template <int D>
@@ -84,11 +119,19 @@ struct PrSmem {
     static constexpr uint32_t Q_HALF = kPrRows * 128;
     static constexpr uint32_t Q_TILE = HALVES * Q_HALF;
     static constexpr uint32_t ST_OFF = kPrTiles * Q_TILE;
-    static constexpr uint32_t BAR_OFF = ST_OFF + kPrStages * STAGE;
-    static constexpr int NBARS = 4 * kPrStages + 4 * kPrTiles + 2;
+    static constexpr uint32_t X_OFF = ST_OFF + kPrStages * STAGE;       // 4 KB per softmax warp for the output
+    static constexpr uint32_t BAR_OFF = X_OFF + kPrSoft / 32 * 4096;
+    static constexpr int NBARS = 32;
     static constexpr uint32_t SLOT_OFF = BAR_OFF + NBARS * 8;
-    static constexpr uint32_t NOTE_OFF = SLOT_OFF + 16;  // per masked tile: its first key, 4 words of noted rows
-    static constexpr uint32_t BYTES = NOTE_OFF + kPrMasked * 5 * 4 + 16;
+    static constexpr uint32_t ITEM_OFF = SLOT_OFF + 16;                 // [2] PrItem
+    static constexpr uint32_t NOTE_OFF = ITEM_OFF + 2 * sizeof(PrItem); // [2] PrNotes
+    static constexpr uint32_t BYTES = NOTE_OFF + 2 * (kPrMasked * 5 + 1) * 4;
+};
+// noted rows of an item's masked tiles
+struct PrNotes {
+    int32_t n;
+    int32_t key0[kPrMasked];
+    uint32_t rows[kPrMasked][4];
 };
 
 __device__ __forceinline__ uint32_t pr_pack(float lo, float hi)
@@ -97,23 +140,14 @@ __device__ __forceinline__ uint32_t pr_pack(float lo, float hi)
     return *reinterpret_cast<uint32_t *>(&v);
 }
 
-// A CTA's share: tokens [i0, i1) of sequence s, its keys.
-struct PrWork {
-    int32_t s;
-    int32_t row0;      // q row of token i0
-    int32_t ntok;      // tokens of this CTA (0: none)
-    int32_t p0, p1;    // positions of its first and last token
-    int32_t lo;        // first token of the first query's window
-    int32_t head;      // key tiles of the sinks before the window's tiles
-    int32_t gap;       // key tiles left out between the two
-    int32_t nt;        // key tiles in all
-    __device__ __forceinline__ int32_t key0(int32_t i) const { return (i < head ? i : i + gap) * kPrKeys; }
-};
-
-// The work of row tile `tile` (each warp for itself, converged).
-__device__ __forceinline__ PrWork pr_work(const PromptArgs &a, int tile, int TT, int lane)
+// Item i (a converged warp); ntok = 0 where there is none.
+__device__ __forceinline__ PrItem pr_item(const PromptArgs &a, int i, int TT, int lane)
 {
-    PrWork w{};
+    PrItem w{};
+    w.ks = i % a.KS;
+    i /= a.KS;
+    w.g = i % a.Hkv;
+    const int tile = a.tiles - 1 - i / a.Hkv;  // the longest key ranges first
     int before = 0;  // row tiles of the sequences before
     for (int s0 = 0; s0 < a.S; s0 += 32) {
         const int s = s0 + lane;
@@ -134,14 +168,13 @@ __device__ __forceinline__ PrWork pr_work(const PromptArgs &a, int tile, int TT,
             w.s = s0 + l;
             const int i0 = (tile - t0) * TT;
             const int32_t st = a.starts[w.s];
+            int32_t n = a.ctx_lens[w.s];
             w.row0 = st + i0;
-            w.ntok = min(TT, nq - i0);
             if (st < 0 || (int64_t)st + nq > a.T) {  // a bad array: nothing of it is touched
                 report(a.err, KV_ERR_DEVICE_BOUNDS);
-                w.ntok = 0;
                 return w;
             }
-            int32_t n = a.ctx_lens[w.s];
+            w.ntok = min(TT, nq - i0);
             const int32_t cap = a.max_blocks * a.bs;
             if (n < nq || n > cap) {
                 report(a.err, KV_ERR_DEVICE_BOUNDS);
@@ -154,7 +187,9 @@ __device__ __forceinline__ PrWork pr_work(const PromptArgs &a, int tile, int TT,
             const int32_t sk = min(a.sinks, w.lo);  // sinks before the window
             w.head = (sk + kPrKeys - 1) / kPrKeys;
             w.gap = max(0, w.lo / kPrKeys - w.head);
-            w.nt = w.p1 / kPrKeys + 1 - w.gap;
+            const int32_t all = w.p1 / kPrKeys + 1 - w.gap;
+            w.t0 = (int32_t)((int64_t)w.ks * all / a.KS);
+            w.nt = (int32_t)((int64_t)(w.ks + 1) * all / a.KS) - w.t0;
             return w;
         }
         before += __shfl_sync(0xffffffffu, incl, 31);
@@ -175,7 +210,7 @@ __device__ __forceinline__ int32_t pr_pool_row(const PromptArgs &a, int s, int g
 __device__ __forceinline__ uint32_t pr_bits(int n) { return n < 0 ? 0u : 0xffffffffu >> (31 - min(n, 31)); }
 // 32 scores of a row: those of unseen tokens to -inf (column k is seen when
 // k <= hi and not wl >= k >= sk).  The columns' bits first, then a select each:
-// what a masked tile executes is fetched anew by every CTA, and with the
+// what a masked tile executes is rarely in the instruction caches, and with the
 // comparisons per column it took 16000 clocks, 2500 unmasked.
 __device__ __forceinline__ void pr_mask(uint32_t (&x)[32], int hi, int wl, int sk)
 {
@@ -183,6 +218,12 @@ __device__ __forceinline__ void pr_mask(uint32_t (&x)[32], int hi, int wl, int s
 #pragma unroll
     for (int k = 0; k < 32; ++k)
         if (!(seen >> k & 1u)) x[k] = 0xff800000u;
+}
+// and times -1 or 0, where the scale is negative or 0
+__device__ __forceinline__ void pr_times(uint32_t (&x)[32], float f)
+{
+#pragma unroll
+    for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * f);
 }
 // and their maximum, in four chains
 __device__ __forceinline__ void pr_max(const uint32_t (&x)[32], float (&mx)[4])
@@ -194,7 +235,8 @@ __device__ __forceinline__ void pr_max(const uint32_t (&x)[32], float (&mx)[4])
 
 template <int D>
 __global__ void __launch_bounds__(kPrThreads, 1)
-prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ PromptArgs a)
+prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap qmap,
+                   const __grid_constant__ PromptArgs a)
 {
     using L = PrSmem<D>;
     constexpr int HALVES = L::HALVES;
@@ -204,35 +246,28 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
     const uint32_t sbase = smem_u32(smem);
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + L::BAR_OFF);
     uint32_t *tslot = reinterpret_cast<uint32_t *>(smem + L::SLOT_OFF);
-    int32_t *note_key = reinterpret_cast<int32_t *>(smem + L::NOTE_OFF);      // [kPrMasked]
-    uint32_t *note = reinterpret_cast<uint32_t *>(note_key + kPrMasked);      // [kPrMasked][4]
-    int32_t *n_notes = reinterpret_cast<int32_t *>(note + kPrMasked * 4);
+    PrItem *items = reinterpret_cast<PrItem *>(smem + L::ITEM_OFF);
+    PrNotes *notes = reinterpret_cast<PrNotes *>(smem + L::NOTE_OFF);
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
-    constexpr int FULL_K = 0, EMPTY_K = kPrStages, FULL_V = 2 * kPrStages, EMPTY_V = 3 * kPrStages;
-    constexpr int QB = 4 * kPrStages, FIN = QB + 4 * kPrTiles, Q_READY = FIN + 1;
-    auto s_full = [&](int t) { return bar(QB + 4 * t); };
-    auto p_full = [&](int t, int half) { return bar(QB + 4 * t + 1 + half); };
-    auto o_done = [&](int t) { return bar(QB + 4 * t + 3); };
+    // K and V of a stage loaded, free (V of a masked tile: loaded is V_RAW, and
+    // FULL_V follows its check); per Q tile: S done, P of keys 64 half .. 64 half + 63 written, O done; an item's Q
+    // loaded, used; an item published, read; its notes complete, read; all MMAs done
+    constexpr int FULL_K = 0, EMPTY_K = 2, FULL_V = 4, EMPTY_V = 6, V_RAW = 8;
+    constexpr int S_FULL = 10, P_FULL = 12, O_DONE = 16, Q_FULL = 18, Q_FREE = 19, ITEM_FULL = 20, ITEM_EMPTY = 22,
+                  NOTED = 24, NOTE_FREE = 26, FIN = 28;
+    static_assert(kPrStages == 2 && kPrTiles == 2 && FIN < L::NBARS, "the barriers' numbers");
 
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const int G = a.G, Hq = a.Hkv * G, TQ = kPrRows / G, TT = kPrTiles * TQ;
-    int bid = blockIdx.x;
-    const int ks = bid % a.KS;
-    bid /= a.KS;
-    const int g = bid % a.Hkv;
-    const int tile = a.tiles - 1 - bid / a.Hkv;  // the longest key ranges first
+    constexpr int K_WARP = kPrSoft / 32, V_WARP = K_WARP + 1, MMA_WARP = K_WARP + 2, PLAN_WARP = K_WARP + 3;
 
     if (tid == 0) {
-        for (int i = 0; i < 4 * kPrStages; ++i) mbar_init(bar(i), 1);
-        for (int t = 0; t < kPrTiles; ++t) {
-            mbar_init(s_full(t), 1);
-            mbar_init(p_full(t, 0), 128);
-            mbar_init(p_full(t, 1), 128);
-            mbar_init(o_done(t), 1);
-        }
-        mbar_init(bar(FIN), 1);
-        mbar_init(bar(Q_READY), kPrSoft);
+        for (int i = 0; i < L::NBARS; ++i)
+            mbar_init(bar(i), i >= P_FULL && i < O_DONE ? 128
+                              : i >= ITEM_EMPTY && i < NOTED          ? kPrSoft / 32 + 3
+                              : i >= NOTE_FREE && i < FIN             ? kPrSoft / 32
+                                                                      : 1);
         fence_mbar_init();
     }
     if (warp == 0) {
@@ -240,6 +275,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
         tmem_relinquish();
     }
     if (tid == 32) prefetch_tensormap(&tmap);
+    if (tid == 64) prefetch_tensormap(&qmap);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -248,122 +284,221 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
     grid_dependency_wait();
     grid_launch_dependents();
 
-    const PrWork w = pr_work(a, tile, TT, lane);
-    const int nqt = (w.ntok + TQ - 1) / TQ;  // Q tiles with tokens
-    const int t0 = (int)((int64_t)ks * w.nt / a.KS), t1 = (int)((int64_t)(ks + 1) * w.nt / a.KS);
-    const int nt = t1 - t0;  // this CTA's key tiles
-    auto key0 = [&](int t) { return w.key0(t0 + t); };
-    // some query of the CTA does not see some token of the tile
-    auto masked = [&](int k0) {
-        return k0 + kPrKeys - 1 > w.p0 ||
-               (a.window > 0 && k0 <= w.p1 - a.window && k0 + kPrKeys > a.sinks);
+    // item k as the planning warp published it; each reading warp gives its slot
+    // back at once
+    auto item = [&](int k) {
+        wait_phase(bar(ITEM_FULL + (k & 1)), (uint32_t)(k >> 1) & 1u, a.err, dead);
+        const PrItem w = items[k & 1];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(ITEM_EMPTY + (k & 1)));
+        return w;
     };
-    // some query of the CTA sees some token of [tok, tok + n)
-    auto seen_by_any = [&](int tok, int n) { return tok <= w.p1 && (tok + n > w.lo || tok < a.sinks); };
 
-    const int qa = tid / kPrRows, r = tid % kPrRows;  // Q tile and row of a softmax thread
-    const int itok = qa * TQ + r / G;                 // its token in the CTA
-    const bool row_ok = tid < kPrSoft && r < TQ * G && itok < w.ntok;
-    const int64_t qrow_off = ((int64_t)(w.row0 + itok) * Hq + (int64_t)g * G + r % G) * D;
-    constexpr int LOAD_WARP = kPrSoft / 32, MMA_WARP = LOAD_WARP + 2;
-
-    if (warp >= LOAD_WARP) {
+    if (warp >= K_WARP) {
         reg_dec<kPrRegsOther>();
-        if (nt == 0) {
-            // nothing to load
-        } else if (warp == LOAD_WARP || warp == LOAD_WARP + 1) {
+        if (warp == PLAN_WARP) {
+            // ---- the items' order, Q, and the check of V in masked tiles ----
+            int next = blockIdx.x, pub = 0;  // next item to look up, items published
+            auto publish = [&]() {           // the next item that has tokens, or the end
+                PrItem w{};
+                w.s = -1;
+                while (next < a.n_items) {
+                    w = pr_item(a, next, TT, lane);
+                    next += gridDim.x;
+                    if (w.ntok > 0) break;
+                    w.s = -1;
+                }
+                if (pub >= 2) wait_phase(bar(ITEM_EMPTY + (pub & 1)), (uint32_t)((pub >> 1) - 1) & 1u, a.err, dead);
+                if (lane == 0) {
+                    items[pub & 1] = w;
+                    mbar_arrive(bar(ITEM_FULL + (pub & 1)));
+                }
+                __syncwarp();
+                ++pub;
+                return w;
+            };
+            const uint64_t pol = l2_policy_evict_normal();
+            PrItem w = publish();
+            int qn = 0, cnt = 0;        // items with Q loaded; tiles so far
+            uint32_t vn = 0;            // parities: bit st, masked tiles of stage st so far
+            for (int k = 0; w.s >= 0; ++k) {
+                if (w.nt > 0) {
+                    if (qn > 0) wait_phase(bar(Q_FREE), (uint32_t)(qn - 1) & 1u, a.err, dead);
+                    if (lane == 0) {
+                        const int nqt = (w.ntok + TQ - 1) / TQ;
+                        mbar_arrive_expect_tx(bar(Q_FULL), (uint32_t)(nqt * HALVES * TQ * G * 128));
+                        for (int t = 0; t < nqt; ++t)
+                            for (int h = 0; h < HALVES; ++h)
+                                tma_load_3d(sbase + t * L::Q_TILE + h * L::Q_HALF, &qmap, h * 64, w.g * G,
+                                            w.row0 + t * TQ, bar(Q_FULL), pol);
+                    }
+                    __syncwarp();
+                    ++qn;
+                }
+                const PrItem after = publish();  // the other warps may go on to it
+                // V of masked tiles: rows that no query sees are cleared, and so
+                // are rows with a NaN or an infinity, which are noted
+                PrNotes &nb = notes[k & 1];
+                int n_masked = 0;
+                if (k >= 2) wait_phase(bar(NOTE_FREE + (k & 1)), (uint32_t)((k >> 1) - 1) & 1u, a.err, dead);
+                for (int t = 0; t < w.nt; ++t, ++cnt) {
+                    const int k0 = w.key0(t), st = cnt % kPrStages;
+                    if (!w.masked(a, k0)) continue;
+                    wait_phase(bar(V_RAW + st), vn >> st & 1u, a.err, dead);
+                    vn ^= 1u << st;
+                    uint8_t *vt = smem + L::ST_OFF + st * L::STAGE + L::KV_TILE;
+#pragma unroll 1
+                    for (int q4 = 0; q4 < 4; ++q4) {
+                        const int r = q4 * 32 + lane;
+                        const bool any = w.sees(a, k0 + r, 1);
+                        uint32_t odd = 0;  // a half-word with all exponent bits set: one more carries into its sign bit
+#pragma unroll
+                        for (int c = 0; c < D / 8; ++c) {
+                            const uint4 x =
+                                *reinterpret_cast<const uint4 *>(vt + r * 128 + (c / 8) * L::KV_HALF + ((c ^ r) & 7) * 16);
+                            odd |= ((x.x & 0x7fff7fffu) + 0x00800080u) | ((x.y & 0x7fff7fffu) + 0x00800080u) |
+                                   ((x.z & 0x7fff7fffu) + 0x00800080u) | ((x.w & 0x7fff7fffu) + 0x00800080u);
+                        }
+                        odd &= 0x80008000u;
+                        if (!any || odd)
+#pragma unroll 1
+                            for (int c = 0; c < D / 8; ++c)
+                                *reinterpret_cast<uint4 *>(vt + r * 128 + (c / 8) * L::KV_HALF + c % 8 * 16) =
+                                    make_uint4(0u, 0u, 0u, 0u);
+                        __syncwarp();
+                        const uint32_t bits = __ballot_sync(0xffffffffu, any && odd != 0);
+                        if (lane == 0) nb.rows[n_masked][q4] = bits;
+                    }
+                    if (lane == 0) nb.key0[n_masked] = k0;
+                    ++n_masked;
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(FULL_V + st));
+                }
+                if (lane == 0) {
+                    nb.n = n_masked;
+                    mbar_arrive(bar(NOTED + (k & 1)));
+                }
+                __syncwarp();
+                w = after;
+            }
+        } else if (warp != MMA_WARP) {
             // ---- TMA producer warps, one of K and one of V: one box per lane ----
-            const bool is_v = warp != LOAD_WARP;
+            const bool is_v = warp == V_WARP;
             const uint64_t pol = l2_policy_evict_normal();
             constexpr int NBOX = kPrKeys / kTile * HALVES;
             const int full0 = is_v ? FULL_V : FULL_K, empty0 = is_v ? EMPTY_V : EMPTY_K;
             const int j = lane / HALVES, h = lane % HALVES;
-            // pool row of this lane's box of tile t: -1 outside the pool, -2 not wanted
-            auto box_row = [&](int t) {
-                const int32_t tok = key0(t) + j * kTile;
-                if (lane >= NBOX || t >= nt || !seen_by_any(tok, kTile)) return -2;
-                const int32_t y = pr_pool_row(a, w.s, g, tok);
-                return y < 0 ? -1 : y + (is_v ? a.Hkv * a.bs : 0);
-            };
-            int32_t y = box_row(0);
-            for (int t = 0; t < nt; ++t) {
-                const int st = t % kPrStages;
-                const int32_t y_next = box_row(t + 1);
-                const bool bad = __any_sync(0xffffffffu, y == -1);
-                const uint32_t n = __popc(__ballot_sync(0xffffffffu, y >= 0));
-                const uint32_t full = bar(full0 + st);
-                if (t >= kPrStages) wait_phase(bar(empty0 + st), (uint32_t)(t / kPrStages - 1) & 1u, a.err, dead);
-                if (lane == 0) {
-                    if (bad || n == 0) {
-                        if (bad) report(a.err, KV_ERR_DEVICE_BOUNDS);
-                        mbar_arrive(full);  // complete the phase without data
-                    } else {
-                        mbar_arrive_expect_tx(full, n * kHalfBytes);
+            int cnt = 0;
+            for (int k = 0;; ++k) {
+                const PrItem w = item(k);
+                if (w.s < 0) break;
+                // pool row of this lane's box of tile t: -1 outside the pool, -2 not wanted
+                auto box_row = [&](int t) {
+                    if (lane >= NBOX || t >= w.nt) return -2;
+                    const int32_t tok = w.key0(t) + j * kTile;
+                    if (!w.sees(a, tok, kTile)) return -2;
+                    const int32_t y = pr_pool_row(a, w.s, w.g, tok);
+                    return y < 0 ? -1 : y + (is_v ? a.Hkv * a.bs : 0);
+                };
+                int32_t y = box_row(0);
+                for (int t = 0; t < w.nt; ++t, ++cnt) {
+                    const int st = cnt % kPrStages;
+                    const int32_t y_next = box_row(t + 1);
+                    const bool bad = __any_sync(0xffffffffu, y == -1);
+                    const uint32_t n = __popc(__ballot_sync(0xffffffffu, y >= 0));
+                    const uint32_t full = bar(is_v && w.masked(a, w.key0(t)) ? V_RAW + st : full0 + st);
+                    if (cnt >= kPrStages)
+                        wait_phase(bar(empty0 + st), (uint32_t)(cnt / kPrStages - 1) & 1u, a.err, dead);
+                    if (lane == 0) {
+                        if (bad || n == 0) {
+                            if (bad) report(a.err, KV_ERR_DEVICE_BOUNDS);
+                            mbar_arrive(full);  // complete the phase without data
+                        } else {
+                            mbar_arrive_expect_tx(full, n * kHalfBytes);
+                        }
                     }
+                    __syncwarp();
+                    if (!bad && y >= 0)
+                        tma_load_2d(sbase + L::ST_OFF + st * L::STAGE + (is_v ? L::KV_TILE : 0) + h * L::KV_HALF +
+                                        j * (kTile * 128),
+                                    &tmap, h * 64, y, full, pol);
+                    __syncwarp();
+                    y = y_next;
                 }
-                __syncwarp();
-                if (!bad && y >= 0)
-                    tma_load_2d(sbase + L::ST_OFF + st * L::STAGE + (is_v ? L::KV_TILE : 0) + h * L::KV_HALF +
-                                    j * (kTile * 128),
-                                &tmap, h * 64, y, full, pol);
-                __syncwarp();
-                y = y_next;
             }
             // drain: the last stages' loads have landed
             if (lane == 0)
-                for (int t = max(0, nt - kPrStages); t < nt; ++t)
-                    wait_phase(bar(full0 + t % kPrStages), (uint32_t)(t / kPrStages) & 1u, a.err, dead);
-        } else if (warp == MMA_WARP) {
+                for (int c = max(0, cnt - kPrStages); c < cnt; ++c)
+                    wait_phase(bar(full0 + c % kPrStages), (uint32_t)(c / kPrStages) & 1u, a.err, dead);
+        } else {
             // ---- MMA issuer: S_0(0) S_1(0) | PV_0(t) S_0(t+1) PV_1(t) S_1(t+1) | ... ; the
-            // pipe runs one thread's MMAs in issue order, so S_a(t+1) overwrites P
-            // only after PV_a(t) has read it ----
+            // pipe runs one thread's MMAs in issue order, so S_a(t+1), or S_a(0) of
+            // the next item, overwrites P only after PV_a(t) has read it.  O is
+            // overwritten by PV_a(0) of the next item once its P is there, which
+            // the softmax warps write after they have read O ----
             const uint32_t el = elect_one();
             constexpr uint32_t ID_S = idesc_bf16_f32(kPrRows, kPrKeys, 0, 0);
             constexpr uint32_t ID_O = idesc_bf16_f32(kPrRows, D, 0, 1);
-            auto issue_s = [&](int t_, int t) {
-                const uint32_t ka = sbase + L::ST_OFF + (t % kPrStages) * L::STAGE;
-                const uint32_t q_ = sbase + t_ * L::Q_TILE;
+            int cnt = 0, qn = 0;           // tiles, items with Q so far
+            uint32_t pn = 0;               // parities: bit q, tiles of Q tile q so far
+            auto issue_s = [&](int q, int c) {
+                const uint32_t ka = sbase + L::ST_OFF + (c % kPrStages) * L::STAGE;
+                const uint32_t qa = sbase + q * L::Q_TILE;
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk)
-                    umma_bf16(tbase + t_ * kPrTmemCols, smem_desc_sw128(q_ + (kk / 4) * L::Q_HALF + (kk % 4) * 32, 16, 1024),
+                    umma_bf16(tbase + q * kPrTmemCols, smem_desc_sw128(qa + (kk / 4) * L::Q_HALF + (kk % 4) * 32, 16, 1024),
                               smem_desc_sw128(ka + (kk / 4) * L::KV_HALF + (kk % 4) * 32, 16, 1024), ID_S, kk > 0, el);
-                umma_commit(s_full(t_), el);
+                umma_commit(bar(S_FULL + q), el);
             };
-            auto issue_pv = [&](int t_, int t, int half) {
-                const uint32_t va = sbase + L::ST_OFF + (t % kPrStages) * L::STAGE + L::KV_TILE;
+            auto issue_pv = [&](int q, int c, int half, bool more) {
+                const uint32_t va = sbase + L::ST_OFF + (c % kPrStages) * L::STAGE + L::KV_TILE;
                 constexpr int STEPS = kPrKeys / 2 / 16;
 #pragma unroll
                 for (int i = 0; i < STEPS; ++i) {
                     const int kk = half * STEPS + i;
-                    umma_bf16_tmem_a(tbase + t_ * kPrTmemCols + O_COL, tbase + t_ * kPrTmemCols + kk * 8,
-                                     smem_desc_sw128(va + kk * (16 * 128), L::KV_HALF, 1024), ID_O, t > 0 || kk > 0, el);
+                    umma_bf16_tmem_a(tbase + q * kPrTmemCols + O_COL, tbase + q * kPrTmemCols + kk * 8,
+                                     smem_desc_sw128(va + kk * (16 * 128), L::KV_HALF, 1024), ID_O, more || kk > 0, el);
                 }
             };
-            wait_phase(bar(Q_READY), 0u, a.err, dead);
-            wait_phase(bar(FULL_K + 0), 0u, a.err, dead);
-            tc_fence_after();
-            for (int t_ = 0; t_ < nqt; ++t_) issue_s(t_, 0);
-            umma_commit(bar(EMPTY_K + 0), el);
-            for (int t = 0; t < nt; ++t) {
-                const bool next = t + 1 < nt;
-                for (int t_ = 0; t_ < nqt; ++t_) {
-                    if (t_ == 0)
-                        wait_phase(bar(FULL_V + t % kPrStages), (uint32_t)(t / kPrStages) & 1u, a.err, dead);
-                    wait_phase(p_full(t_, 0), (uint32_t)t & 1u, a.err, dead);
-                    tc_fence_after();
-                    issue_pv(t_, t, 0);
-                    wait_phase(p_full(t_, 1), (uint32_t)t & 1u, a.err, dead);
-                    tc_fence_after();
-                    issue_pv(t_, t, 1);
-                    umma_commit(o_done(t_), el);
-                    if (t_ == nqt - 1) umma_commit(bar(EMPTY_V + t % kPrStages), el);
-                    if (next) {
-                        if (t_ == 0)
-                            wait_phase(bar(FULL_K + (t + 1) % kPrStages), (uint32_t)((t + 1) / kPrStages) & 1u, a.err,
-                                       dead);
+            auto wait_k = [&](int c) {
+                wait_phase(bar(FULL_K + c % kPrStages), (uint32_t)(c / kPrStages) & 1u, a.err, dead);
+            };
+            for (int k = 0;; ++k) {
+                const PrItem w = item(k);
+                if (w.s < 0) break;
+                if (w.nt == 0) continue;
+                const int nqt = (w.ntok + TQ - 1) / TQ;
+                wait_phase(bar(Q_FULL), (uint32_t)qn & 1u, a.err, dead);
+                ++qn;
+                wait_k(cnt);
+                tc_fence_after();
+                for (int q = 0; q < nqt; ++q) issue_s(q, cnt);
+                umma_commit(bar(EMPTY_K + cnt % kPrStages), el);
+                if (w.nt == 1) umma_commit(bar(Q_FREE), el);
+                for (int t = 0; t < w.nt; ++t, ++cnt) {
+                    const int st = cnt % kPrStages;
+                    const bool next = t + 1 < w.nt;
+                    wait_phase(bar(FULL_V + st), (uint32_t)(cnt / kPrStages) & 1u, a.err, dead);
+                    for (int q = 0; q < nqt; ++q) {
+                        wait_phase(bar(P_FULL + 2 * q), pn >> q & 1u, a.err, dead);
                         tc_fence_after();
-                        issue_s(t_, t + 1);
-                        if (t_ == nqt - 1) umma_commit(bar(EMPTY_K + (t + 1) % kPrStages), el);
+                        issue_pv(q, cnt, 0, t > 0);
+                        wait_phase(bar(P_FULL + 2 * q + 1), pn >> q & 1u, a.err, dead);
+                        pn ^= 1u << q;
+                        tc_fence_after();
+                        issue_pv(q, cnt, 1, true);
+                        if (!next) umma_commit(bar(O_DONE + q), el);
+                        if (q == nqt - 1) umma_commit(bar(EMPTY_V + st), el);
+                        if (next) {
+                            if (q == 0) wait_k(cnt + 1);
+                            tc_fence_after();
+                            issue_s(q, cnt + 1);
+                            if (q == nqt - 1) {
+                                umma_commit(bar(EMPTY_K + (cnt + 1) % kPrStages), el);
+                                if (t + 2 == w.nt) umma_commit(bar(Q_FREE), el);  // Q's last use
+                            }
+                        }
                     }
                 }
             }
@@ -372,85 +507,51 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             wait_phase(bar(FIN), 0u, a.err, dead);
         }
     } else {
+        // ---- softmax: thread r of Q tile qa owns its row r ----
         reg_inc<kPrRegsSoft>();
-        if (nt > 0) {
-            // whole rows per 16-byte load (a lane reading its own row: 4000
-            // clocks more); rows without a token are zero
-            uint8_t *qdst = smem + qa * L::Q_TILE;
-            constexpr int CPR = D / 8, RPI = 32 / CPR;  // chunks of a row, rows a load
-            const int64_t mine = row_ok ? qrow_off : -1;
-#pragma unroll 1
-            for (int i0 = 0; i0 < 32 / RPI; i0 += 8) {
-                uint4 x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int64_t off = __shfl_sync(0xffffffffu, mine, (i0 + i) * RPI + lane / CPR);
-                    x[i] = off >= 0 ? *reinterpret_cast<const uint4 *>(a.q + off + lane % CPR * 8)
-                                    : make_uint4(0u, 0u, 0u, 0u);
+        const int qa = tid / kPrRows, r = tid % kPrRows;
+        const int itok = qa * TQ + r / G;  // the row's token in the item
+        const uint32_t trow = tbase + qa * kPrTmemCols + ((uint32_t)((warp % 4) * 32) << 16);
+        const float scale = a.qk_scale;
+        uint8_t *xb = smem + L::X_OFF + warp * 4096;
+        int pn = 0, on = 0;  // tiles, and items with tiles, of this Q tile so far
+        for (int k = 0;; ++k) {
+            // read where needed: its fields and a row's scores together are more
+            // than the registers
+            const PrItem &w = items[k & 1];
+            wait_phase(bar(ITEM_FULL + (k & 1)), (uint32_t)(k >> 1) & 1u, a.err, dead);
+            if (w.s < 0) break;
+            auto give_back = [&]() {  // the item and its notes
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(bar(NOTE_FREE + (k & 1)));
+                    mbar_arrive(bar(ITEM_EMPTY + (k & 1)));
                 }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int rr = (warp % 4) * 32 + (i0 + i) * RPI + lane / CPR, ch = lane % CPR;
-                    x[i].x = (x[i].x ^ a.q_xor) & a.q_and;
-                    x[i].y = (x[i].y ^ a.q_xor) & a.q_and;
-                    x[i].z = (x[i].z ^ a.q_xor) & a.q_and;
-                    x[i].w = (x[i].w ^ a.q_xor) & a.q_and;
-                    *reinterpret_cast<uint4 *>(qdst + (ch / 8) * L::Q_HALF + swz(rr, ch % 8)) = x[i];
-                }
+            };
+            if (qa * TQ >= w.ntok) {  // no tokens in this Q tile
+                wait_phase(bar(NOTED + (k & 1)), (uint32_t)(k >> 1) & 1u, a.err, dead);
+                give_back();
+                continue;
             }
-            fence_proxy_async_smem();
-            mbar_arrive(bar(Q_READY));
-        }
-        if (qa < nqt) {
-            const int p = w.p0 + itok;  // this row's position
-            const uint32_t trow = tbase + qa * kPrTmemCols + ((uint32_t)((warp % 4) * 32) << 16);
-            const float scale = a.qk_scale;
             float m_run = kMaxStart, l_run = 0.f;
-            int n_masked = 0;
-            for (int t = 0; t < nt; ++t) {
-                const int k0 = key0(t);
-                const bool mk = masked(k0);
-                wait_phase(s_full(qa), (uint32_t)t & 1u, a.err, dead);
+            for (int t = 0; t < w.nt; ++t, ++pn) {
+                const int k0 = w.key0(t);
+                const bool mk = w.masked(a, k0) | (a.sign != 1.f);
+                // tokens of the tile that this row sees: [.., hi] and (> wl or < sk)
+                const int hi = w.p0 + itok - k0;
+                wait_phase(bar(S_FULL + qa), (uint32_t)pn & 1u, a.err, dead);
                 __syncwarp();
                 tc_fence_after();
-                if (mk && qa == 0) {
-                    // rows of V that no query sees, or that hold a NaN or an
-                    // infinity, are cleared; the latter noted
-                    wait_phase(bar(FULL_V + t % kPrStages), (uint32_t)(t / kPrStages) & 1u, a.err, dead);
-                    uint8_t *v = smem + L::ST_OFF + (t % kPrStages) * L::STAGE + L::KV_TILE + r * 128;
-                    const bool any = seen_by_any(k0 + r, 1);
-                    uint32_t odd = 0;  // a half-word with all exponent bits set: one more carries into its sign bit
-                    if (any)
-#pragma unroll 4
-                        for (int c = 0; c < D / 8; ++c) {
-                            const uint4 x = *reinterpret_cast<const uint4 *>(v + (c / 8) * L::KV_HALF + ((c ^ r) & 7) * 16);
-                            odd |= ((x.x & 0x7fff7fffu) + 0x00800080u) | ((x.y & 0x7fff7fffu) + 0x00800080u) |
-                                   ((x.z & 0x7fff7fffu) + 0x00800080u) | ((x.w & 0x7fff7fffu) + 0x00800080u);
-                        }
-                    odd &= 0x80008000u;
-                    if (!any || odd)
-#pragma unroll 1
-                        for (int c = 0; c < D / 8; ++c)
-                            *reinterpret_cast<uint4 *>(v + (c / 8) * L::KV_HALF + ((c ^ r) & 7) * 16) =
-                                make_uint4(0u, 0u, 0u, 0u);
-                    __syncwarp();
-                    const uint32_t bits = __ballot_sync(0xffffffffu, odd != 0);
-                    if (lane == 0) note[n_masked * 4 + warp] = bits;
-                    if (tid == 0) note_key[n_masked] = k0;
-                    ++n_masked;
-                    fence_proxy_async_smem();
-                    __syncwarp();
-                }
-                // tokens of the tile that this row sees: [.., hi] and (> wl or < sk)
-                const int hi = p - k0, wl = a.window > 0 ? hi - a.window : -1, sk = a.sinks - k0;
                 uint32_t v[4][32];  // the row's scores, then its weights
                 tmem_ld32(trow, v[0]);
                 tmem_ld32(trow + 32, v[1]);
                 tmem_wait_ld();
                 tmem_ld32(trow + 64, v[2]);
                 tmem_ld32(trow + 96, v[3]);
+                const int wl = a.window > 0 ? hi - a.window : -1, sk = a.sinks - k0;
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 if (mk) {
+                    if (a.sign != 1.f) pr_times(v[0], a.sign), pr_times(v[1], a.sign);
                     pr_mask(v[0], hi, wl, sk);
                     pr_mask(v[1], hi - 32, wl - 32, sk - 32);
                 }
@@ -458,27 +559,30 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 pr_max(v[1], mx);
                 tmem_wait_ld();
                 if (mk) {
+                    if (a.sign != 1.f) pr_times(v[2], a.sign), pr_times(v[3], a.sign);
                     pr_mask(v[2], hi - 64, wl - 64, sk - 64);
                     pr_mask(v[3], hi - 96, wl - 96, sk - 96);
                 }
                 pr_max(v[2], mx);
                 pr_max(v[3], mx);
                 const float cmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
-                // (a warp's lanes read and write TMEM together: all rows of a warp are
-                // scaled when one of them asks for it, the others by 1)
+                // the reference moves only when a tile exceeds it by 2^8 (o and l share
+                // it, so the ratio is exact).  A warp's lanes read and write TMEM
+                // together: all rows of a warp are scaled when one of them asks for
+                // it, the others by 1
                 const bool rise = cmax > m_run + 8.f;
                 if (__any_sync(0xffffffffu, rise)) {
                     const float al = rise ? fast_exp2(m_run - cmax) : 1.f;  // 0 when nothing came before
                     l_run *= al;
                     if (t >= 1) {
-                        uint32_t o[32];
-#pragma unroll
-                        for (int cb = 0; cb < D / 32; ++cb) {
-                            tmem_ld32(trow + O_COL + cb * 32, o);
+                        uint32_t o[16];
+#pragma unroll 1
+                        for (int cb = 0; cb < D / 16; ++cb) {
+                            tmem_ld16(trow + O_COL + cb * 16, o);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * al);
-                            tmem_st32(trow + O_COL + cb * 32, o);
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * al);
+                            tmem_st16(trow + O_COL + cb * 16, o);
                         }
                     }
                     if (rise) m_run = cmax;
@@ -492,7 +596,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                     uint32_t pw[16];
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) {
-                        float2 y = __ffma2_rn(make_float2(__uint_as_float(v[c][i]), __uint_as_float(v[c][i + 1])), sc2, nm2);
+                        float2 y =
+                            __ffma2_rn(make_float2(__uint_as_float(v[c][i]), __uint_as_float(v[c][i + 1])), sc2, nm2);
                         y.x = fast_exp2(y.x);
                         y.y = fast_exp2(y.y);
                         pw[i / 2] = pr_pack(y.x, y.y);
@@ -503,7 +608,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                     if (c & 1) {
                         tmem_wait_st();
                         tc_fence_before();
-                        mbar_arrive(p_full(qa, c / 2));
+                        mbar_arrive(bar(P_FULL + 2 * qa + c / 2));
                     }
                 }
                 // the weights' sum, while the tensor core works on them
@@ -515,48 +620,37 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 const float2 r1 = __fadd2_rn(__fadd2_rn(r2[0], r2[1]), __fadd2_rn(r2[2], r2[3]));
                 l_run += r1.x + r1.y;
             }
-            // ---- the rows' outputs, or this split's records ----
-            if (nt > 0) wait_phase(o_done(qa), (uint32_t)(nt - 1) & 1u, a.err, dead);
+            // ---- the rows' outputs, or this split's records (rolled: it runs once an item) ----
+            if (w.nt > 0) wait_phase(bar(O_DONE + qa), (uint32_t)on++ & 1u, a.err, dead);
+            wait_phase(bar(NOTED + (k & 1)), (uint32_t)(k >> 1) & 1u, a.err, dead);
             __syncwarp();
             tc_fence_after();
-            if (tid == 0) *n_notes = n_masked;
-            asm volatile("bar.sync 1, %0;" ::"r"(nqt * 128) : "memory");  // Q tile 0's notes
-            const int notes = *n_notes;
-            const bool blind = p < 0;  // the row sees nothing: zeros
-            const float inv = blind || nt == 0 ? 0.f : 1.f / l_run;
-            const bool rec = a.KS > 1;
-            // Through shared memory, 128 bytes of a row at a time, so that eight
-            // lanes write 128 consecutive bytes; the buffer is the stage that the
-            // last key tile did not use.
-            uint8_t *xb = smem + L::ST_OFF + (nt % kPrStages) * L::STAGE + warp * (32 * 128);
-            const int64_t rec_i = ((int64_t)ks * a.T + w.row0 + itok) * Hq + (int64_t)g * G + r % G;
-            float *recp = a.ws + rec_i * pr_record<D>();
-            const unsigned long long orow =
-                !row_ok || dead ? 0ull
-                                : rec ? reinterpret_cast<unsigned long long>(recp)
-                                      : reinterpret_cast<unsigned long long>(a.out + qrow_off);
-            // noted tokens that this row sees: added to O in TMEM
+            const bool row_ok = r < TQ * G && itok < w.ntok;
+            const int64_t qrow_off = ((int64_t)(w.row0 + itok) * Hq + (int64_t)w.g * G + r % G) * D;
+            const int p = w.p0 + itok, nt = w.nt;  // this row's position; the item's tiles
+            const PrNotes &nb = notes[k & 1];
+            const int n_notes = nb.n * 4;
             bool any_note = false;
-            for (int b = lane; b < notes * 4; b += 32) any_note |= note[b] != 0;
+            for (int b = lane; b < n_notes; b += 32) any_note |= nb.rows[b / 4][b % 4] != 0;
             if (__any_sync(0xffffffffu, any_note)) {
+                // noted tokens that this row sees: added to O in TMEM
 #pragma unroll 1
                 for (int cb = 0; cb < D / 32; ++cb) {
                     uint32_t o[32];
                     tmem_ld32(trow + O_COL + cb * 32, o);
                     tmem_wait_ld();
 #pragma unroll 1
-                    for (int b = 0; b < notes * 4; ++b)
-                        for (uint32_t bits = note[b]; bits; bits &= bits - 1) {
-                            const int tok = note_key[b / 4] + b % 4 * 32 + __ffs((int)bits) - 1;
+                    for (int b = 0; b < n_notes; ++b)
+                        for (uint32_t bits = nb.rows[b / 4][b % 4]; bits; bits &= bits - 1) {
+                            const int tok = nb.key0[b / 4] + b % 4 * 32 + __ffs((int)bits) - 1;
                             if (!row_ok || tok > p || (a.window > 0 && tok <= p - a.window && tok >= a.sinks)) continue;
-                            const int32_t y = pr_pool_row(a, w.s, g, tok);
+                            const int32_t y = pr_pool_row(a, w.s, w.g, tok);
                             if (y < 0) continue;
                             const uint16_t *kr = a.pool + (int64_t)y * D, *vr = kr + (int64_t)a.Hkv * a.bs * D;
                             float s = 0.f;
 #pragma unroll 1
-                            for (int e = 0; e < D; ++e)
-                                s = fmaf(bf_lo((a.q[qrow_off + e] ^ (a.q_xor & 0xffffu)) & a.q_and), bf_lo(kr[e]), s);
-                            const float pj = fast_exp2(fmaf(s, scale, -m_run));
+                            for (int e = 0; e < D; ++e) s = fmaf(bf_lo(a.q[qrow_off + e]), bf_lo(kr[e]), s);
+                            const float pj = fast_exp2(fmaf(s * a.sign, scale, -m_run));
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
                                 o[i] = __float_as_uint(fmaf(pj, bf_lo(vr[cb * 32 + i]), __uint_as_float(o[i])));
@@ -566,9 +660,21 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                     tmem_wait_st();
                 }
             }
-            auto send = [&](int part, const uint4 (&x)[8]) {  // 128 bytes of each row
+            const bool blind = p < 0;  // the row sees nothing: zeros
+            const float inv = blind || nt == 0 ? 0.f : 1.f / l_run;
+            const bool rec = a.KS > 1;
+            float *recp = a.ws + (((int64_t)w.ks * a.T + w.row0 + itok) * Hq + (int64_t)w.g * G + r % G) * pr_record<D>();
+            const unsigned long long orow =
+                !row_ok || dead ? 0ull
+                                : rec ? reinterpret_cast<unsigned long long>(recp)
+                                      : reinterpret_cast<unsigned long long>(a.out + qrow_off);
+            give_back();
+            // 128 bytes of each row through shared memory, so that eight lanes
+            // write 128 consecutive bytes
+            auto send = [&](int part, const uint4 (&x)[8]) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4 *>(xb + lane * 128 + ((i ^ (lane & 7)) * 16)) = x[i];
+                for (int i = 0; i < 8; ++i)
+                    *reinterpret_cast<uint4 *>(xb + lane * 128 + ((i ^ (lane & 7)) * 16)) = x[i];
                 __syncwarp();
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -579,7 +685,6 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 }
                 __syncwarp();
             };
-            // (rolled: each CTA fetches this code anew)
             if (rec) {
 #pragma unroll 1
                 for (int cb = 0; cb < D / 32 && nt > 0; ++cb) {
@@ -610,14 +715,15 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                         uint32_t y[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const int k = 8 * (i % 4) + 2 * e;
-                            y[e] = pr_pack(__uint_as_float(o[i / 4][k]) * inv, __uint_as_float(o[i / 4][k + 1]) * inv);
+                            const int c = 8 * (i % 4) + 2 * e;
+                            y[e] = pr_pack(__uint_as_float(o[i / 4][c]) * inv, __uint_as_float(o[i / 4][c + 1]) * inv);
                         }
                         x[i] = blind ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(y[0], y[1], y[2], y[3]);
                     }
                     send(cb, x);
                 }
             }
+            tc_fence_before();  // O has been read: the next item's P may let it be overwritten
         }
     }
     tc_fence_before();
