@@ -42,6 +42,8 @@ namespace kvp {
 constexpr int kPrRows = 128;   // rows of a Q tile: the MMA's M
 constexpr int kPrTiles = 2;    // Q tiles per item
 constexpr int kPrKeys = 128;   // keys per tile: S's N, P.V's K
+constexpr int kPrFirst = 96;   // keys whose weights are handed over first: the tensor core, which takes the Q
+                               // tiles in turn, should not run out of them before the others are there
 constexpr int kPrStages = 2;
 constexpr int kPrSoft = kPrTiles * 128;     // softmax threads, one per row
 constexpr int kPrThreads = kPrSoft + 128;   // + K and V load warps, MMA warp, scheduling warp
@@ -233,6 +235,22 @@ __device__ __forceinline__ void pr_max(const uint32_t (&x)[32], float (&mx)[4])
         mx[(k >> 1) & 3] = fmaxf(fmaxf(mx[(k >> 1) & 3], __uint_as_float(x[k])), __uint_as_float(x[k + 1]));
 }
 
+// the weights of 32 scores as bf16 pairs, and their sums, in four chains (begun
+// anew with `first`)
+__device__ __forceinline__ void pr_weights(const uint32_t (&x)[32], uint32_t (&pw)[16], float2 (&r)[4], float scale,
+                                           float m, bool first)
+{
+    const float2 sc = make_float2(scale, scale), nm = make_float2(-m, -m);
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+        float2 y = __ffma2_rn(make_float2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), sc, nm);
+        y.x = fast_exp2(y.x);
+        y.y = fast_exp2(y.y);
+        pw[i / 2] = pr_pack(y.x, y.y);
+        r[(i >> 1) & 3] = first && i < 8 ? y : __fadd2_rn(r[(i >> 1) & 3], y);
+    }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kPrThreads, 1)
 prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap qmap,
@@ -250,7 +268,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
     PrNotes *notes = reinterpret_cast<PrNotes *>(smem + L::NOTE_OFF);
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     // K and V of a stage loaded, free (V of a masked tile: loaded is V_RAW, and
-    // FULL_V follows its check); per Q tile: S done, P of keys 64 half .. 64 half + 63 written, O done; an item's Q
+    // FULL_V follows its check); per Q tile: S done, P of the first kPrFirst keys and of the others written, O done; an item's Q
     // loaded, used; an item published, read; its notes complete, read; all MMAs done
     constexpr int FULL_K = 0, EMPTY_K = 2, FULL_V = 4, EMPTY_V = 6, V_RAW = 8;
     constexpr int S_FULL = 10, P_FULL = 12, O_DONE = 16, Q_FULL = 18, Q_FREE = 19, ITEM_FULL = 20, ITEM_EMPTY = 22,
@@ -351,22 +369,27 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                     for (int q4 = 0; q4 < 4; ++q4) {
                         const int r = q4 * 32 + lane;
                         const bool any = w.sees(a, k0 + r, 1);
-                        uint32_t odd = 0;  // a half-word with all exponent bits set: one more carries into its sign bit
+                        // x * 0 + acc: acc stays 0 while every value is finite
+                        __nv_bfloat162 acc[2] = {__floats2bfloat162_rn(0.f, 0.f), __floats2bfloat162_rn(0.f, 0.f)};
+                        const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
 #pragma unroll
                         for (int c = 0; c < D / 8; ++c) {
                             const uint4 x =
                                 *reinterpret_cast<const uint4 *>(vt + r * 128 + (c / 8) * L::KV_HALF + ((c ^ r) & 7) * 16);
-                            odd |= ((x.x & 0x7fff7fffu) + 0x00800080u) | ((x.y & 0x7fff7fffu) + 0x00800080u) |
-                                   ((x.z & 0x7fff7fffu) + 0x00800080u) | ((x.w & 0x7fff7fffu) + 0x00800080u);
+                            acc[0] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.x), zero, acc[0]);
+                            acc[1] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.y), zero, acc[1]);
+                            acc[0] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.z), zero, acc[0]);
+                            acc[1] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.w), zero, acc[1]);
                         }
-                        odd &= 0x80008000u;
+                        const bool odd = ((*reinterpret_cast<uint32_t *>(&acc[0]) | *reinterpret_cast<uint32_t *>(&acc[1])) &
+                                          0x7fff7fffu) != 0;
                         if (!any || odd)
 #pragma unroll 1
                             for (int c = 0; c < D / 8; ++c)
                                 *reinterpret_cast<uint4 *>(vt + r * 128 + (c / 8) * L::KV_HALF + c % 8 * 16) =
                                     make_uint4(0u, 0u, 0u, 0u);
                         __syncwarp();
-                        const uint32_t bits = __ballot_sync(0xffffffffu, any && odd != 0);
+                        const uint32_t bits = __ballot_sync(0xffffffffu, any && odd);
                         if (lane == 0) nb.rows[n_masked][q4] = bits;
                     }
                     if (lane == 0) nb.key0[n_masked] = k0;
@@ -453,10 +476,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             };
             auto issue_pv = [&](int q, int c, int half, bool more) {
                 const uint32_t va = sbase + L::ST_OFF + (c % kPrStages) * L::STAGE + L::KV_TILE;
-                constexpr int STEPS = kPrKeys / 2 / 16;
+                constexpr int STEPS = kPrKeys / 16, FIRST = kPrFirst / 16;
 #pragma unroll
-                for (int i = 0; i < STEPS; ++i) {
-                    const int kk = half * STEPS + i;
+                for (int kk = half ? FIRST : 0; kk < (half ? STEPS : FIRST); ++kk) {
                     umma_bf16_tmem_a(tbase + q * kPrTmemCols + O_COL, tbase + q * kPrTmemCols + kk * 8,
                                      smem_desc_sw128(va + kk * (16 * 128), L::KV_HALF, 1024), ID_O, more || kk > 0, el);
                 }
@@ -510,7 +532,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
         // ---- softmax: thread r of Q tile qa owns its row r ----
         reg_inc<kPrRegsSoft>();
         const int qa = tid / kPrRows, r = tid % kPrRows;
-        const int itok = qa * TQ + r / G;  // the row's token in the item
+        const int itok = qa * TQ + r / G, hrow = r % G;  // the row's token in the item, its head in the group
         const uint32_t trow = tbase + qa * kPrTmemCols + ((uint32_t)((warp % 4) * 32) << 16);
         const float scale = a.qk_scale;
         uint8_t *xb = smem + L::X_OFF + warp * 4096;
@@ -534,42 +556,48 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 continue;
             }
             float m_run = kMaxStart, l_run = 0.f;
-            for (int t = 0; t < w.nt; ++t, ++pn) {
+            // tile t: whether it is masked; this row sees its columns [.., hi], of
+            // which from the window's edge on or below sk
+            bool mk;
+            int hi, sk;
+            auto tile_of = [&](int t) {
                 const int k0 = w.key0(t);
-                const bool mk = w.masked(a, k0) | (a.sign != 1.f);
-                // tokens of the tile that this row sees: [.., hi] and (> wl or < sk)
-                const int hi = w.p0 + itok - k0;
+                mk = w.masked(a, k0) | (a.sign != 1.f);
+                hi = w.p0 + itok - k0;
+                sk = a.sinks - k0;
+            };
+            tile_of(0);
+            for (int t = 0; t < w.nt; ++t, ++pn) {
                 wait_phase(bar(S_FULL + qa), (uint32_t)pn & 1u, a.err, dead);
                 __syncwarp();
                 tc_fence_after();
-                uint32_t v[4][32];  // the row's scores, then its weights
+                uint32_t v[4][32];  // the row's scores
                 tmem_ld32(trow, v[0]);
                 tmem_ld32(trow + 32, v[1]);
                 tmem_wait_ld();
                 tmem_ld32(trow + 64, v[2]);
                 tmem_ld32(trow + 96, v[3]);
-                const int wl = a.window > 0 ? hi - a.window : -1, sk = a.sinks - k0;
-                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 if (mk) {
+                    const int wl = a.window > 0 ? hi - a.window : -1;
                     if (a.sign != 1.f) pr_times(v[0], a.sign), pr_times(v[1], a.sign);
                     pr_mask(v[0], hi, wl, sk);
                     pr_mask(v[1], hi - 32, wl - 32, sk - 32);
-                }
-                pr_max(v[0], mx);
-                pr_max(v[1], mx);
-                tmem_wait_ld();
-                if (mk) {
+                    tmem_wait_ld();
                     if (a.sign != 1.f) pr_times(v[2], a.sign), pr_times(v[3], a.sign);
                     pr_mask(v[2], hi - 64, wl - 64, sk - 64);
                     pr_mask(v[3], hi - 96, wl - 96, sk - 96);
                 }
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                pr_max(v[0], mx);
+                pr_max(v[1], mx);
+                tmem_wait_ld();
                 pr_max(v[2], mx);
                 pr_max(v[3], mx);
                 const float cmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
-                // the reference moves only when a tile exceeds it by 2^8 (o and l share
-                // it, so the ratio is exact).  A warp's lanes read and write TMEM
-                // together: all rows of a warp are scaled when one of them asks for
-                // it, the others by 1
+                // The reference m_run moves only when a tile exceeds it by 2^8 (o and l
+                // share it, so the ratio is exact).  A warp's lanes read and write
+                // TMEM together: all rows of a warp are scaled when one of them asks
+                // for it, the others by 1
                 const bool rise = cmax > m_run + 8.f;
                 if (__any_sync(0xffffffffu, rise)) {
                     const float al = rise ? fast_exp2(m_run - cmax) : 1.f;  // 0 when nothing came before
@@ -589,34 +617,31 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                     __syncwarp();
                 }
                 // p = 2^(s * scale - m_run), as bf16 pairs over the first columns of S,
-                // handed over in halves
-                const float2 sc2 = make_float2(scale, scale), nm2 = make_float2(-m_run, -m_run);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t pw[16];
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        float2 y =
-                            __ffma2_rn(make_float2(__uint_as_float(v[c][i]), __uint_as_float(v[c][i + 1])), sc2, nm2);
-                        y.x = fast_exp2(y.x);
-                        y.y = fast_exp2(y.y);
-                        pw[i / 2] = pr_pack(y.x, y.y);
-                        v[c][i] = __float_as_uint(y.x);
-                        v[c][i + 1] = __float_as_uint(y.y);
-                    }
-                    tmem_st16(trow + c * 16, pw);
-                    if (c & 1) {
-                        tmem_wait_st();
-                        tc_fence_before();
-                        mbar_arrive(bar(P_FULL + 2 * qa + c / 2));
-                    }
+                // handed over in two parts
+                uint32_t pw[2][16];
+                float2 r2[4];
+                pr_weights(v[0], pw[0], r2, scale, m_run, true);
+                tmem_st16(trow, pw[0]);
+                pr_weights(v[1], pw[1], r2, scale, m_run, false);
+                tmem_st16(trow + 16, pw[1]);
+                if (kPrFirst == 64) {
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(bar(P_FULL + 2 * qa));
                 }
-                // the weights' sum, while the tensor core works on them
-                float2 r2[4] = {};
-#pragma unroll
-                for (int i = 0; i < 128; i += 2)
-                    r2[(i >> 1) & 3] = __fadd2_rn(r2[(i >> 1) & 3], make_float2(__uint_as_float(v[i >> 5][i & 31]),
-                                                                                 __uint_as_float(v[i >> 5][(i & 31) + 1])));
+                tile_of(t + 1);  // (the loads it needs, before they are waited for)
+                pr_weights(v[2], pw[0], r2, scale, m_run, false);
+                tmem_st16(trow + 32, pw[0]);
+                if (kPrFirst == 96) {
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(bar(P_FULL + 2 * qa));
+                }
+                pr_weights(v[3], pw[1], r2, scale, m_run, false);
+                tmem_st16(trow + 48, pw[1]);
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(bar(P_FULL + 2 * qa + 1));
                 const float2 r1 = __fadd2_rn(__fadd2_rn(r2[0], r2[1]), __fadd2_rn(r2[2], r2[3]));
                 l_run += r1.x + r1.y;
             }
@@ -626,7 +651,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             __syncwarp();
             tc_fence_after();
             const bool row_ok = r < TQ * G && itok < w.ntok;
-            const int64_t qrow_off = ((int64_t)(w.row0 + itok) * Hq + (int64_t)w.g * G + r % G) * D;
+            const int64_t qrow_off = ((int64_t)(w.row0 + itok) * Hq + w.g * G + hrow) * D;
             const int p = w.p0 + itok, nt = w.nt;  // this row's position; the item's tiles
             const PrNotes &nb = notes[k & 1];
             const int n_notes = nb.n * 4;
@@ -663,7 +688,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             const bool blind = p < 0;  // the row sees nothing: zeros
             const float inv = blind || nt == 0 ? 0.f : 1.f / l_run;
             const bool rec = a.KS > 1;
-            float *recp = a.ws + (((int64_t)w.ks * a.T + w.row0 + itok) * Hq + (int64_t)w.g * G + r % G) * pr_record<D>();
+            float *recp = a.ws + (((int64_t)w.ks * a.T + w.row0 + itok) * Hq + w.g * G + hrow) * pr_record<D>();
             const unsigned long long orow =
                 !row_ok || dead ? 0ull
                                 : rec ? reinterpret_cast<unsigned long long>(recp)
@@ -676,13 +701,18 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 for (int i = 0; i < 8; ++i)
                     *reinterpret_cast<uint4 *>(xb + lane * 128 + ((i ^ (lane & 7)) * 16)) = x[i];
                 __syncwarp();
+                // (all loads first: the compiler cannot know that the stores go elsewhere)
+                uint4 y[8];
+                unsigned long long dst[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int rr = i * 4 + lane / 8, ch = lane % 8;
-                    const unsigned long long dst = __shfl_sync(0xffffffffu, orow, rr);
-                    const uint4 y = *reinterpret_cast<const uint4 *>(xb + rr * 128 + ((ch ^ (rr & 7)) * 16));
-                    if (dst) *reinterpret_cast<uint4 *>(dst + part * 128 + ch * 16) = y;
+                    const int rr = i * 4 + lane / 8;
+                    y[i] = *reinterpret_cast<const uint4 *>(xb + rr * 128 + ((lane % 8) ^ (rr & 7)) * 16);
+                    dst[i] = __shfl_sync(0xffffffffu, orow, rr);
                 }
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (dst[i]) *reinterpret_cast<uint4 *>(dst[i] + part * 128 + lane % 8 * 16) = y[i];
                 __syncwarp();
             };
             if (rec) {
