@@ -59,8 +59,8 @@ int prompt_shape(const kv_pool *p, int layout, int S, int Hq, int T, int max_q, 
 }
 
 template <int D>
-int prompt_run(const CUtensorMap *tmap, const CUtensorMap &qmap, const kvp::PromptArgs &a, int sm_count,
-               cudaStream_t st)
+int prompt_run(const CUtensorMap *tmap, const CUtensorMap &qmap, const CUtensorMap &omap, const kvp::PromptArgs &a,
+               int sm_count, cudaStream_t st)
 {
     static std::atomic<bool> attr_set{false};
     const size_t smem = kvp::prompt_smem_bytes<D>();
@@ -85,7 +85,7 @@ int prompt_run(const CUtensorMap *tmap, const CUtensorMap &qmap, const kvp::Prom
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, kvp::prompt_attn_kernel<D>, *tmap, qmap, a) != cudaSuccess) return KV_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, kvp::prompt_attn_kernel<D>, *tmap, qmap, omap, a) != cudaSuccess) return KV_ERR_CUDA;
     kvp_note_stream(st, false);
     if (a.KS == 1) return KV_OK;
     const int64_t rows = (int64_t)a.T * a.Hkv * a.G;
@@ -154,12 +154,14 @@ int paged_prompt_attn(kv_pool *p, int layout, const uint16_t *q, uint16_t *out, 
     a.sign = scale > 0.f ? 1.f : scale < 0.f ? -1.f : 0.f;
     a.qk_scale = scale == 0.f ? 1.f : std::fabs(scale) * 1.4426950408889634f;
     const cudaStream_t st = (cudaStream_t)stream;
-    // q as [T][Hq][d]: a box is half the columns of TQ tokens x G heads
-    CUtensorMap qmap;
+    // q and out as [T][Hq][d]: boxes of 64 columns of G heads, a Q tile's tokens
+    // of q, a warp's rows of out
+    CUtensorMap qmap, omap;
     rc = kvp_tmap_3d(&qmap, q, s.D, Hq, T, 64, s.G, kvp::kPrRows / s.G);
+    if (rc == KV_OK) rc = kvp_tmap_3d(&omap, out, s.D, Hq, T, 64, s.G, 32 / s.G);
     if (rc) return rc;
-    return s.D == 64 ? prompt_run<64>(&p->tmap[layout], qmap, a, p->sm_count, st)
-                     : prompt_run<128>(&p->tmap[layout], qmap, a, p->sm_count, st);
+    return s.D == 64 ? prompt_run<64>(&p->tmap[layout], qmap, omap, a, p->sm_count, st)
+                     : prompt_run<128>(&p->tmap[layout], qmap, omap, a, p->sm_count, st);
 }
 
 }  // extern "C"

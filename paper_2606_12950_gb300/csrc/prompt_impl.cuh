@@ -45,16 +45,27 @@ constexpr int kPrKeys = 128;   // keys per tile: S's N, P.V's K
 constexpr int kPrFirst = 96;   // keys whose weights are handed over first: the tensor core, which takes the Q
                                // tiles in turn, should not run out of them before the others are there
 constexpr int kPrStages = 2;
+constexpr int kPrSlots = 4;    // published items: the softmax warps hold one until its output is written
 constexpr int kPrSoft = kPrTiles * 128;     // softmax threads, one per row
 constexpr int kPrThreads = kPrSoft + 128;   // + K and V load warps, MMA warp, scheduling warp
 // Registers a thread, by warpgroup: launched with 168; a softmax thread holds a
-// row's 128 scores, the others need fewer.  2 x 128 x 216 + 128 x 72 = 384 x 168.
-constexpr int kPrRegsLaunch = 168, kPrRegsSoft = 216, kPrRegsOther = 72;
+// row's 128 scores, the others need fewer.  2 x 128 x 200 + 128 x 104 = 384 x 168.
+constexpr int kPrRegsLaunch = 168, kPrRegsSoft = 200, kPrRegsOther = 104;
 static_assert(kPrSoft * kPrRegsSoft + 128 * kPrRegsOther <= kPrThreads * kPrRegsLaunch, "what the launch holds");
 constexpr int kPrMasked = 16;  // masked tiles of an item: 3 on the diagonal, 3 at the window's edge, 2 of sinks at most
 constexpr int kPrMaxSplits = 16;
-// TMEM per Q tile: S [0, 128) fp32, P over S's first 64 columns (bf16 pairs), O [128, 128 + d)
-constexpr uint32_t kPrTmemCols = 256;
+// TMEM's 512 columns.  At d = 128: per Q tile S (128, fp32) with P (64, bf16
+// pairs) over it, and O (128).  At d = 64 O takes half of that and P has columns
+// of its own: S of the next tile is computed while the softmax still works on
+// this one, so that only the softmax's own time counts.
+constexpr uint32_t kPrTmem = 512;
+template <int D>
+struct PrCols {
+    static constexpr bool SEP = D == 64;  // P apart from S
+    static __device__ __forceinline__ uint32_t s(int q) { return SEP ? q * 128 : q * 256; }
+    static __device__ __forceinline__ uint32_t p(int q) { return SEP ? 256 + q * 64 : q * 256; }
+    static __device__ __forceinline__ uint32_t o(int q) { return SEP ? 384 + q * 64 : q * 256 + 128; }
+};
 
 struct PromptArgs {
     const uint16_t *q;
@@ -123,10 +134,10 @@ struct PrSmem {
     static constexpr uint32_t ST_OFF = kPrTiles * Q_TILE;
     static constexpr uint32_t X_OFF = ST_OFF + kPrStages * STAGE;       // 4 KB per softmax warp for the output
     static constexpr uint32_t BAR_OFF = X_OFF + kPrSoft / 32 * 4096;
-    static constexpr int NBARS = 32;
+    static constexpr int NBARS = 36;
     static constexpr uint32_t SLOT_OFF = BAR_OFF + NBARS * 8;
-    static constexpr uint32_t ITEM_OFF = SLOT_OFF + 16;                 // [2] PrItem
-    static constexpr uint32_t NOTE_OFF = ITEM_OFF + 2 * sizeof(PrItem); // [2] PrNotes
+    static constexpr uint32_t ITEM_OFF = SLOT_OFF + 16;                 // [kPrSlots] PrItem
+    static constexpr uint32_t NOTE_OFF = ITEM_OFF + kPrSlots * sizeof(PrItem); // [2] PrNotes
     static constexpr uint32_t BYTES = NOTE_OFF + 2 * (kPrMasked * 5 + 1) * 4;
 };
 // noted rows of an item's masked tiles
@@ -142,60 +153,135 @@ __device__ __forceinline__ uint32_t pr_pack(float lo, float hi)
     return *reinterpret_cast<uint32_t *>(&v);
 }
 
-// Item i (a converged warp); ntok = 0 where there is none.
-__device__ __forceinline__ PrItem pr_item(const PromptArgs &a, int i, int TT, int lane)
-{
-    PrItem w{};
-    w.ks = i % a.KS;
-    i /= a.KS;
-    w.g = i % a.Hkv;
-    const int tile = a.tiles - 1 - i / a.Hkv;  // the longest key ranges first
-    int before = 0;  // row tiles of the sequences before
-    for (int s0 = 0; s0 < a.S; s0 += 32) {
-        const int s = s0 + lane;
-        int cnt = 0;
-        if (s < a.S) cnt = max(0, a.starts[s + 1] - a.starts[s]);
-        const int nt = (cnt + TT - 1) / TT;
-        int incl = nt;
+// Row tiles in the order of their key ranges, the longest first, for up to 32
+// sequences (one a lane): CTAs that take every P-th of them then end at about
+// the same time (five causal prompts of 700 to 2500 tokens, 16 heads of 64: the
+// longest-running CTA had twice the shortest's work with the tiles in sequence
+// order).
+struct PrOrder {
+    int32_t start, n;     // this lane's sequence: first row of q, length
+    int32_t ctx, nq, nt;  // tokens before the chunk (>= 0), the chunk's, its row tiles
+    int32_t reach;        // most keys of a tile by this measure, in kUnits
+    static constexpr int kUnits = 64;
+    // tiles of this lane's sequence with at least kUnits x keys up to their last
+    // token (or the reach): the last ones.  (The quotient need not be exact, only
+    // the same for the same x and never smaller for a larger one.)
+    __device__ __forceinline__ int at_least(int32_t x, float inv) const
+    {
+        if (nt == 0 || x > min((ctx + nq) / kUnits, reach)) return 0;
+        return nt - max(0, min(nt - 1, __float2int_ru((float)(x * kUnits - ctx) * inv) - 1));
+    }
+    // the tile of rank `rank`: its lane (-1: none), and its number in the sequence
+    __device__ __forceinline__ int find(int rank, int TT, int lane, int &tile) const
+    {
+        if ((int)__reduce_add_sync(0xffffffffu, (unsigned)nt) <= rank) return -1;
+        const float inv = 1.f / (float)TT;
+        int32_t lo = -1, hi = reach + 1;  // count(lo) > rank >= count(hi)
+        while (hi - lo > 1) {
+            const int32_t mid = lo + (hi - lo) / 2;
+            if ((int)__reduce_add_sync(0xffffffffu, (unsigned)at_least(mid, inv)) > rank)
+                lo = mid;
+            else
+                hi = mid;
+        }
+        const int here = at_least(lo, inv), more = at_least(lo + 1, inv);
+        const int j = rank - (int)__reduce_add_sync(0xffffffffu, (unsigned)more);  // among those with lo keys
+        int incl = here - more;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
             const int v = __shfl_up_sync(0xffffffffu, incl, off);
             if (lane >= off) incl += v;
         }
-        const unsigned hit = __ballot_sync(0xffffffffu, before + incl > tile);
-        if (hit) {
-            const int l = __ffs((int)hit) - 1;
-            const int t0 = before + __shfl_sync(0xffffffffu, incl - nt, l);
-            const int nq = __shfl_sync(0xffffffffu, cnt, l);
-            w.s = s0 + l;
-            const int i0 = (tile - t0) * TT;
-            const int32_t st = a.starts[w.s];
-            int32_t n = a.ctx_lens[w.s];
-            w.row0 = st + i0;
-            if (st < 0 || (int64_t)st + nq > a.T) {  // a bad array: nothing of it is touched
-                report(a.err, KV_ERR_DEVICE_BOUNDS);
-                return w;
-            }
-            w.ntok = min(TT, nq - i0);
-            const int32_t cap = a.max_blocks * a.bs;
-            if (n < nq || n > cap) {
-                report(a.err, KV_ERR_DEVICE_BOUNDS);
-                n = n > cap ? cap : max(n, 0);
-            }
-            w.p0 = n - nq + i0;
-            w.p1 = w.p0 + w.ntok - 1;
-            if (w.p1 < 0) return w;
-            w.lo = a.window > 0 ? max(0, w.p0 - a.window + 1) : 0;
-            const int32_t sk = min(a.sinks, w.lo);  // sinks before the window
-            w.head = (sk + kPrKeys - 1) / kPrKeys;
-            w.gap = max(0, w.lo / kPrKeys - w.head);
-            const int32_t all = w.p1 / kPrKeys + 1 - w.gap;
-            w.t0 = (int32_t)((int64_t)w.ks * all / a.KS);
-            w.nt = (int32_t)((int64_t)(w.ks + 1) * all / a.KS) - w.t0;
-            return w;
-        }
-        before += __shfl_sync(0xffffffffu, incl, 31);
+        const int l = __ffs((int)__ballot_sync(0xffffffffu, incl > j)) - 1;
+        tile = __shfl_sync(0xffffffffu, nt - here + j - (incl - (here - more)), l);
+        return l;
     }
+};
+__device__ __forceinline__ PrOrder pr_order(const PromptArgs &a, int TT, int lane)
+{
+    PrOrder o{};
+    if (lane < a.S) {
+        o.start = a.starts[lane];
+        o.n = a.ctx_lens[lane];
+        o.nq = max(0, a.starts[lane + 1] - o.start);
+        o.nt = (o.nq + TT - 1) / TT;
+        o.ctx = max(0, min(o.n, a.max_blocks * a.bs) - o.nq);
+    }
+    o.reach = (int32_t)__reduce_max_sync(0xffffffffu, (unsigned)(o.ctx + o.nq)) / PrOrder::kUnits;
+    if (a.window > 0) o.reach = min(o.reach, (a.window + TT) / PrOrder::kUnits);
+    return o;
+}
+
+// Item i (a converged warp); ntok = 0 where there is none.  `order`: the row
+// tiles by their key ranges, or null: in sequence order, the last first.
+__device__ __forceinline__ PrItem pr_item(const PromptArgs &a, int i, int TT, int lane, const PrOrder *order)
+{
+    PrItem w{};
+    w.ks = i % a.KS;
+    i /= a.KS;
+    w.g = i % a.Hkv;
+    const int rank = i / a.Hkv;
+    int tile = a.tiles - 1 - rank, st = 0, nq = 0;
+    int32_t n = 0;
+    if (order) {
+        const int l = order->find(rank, TT, lane, tile);
+        if (l < 0) return w;
+        w.s = l;
+        st = __shfl_sync(0xffffffffu, order->start, l);
+        nq = __shfl_sync(0xffffffffu, order->nq, l);
+        n = __shfl_sync(0xffffffffu, order->n, l);
+    } else {
+        int l = -1;
+        for (int s0 = 0, before = 0; s0 < a.S; s0 += 32) {  // before: row tiles of the sequences before
+            const int s = s0 + lane;
+            int first = 0, cnt = 0;
+            if (s < a.S) {
+                first = a.starts[s];
+                cnt = max(0, a.starts[s + 1] - first);
+            }
+            const int nt = (cnt + TT - 1) / TT;
+            int incl = nt;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, incl, off);
+                if (lane >= off) incl += v;
+            }
+            const unsigned hit = __ballot_sync(0xffffffffu, before + incl > tile);
+            if (hit) {
+                l = __ffs((int)hit) - 1;
+                tile -= before + __shfl_sync(0xffffffffu, incl - nt, l);
+                st = __shfl_sync(0xffffffffu, first, l);
+                nq = __shfl_sync(0xffffffffu, cnt, l);
+                w.s = s0 + l;
+                break;
+            }
+            before += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        if (l < 0) return w;
+        n = a.ctx_lens[w.s];
+    }
+    const int i0 = tile * TT;  // its first token in the chunk
+    w.row0 = st + i0;
+    if (st < 0 || (int64_t)st + nq > a.T) {  // a bad array: nothing of it is touched
+        report(a.err, KV_ERR_DEVICE_BOUNDS);
+        return w;
+    }
+    w.ntok = min(TT, nq - i0);
+    const int32_t cap = a.max_blocks * a.bs;
+    if (n < nq || n > cap) {
+        report(a.err, KV_ERR_DEVICE_BOUNDS);
+        n = n > cap ? cap : max(n, 0);
+    }
+    w.p0 = n - nq + i0;
+    w.p1 = w.p0 + w.ntok - 1;
+    if (w.p1 < 0) return w;
+    w.lo = a.window > 0 ? max(0, w.p0 - a.window + 1) : 0;
+    const int32_t sk = min(a.sinks, w.lo);  // sinks before the window
+    w.head = (sk + kPrKeys - 1) / kPrKeys;
+    w.gap = max(0, w.lo / kPrKeys - w.head);
+    const int32_t all = w.p1 / kPrKeys + 1 - w.gap;
+    w.t0 = (int32_t)((int64_t)w.ks * all / a.KS);
+    w.nt = (int32_t)((int64_t)(w.ks + 1) * all / a.KS) - w.t0;
     return w;
 }
 
@@ -254,11 +340,12 @@ __device__ __forceinline__ void pr_weights(const uint32_t (&x)[32], uint32_t (&p
 template <int D>
 __global__ void __launch_bounds__(kPrThreads, 1)
 prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap qmap,
-                   const __grid_constant__ PromptArgs a)
+                   const __grid_constant__ CUtensorMap omap, const __grid_constant__ PromptArgs a)
 {
     using L = PrSmem<D>;
     constexpr int HALVES = L::HALVES;
-    constexpr uint32_t O_COL = kPrKeys;
+    using C = PrCols<D>;
+    constexpr bool SEP = C::SEP;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t sbase = smem_u32(smem);
@@ -269,10 +356,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     // K and V of a stage loaded, free (V of a masked tile: loaded is V_RAW, and
     // FULL_V follows its check); per Q tile: S done, P of the first kPrFirst keys and of the others written, O done; an item's Q
-    // loaded, used; an item published, read; its notes complete, read; all MMAs done
+    // loaded, used; an item published, read; its notes complete, read; per Q
+    // tile (SEP): S read; all MMAs done
     constexpr int FULL_K = 0, EMPTY_K = 2, FULL_V = 4, EMPTY_V = 6, V_RAW = 8;
-    constexpr int S_FULL = 10, P_FULL = 12, O_DONE = 16, Q_FULL = 18, Q_FREE = 19, ITEM_FULL = 20, ITEM_EMPTY = 22,
-                  NOTED = 24, NOTE_FREE = 26, FIN = 28;
+    constexpr int S_FULL = 10, P_FULL = 12, O_DONE = 16, Q_FULL = 18, Q_FREE = 19, NOTED = 20, NOTE_FREE = 22,
+                  S_FREE = 24, ITEM_FULL = 26, ITEM_EMPTY = ITEM_FULL + kPrSlots, FIN = ITEM_EMPTY + kPrSlots;
     static_assert(kPrStages == 2 && kPrTiles == 2 && FIN < L::NBARS, "the barriers' numbers");
 
     const int tid = threadIdx.x, lane = tid & 31;
@@ -281,15 +369,17 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
     constexpr int K_WARP = kPrSoft / 32, V_WARP = K_WARP + 1, MMA_WARP = K_WARP + 2, PLAN_WARP = K_WARP + 3;
 
     if (tid == 0) {
-        for (int i = 0; i < L::NBARS; ++i)
-            mbar_init(bar(i), i >= P_FULL && i < O_DONE ? 128
-                              : i >= ITEM_EMPTY && i < NOTED          ? kPrSoft / 32 + 3
-                              : i >= NOTE_FREE && i < FIN             ? kPrSoft / 32
-                                                                      : 1);
+        for (int i = 0; i < L::NBARS; ++i) {
+            int n = 1;
+            if ((i >= P_FULL && i < O_DONE) || (i >= S_FREE && i < ITEM_FULL)) n = 128;
+            if (i >= NOTE_FREE && i < S_FREE) n = kPrSoft / 32;
+            if (i >= ITEM_EMPTY && i < FIN) n = kPrSoft / 32 + 3;
+            mbar_init(bar(i), n);
+        }
         fence_mbar_init();
     }
     if (warp == 0) {
-        tmem_alloc(smem_u32(tslot), kPrTiles * kPrTmemCols);
+        tmem_alloc(smem_u32(tslot), kPrTmem);
         tmem_relinquish();
     }
     if (tid == 32) prefetch_tensormap(&tmap);
@@ -305,10 +395,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
     // item k as the planning warp published it; each reading warp gives its slot
     // back at once
     auto item = [&](int k) {
-        wait_phase(bar(ITEM_FULL + (k & 1)), (uint32_t)(k >> 1) & 1u, a.err, dead);
-        const PrItem w = items[k & 1];
+        wait_phase(bar(ITEM_FULL + k % kPrSlots), (uint32_t)(k / kPrSlots) & 1u, a.err, dead);
+        const PrItem w = items[k % kPrSlots];
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(ITEM_EMPTY + (k & 1)));
+        if (lane == 0) mbar_arrive(bar(ITEM_EMPTY + k % kPrSlots));
         return w;
     };
 
@@ -316,27 +406,43 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
         reg_dec<kPrRegsOther>();
         if (warp == PLAN_WARP) {
             // ---- the items' order, Q, and the check of V in masked tiles ----
-            int next = blockIdx.x, pub = 0;  // next item to look up, items published
-            auto publish = [&]() {           // the next item that has tokens, or the end
+            int turn = 0, pub = 0;   // rounds of items looked up, items published
+            // (with an item a CTA the order is worth nothing)
+            const bool sorted = a.S <= 32 && a.n_items > (int)gridDim.x;
+            PrOrder order{};
+            if (sorted) order = pr_order(a, TT, lane);
+            auto look_up = [&]() {   // the next item that has tokens, or the end
                 PrItem w{};
                 w.s = -1;
-                while (next < a.n_items) {
-                    w = pr_item(a, next, TT, lane);
-                    next += gridDim.x;
+                const int P = gridDim.x, b = blockIdx.x;
+                while ((int64_t)turn * P < a.n_items) {  // an item of each round of P, forwards and backwards in turn
+                    const int64_t i = (int64_t)turn * P + (turn & 1 ? P - 1 - b : b);
+                    ++turn;
+                    if (i >= a.n_items) continue;
+                    w = pr_item(a, (int)i, TT, lane, sorted ? &order : nullptr);
                     if (w.ntok > 0) break;
                     w.s = -1;
                 }
-                if (pub >= 2) wait_phase(bar(ITEM_EMPTY + (pub & 1)), (uint32_t)((pub >> 1) - 1) & 1u, a.err, dead);
+                return w;
+            };
+            auto publish = [&](const PrItem &w) {
+                const int sl = pub % kPrSlots;
+                if (pub >= kPrSlots)
+                    wait_phase(bar(ITEM_EMPTY + sl), (uint32_t)(pub / kPrSlots - 1) & 1u, a.err, dead);
                 if (lane == 0) {
-                    items[pub & 1] = w;
-                    mbar_arrive(bar(ITEM_FULL + (pub & 1)));
+                    items[sl] = w;
+                    mbar_arrive(bar(ITEM_FULL + sl));
                 }
                 __syncwarp();
                 ++pub;
-                return w;
             };
             const uint64_t pol = l2_policy_evict_normal();
-            PrItem w = publish();
+            // An item is published while the one before is worked on, and looked up
+            // (3000 clocks and more) while the one before that is.
+            PrItem w = look_up();
+            publish(w);
+            PrItem after{};
+            bool have = false;  // `after` has been looked up
             int qn = 0, cnt = 0;        // items with Q loaded; tiles so far
             uint32_t vn = 0;            // parities: bit st, masked tiles of stage st so far
             for (int k = 0; w.s >= 0; ++k) {
@@ -353,7 +459,17 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                     __syncwarp();
                     ++qn;
                 }
-                const PrItem after = publish();  // the other warps may go on to it
+                PrItem next{};
+                bool posted = false;
+                auto post_next = [&]() {
+                    if (posted) return;
+                    if (!have) after = look_up();
+                    next = after;
+                    publish(next);
+                    have = next.s < 0;  // nothing more to look up
+                    posted = true;
+                };
+                if (have) post_next();
                 // V of masked tiles: rows that no query sees are cleared, and so
                 // are rows with a NaN or an infinity, which are noted
                 PrNotes &nb = notes[k & 1];
@@ -361,7 +477,15 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 if (k >= 2) wait_phase(bar(NOTE_FREE + (k & 1)), (uint32_t)((k >> 1) - 1) & 1u, a.err, dead);
                 for (int t = 0; t < w.nt; ++t, ++cnt) {
                     const int k0 = w.key0(t), st = cnt % kPrStages;
-                    if (!w.masked(a, k0)) continue;
+                    if (!w.masked(a, k0)) {
+                        if (!posted) {
+                            post_next();
+                        } else if (!have) {
+                            after = look_up();
+                            have = true;
+                        }
+                        continue;
+                    }
                     wait_phase(bar(V_RAW + st), vn >> st & 1u, a.err, dead);
                     vn ^= 1u << st;
                     uint8_t *vt = smem + L::ST_OFF + st * L::STAGE + L::KV_TILE;
@@ -397,13 +521,15 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar(FULL_V + st));
+                    if (t > 0) post_next();  // (the first tile's check is waited for first)
                 }
+                post_next();
                 if (lane == 0) {
                     nb.n = n_masked;
                     mbar_arrive(bar(NOTED + (k & 1)));
                 }
                 __syncwarp();
-                w = after;
+                w = next;
             }
         } else if (warp != MMA_WARP) {
             // ---- TMA producer warps, one of K and one of V: one box per lane ----
@@ -455,8 +581,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 for (int c = max(0, cnt - kPrStages); c < cnt; ++c)
                     wait_phase(bar(full0 + c % kPrStages), (uint32_t)(c / kPrStages) & 1u, a.err, dead);
         } else {
-            // ---- MMA issuer: S_0(0) S_1(0) | PV_0(t) S_0(t+1) PV_1(t) S_1(t+1) | ... ; the
-            // pipe runs one thread's MMAs in issue order, so S_a(t+1), or S_a(0) of
+            // ---- MMA issuer: S_0(0) S_1(0) | PV_0(t) S_0(t+1) PV_1(t) S_1(t+1) | ... (SEP:
+            // S_0(t+1) S_1(t+1) PV_0(t) PV_1(t)); the pipe runs one thread's MMAs in issue order, so S_a(t+1), or S_a(0) of
             // the next item, overwrites P only after PV_a(t) has read it.  O is
             // overwritten by PV_a(0) of the next item once its P is there, which
             // the softmax warps write after they have read O ----
@@ -465,12 +591,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             constexpr uint32_t ID_O = idesc_bf16_f32(kPrRows, D, 0, 1);
             int cnt = 0, qn = 0;           // tiles, items with Q so far
             uint32_t pn = 0;               // parities: bit q, tiles of Q tile q so far
+            uint32_t sn = 0, used = 0;     // (SEP) waits on S_FREE so far; S written before
             auto issue_s = [&](int q, int c) {
                 const uint32_t ka = sbase + L::ST_OFF + (c % kPrStages) * L::STAGE;
                 const uint32_t qa = sbase + q * L::Q_TILE;
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk)
-                    umma_bf16(tbase + q * kPrTmemCols, smem_desc_sw128(qa + (kk / 4) * L::Q_HALF + (kk % 4) * 32, 16, 1024),
+                    umma_bf16(tbase + C::s(q), smem_desc_sw128(qa + (kk / 4) * L::Q_HALF + (kk % 4) * 32, 16, 1024),
                               smem_desc_sw128(ka + (kk / 4) * L::KV_HALF + (kk % 4) * 32, 16, 1024), ID_S, kk > 0, el);
                 umma_commit(bar(S_FULL + q), el);
             };
@@ -479,7 +606,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 constexpr int STEPS = kPrKeys / 16, FIRST = kPrFirst / 16;
 #pragma unroll
                 for (int kk = half ? FIRST : 0; kk < (half ? STEPS : FIRST); ++kk) {
-                    umma_bf16_tmem_a(tbase + q * kPrTmemCols + O_COL, tbase + q * kPrTmemCols + kk * 8,
+                    umma_bf16_tmem_a(tbase + C::o(q), tbase + C::p(q) + kk * 8,
                                      smem_desc_sw128(va + kk * (16 * 128), L::KV_HALF, 1024), ID_O, more || kk > 0, el);
                 }
             };
@@ -494,13 +621,33 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 wait_phase(bar(Q_FULL), (uint32_t)qn & 1u, a.err, dead);
                 ++qn;
                 wait_k(cnt);
-                tc_fence_after();
-                for (int q = 0; q < nqt; ++q) issue_s(q, cnt);
+                // S of tile c for Q tile q; with SEP once the softmax has read the one before
+                auto next_s = [&](int q, int c) {
+                    if (SEP) {
+                        if (used >> q & 1u) {
+                            wait_phase(bar(S_FREE + q), sn >> q & 1u, a.err, dead);
+                            sn ^= 1u << q;
+                        }
+                        used |= 1u << q;
+                    }
+                    tc_fence_after();
+                    issue_s(q, c);
+                };
+                for (int q = 0; q < nqt; ++q) next_s(q, cnt);
                 umma_commit(bar(EMPTY_K + cnt % kPrStages), el);
                 if (w.nt == 1) umma_commit(bar(Q_FREE), el);
                 for (int t = 0; t < w.nt; ++t, ++cnt) {
                     const int st = cnt % kPrStages;
                     const bool next = t + 1 < w.nt;
+                    auto k_used = [&]() {  // K of tile cnt + 1, and Q after its last tile
+                        umma_commit(bar(EMPTY_K + (cnt + 1) % kPrStages), el);
+                        if (t + 2 == w.nt) umma_commit(bar(Q_FREE), el);
+                    };
+                    if (SEP && next) {
+                        wait_k(cnt + 1);
+                        for (int q = 0; q < nqt; ++q) next_s(q, cnt + 1);
+                        k_used();
+                    }
                     wait_phase(bar(FULL_V + st), (uint32_t)(cnt / kPrStages) & 1u, a.err, dead);
                     for (int q = 0; q < nqt; ++q) {
                         wait_phase(bar(P_FULL + 2 * q), pn >> q & 1u, a.err, dead);
@@ -510,16 +657,12 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                         pn ^= 1u << q;
                         tc_fence_after();
                         issue_pv(q, cnt, 1, true);
-                        if (!next) umma_commit(bar(O_DONE + q), el);
+                        if (SEP || !next) umma_commit(bar(O_DONE + q), el);
                         if (q == nqt - 1) umma_commit(bar(EMPTY_V + st), el);
-                        if (next) {
+                        if (!SEP && next) {
                             if (q == 0) wait_k(cnt + 1);
-                            tc_fence_after();
-                            issue_s(q, cnt + 1);
-                            if (q == nqt - 1) {
-                                umma_commit(bar(EMPTY_K + (cnt + 1) % kPrStages), el);
-                                if (t + 2 == w.nt) umma_commit(bar(Q_FREE), el);  // Q's last use
-                            }
+                            next_s(q, cnt + 1);
+                            if (q == nqt - 1) k_used();
                         }
                     }
                 }
@@ -533,21 +676,22 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
         reg_inc<kPrRegsSoft>();
         const int qa = tid / kPrRows, r = tid % kPrRows;
         const int itok = qa * TQ + r / G, hrow = r % G;  // the row's token in the item, its head in the group
-        const uint32_t trow = tbase + qa * kPrTmemCols + ((uint32_t)((warp % 4) * 32) << 16);
+        const uint32_t trow = tbase + ((uint32_t)((warp % 4) * 32) << 16);
+        const uint32_t ts = trow + C::s(qa), tp = trow + C::p(qa), to = trow + C::o(qa);
         const float scale = a.qk_scale;
         uint8_t *xb = smem + L::X_OFF + warp * 4096;
-        int pn = 0, on = 0;  // tiles, and items with tiles, of this Q tile so far
+        int pn = 0, on = 0;  // tiles of this Q tile, waits on O_DONE so far
         for (int k = 0;; ++k) {
             // read where needed: its fields and a row's scores together are more
             // than the registers
-            const PrItem &w = items[k & 1];
-            wait_phase(bar(ITEM_FULL + (k & 1)), (uint32_t)(k >> 1) & 1u, a.err, dead);
+            const PrItem &w = items[k % kPrSlots];
+            wait_phase(bar(ITEM_FULL + k % kPrSlots), (uint32_t)(k / kPrSlots) & 1u, a.err, dead);
             if (w.s < 0) break;
             auto give_back = [&]() {  // the item and its notes
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(bar(NOTE_FREE + (k & 1)));
-                    mbar_arrive(bar(ITEM_EMPTY + (k & 1)));
+                    mbar_arrive(bar(ITEM_EMPTY + k % kPrSlots));
                 }
             };
             if (qa * TQ >= w.ntok) {  // no tokens in this Q tile
@@ -572,11 +716,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 __syncwarp();
                 tc_fence_after();
                 uint32_t v[4][32];  // the row's scores
-                tmem_ld32(trow, v[0]);
-                tmem_ld32(trow + 32, v[1]);
+                tmem_ld32(ts, v[0]);
+                tmem_ld32(ts + 32, v[1]);
                 tmem_wait_ld();
-                tmem_ld32(trow + 64, v[2]);
-                tmem_ld32(trow + 96, v[3]);
+                tmem_ld32(ts + 64, v[2]);
+                tmem_ld32(ts + 96, v[3]);
                 if (mk) {
                     const int wl = a.window > 0 ? hi - a.window : -1;
                     if (a.sign != 1.f) pr_times(v[0], a.sign), pr_times(v[1], a.sign);
@@ -591,6 +735,15 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 pr_max(v[0], mx);
                 pr_max(v[1], mx);
                 tmem_wait_ld();
+                if (SEP) {
+                    tc_fence_before();
+                    mbar_arrive(bar(S_FREE + qa));
+                    if (t > 0) {  // the tile before: its P read, its O there
+                        wait_phase(bar(O_DONE + qa), (uint32_t)on++ & 1u, a.err, dead);
+                        __syncwarp();
+                        tc_fence_after();
+                    }
+                }
                 pr_max(v[2], mx);
                 pr_max(v[3], mx);
                 const float cmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
@@ -606,11 +759,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                         uint32_t o[16];
 #pragma unroll 1
                         for (int cb = 0; cb < D / 16; ++cb) {
-                            tmem_ld16(trow + O_COL + cb * 16, o);
+                            tmem_ld16(to + cb * 16, o);
                             tmem_wait_ld();
 #pragma unroll
                             for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * al);
-                            tmem_st16(trow + O_COL + cb * 16, o);
+                            tmem_st16(to + cb * 16, o);
                         }
                     }
                     if (rise) m_run = cmax;
@@ -621,9 +774,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 uint32_t pw[2][16];
                 float2 r2[4];
                 pr_weights(v[0], pw[0], r2, scale, m_run, true);
-                tmem_st16(trow, pw[0]);
+                tmem_st16(tp, pw[0]);
                 pr_weights(v[1], pw[1], r2, scale, m_run, false);
-                tmem_st16(trow + 16, pw[1]);
+                tmem_st16(tp + 16, pw[1]);
                 if (kPrFirst == 64) {
                     tmem_wait_st();
                     tc_fence_before();
@@ -631,14 +784,14 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 }
                 tile_of(t + 1);  // (the loads it needs, before they are waited for)
                 pr_weights(v[2], pw[0], r2, scale, m_run, false);
-                tmem_st16(trow + 32, pw[0]);
+                tmem_st16(tp + 32, pw[0]);
                 if (kPrFirst == 96) {
                     tmem_wait_st();
                     tc_fence_before();
                     mbar_arrive(bar(P_FULL + 2 * qa));
                 }
                 pr_weights(v[3], pw[1], r2, scale, m_run, false);
-                tmem_st16(trow + 48, pw[1]);
+                tmem_st16(tp + 48, pw[1]);
                 tmem_wait_st();
                 tc_fence_before();
                 mbar_arrive(bar(P_FULL + 2 * qa + 1));
@@ -662,7 +815,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
 #pragma unroll 1
                 for (int cb = 0; cb < D / 32; ++cb) {
                     uint32_t o[32];
-                    tmem_ld32(trow + O_COL + cb * 32, o);
+                    tmem_ld32(to + cb * 32, o);
                     tmem_wait_ld();
 #pragma unroll 1
                     for (int b = 0; b < n_notes; ++b)
@@ -681,7 +834,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                                 o[i] = __float_as_uint(fmaf(pj, bf_lo(vr[cb * 32 + i]), __uint_as_float(o[i])));
                         }
                     __syncwarp();
-                    tmem_st32(trow + O_COL + cb * 32, o);
+                    tmem_st32(to + cb * 32, o);
                     tmem_wait_st();
                 }
             }
@@ -693,13 +846,27 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 !row_ok || dead ? 0ull
                                 : rec ? reinterpret_cast<unsigned long long>(recp)
                                       : reinterpret_cast<unsigned long long>(a.out + qrow_off);
+            const int g_out = w.g * G, tok_out = w.row0 + itok;  // (of lane 0: the box's corner)
             give_back();
-            // 128 bytes of each row through shared memory, so that eight lanes
-            // write 128 consecutive bytes
+            // 128 bytes of each row through shared memory.  A warp whose 32 rows are
+            // whole tokens of the chunk sends them as one TMA box; otherwise eight
+            // lanes write 128 consecutive bytes.
+            const bool box = !rec && 32 % G == 0 && __all_sync(0xffffffffu, orow != 0ull);
             auto send = [&](int part, const uint4 (&x)[8]) {
+                if (lane == 0) bulk_wait_read();  // a box before has been read
+                __syncwarp();
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     *reinterpret_cast<uint4 *>(xb + lane * 128 + ((i ^ (lane & 7)) * 16)) = x[i];
+                if (box) {
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_3d(&omap, smem_u32(xb), part * 64, g_out, tok_out);
+                        bulk_commit();
+                    }
+                    return;
+                }
                 __syncwarp();
                 // (all loads first: the compiler cannot know that the stores go elsewhere)
                 uint4 y[8];
@@ -719,7 +886,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
 #pragma unroll 1
                 for (int cb = 0; cb < D / 32 && nt > 0; ++cb) {
                     uint32_t o[32];
-                    tmem_ld32(trow + O_COL + cb * 32, o);
+                    tmem_ld32(to + cb * 32, o);
                     tmem_wait_ld();
                     uint4 x[8];
 #pragma unroll
@@ -735,8 +902,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 for (int cb = 0; cb < D / 64; ++cb) {
                     uint32_t o[2][32] = {};
                     if (nt > 0) {
-                        tmem_ld32(trow + O_COL + cb * 64, o[0]);
-                        tmem_ld32(trow + O_COL + cb * 64 + 32, o[1]);
+                        tmem_ld32(to + cb * 64, o[0]);
+                        tmem_ld32(to + cb * 64 + 32, o[1]);
                         tmem_wait_ld();
                     }
                     uint4 x[8];
@@ -755,11 +922,12 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             }
             tc_fence_before();  // O has been read: the next item's P may let it be overwritten
         }
+        if (lane == 0) bulk_wait_all();
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 0) tmem_dealloc(tbase, kPrTiles * kPrTmemCols);
+    if (warp == 0) tmem_dealloc(tbase, kPrTmem);
 }
 
 // Merge of the KS records of each (row, query head): a warp each, D / 32
