@@ -42,8 +42,11 @@ namespace kvp {
 constexpr int kPrRows = 128;   // rows of a Q tile: the MMA's M
 constexpr int kPrTiles = 2;    // Q tiles per item
 constexpr int kPrKeys = 128;   // keys per tile: S's N, P.V's K
-constexpr int kPrFirst = 96;   // keys whose weights are handed over first: the tensor core, which takes the Q
-                               // tiles in turn, should not run out of them before the others are there
+// Keys whose weights are handed over first: at d = 128, where S of the next tile
+// waits for P.V, 96, so that the tensor core, which takes the Q tiles in turn,
+// does not run out of them before the others are there; at d = 64 all.
+template <int D>
+constexpr int kPrFirst = D == 64 ? 128 : 96;
 constexpr int kPrStages = 2;
 constexpr int kPrSlots = 4;    // published items: the softmax warps hold one until its output is written
 constexpr int kPrSoft = kPrTiles * 128;     // softmax threads, one per row
@@ -294,6 +297,11 @@ __device__ __forceinline__ int32_t pr_pool_row(const PromptArgs &a, int s, int g
     return (int32_t)((int64_t)phys * a.rows_per_page + (int64_t)g * a.bs + (tok - blk * a.bs));
 }
 
+// wait_phase with its slow part out of the way
+__device__ __forceinline__ void pr_wait(uint32_t bar, uint32_t parity, int32_t *err, bool &dead)
+{
+    if (__builtin_expect(!mbar_try_wait(bar, parity), 0)) wait_phase(bar, parity, err, dead);
+}
 // bits 0 .. n of a word (none for n < 0, all from 31 on)
 __device__ __forceinline__ uint32_t pr_bits(int n) { return n < 0 ? 0u : 0xffffffffu >> (31 - min(n, 31)); }
 // 32 scores of a row: those of unseen tokens to -inf (column k is seen when
@@ -355,7 +363,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
     PrNotes *notes = reinterpret_cast<PrNotes *>(smem + L::NOTE_OFF);
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     // K and V of a stage loaded, free (V of a masked tile: loaded is V_RAW, and
-    // FULL_V follows its check); per Q tile: S done, P of the first kPrFirst keys and of the others written, O done; an item's Q
+    // FULL_V follows its check); per Q tile: S done, P of the first kPrFirst keys and of any others written, O done; an item's Q
     // loaded, used; an item published, read; its notes complete, read; per Q
     // tile (SEP): S read; all MMAs done
     constexpr int FULL_K = 0, EMPTY_K = 2, FULL_V = 4, EMPTY_V = 6, V_RAW = 8;
@@ -395,7 +403,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
     // item k as the planning warp published it; each reading warp gives its slot
     // back at once
     auto item = [&](int k) {
-        wait_phase(bar(ITEM_FULL + k % kPrSlots), (uint32_t)(k / kPrSlots) & 1u, a.err, dead);
+        pr_wait(bar(ITEM_FULL + k % kPrSlots), (uint32_t)(k / kPrSlots) & 1u, a.err, dead);
         const PrItem w = items[k % kPrSlots];
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(ITEM_EMPTY + k % kPrSlots));
@@ -428,7 +436,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             auto publish = [&](const PrItem &w) {
                 const int sl = pub % kPrSlots;
                 if (pub >= kPrSlots)
-                    wait_phase(bar(ITEM_EMPTY + sl), (uint32_t)(pub / kPrSlots - 1) & 1u, a.err, dead);
+                    pr_wait(bar(ITEM_EMPTY + sl), (uint32_t)(pub / kPrSlots - 1) & 1u, a.err, dead);
                 if (lane == 0) {
                     items[sl] = w;
                     mbar_arrive(bar(ITEM_FULL + sl));
@@ -447,7 +455,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             uint32_t vn = 0;            // parities: bit st, masked tiles of stage st so far
             for (int k = 0; w.s >= 0; ++k) {
                 if (w.nt > 0) {
-                    if (qn > 0) wait_phase(bar(Q_FREE), (uint32_t)(qn - 1) & 1u, a.err, dead);
+                    if (qn > 0) pr_wait(bar(Q_FREE), (uint32_t)(qn - 1) & 1u, a.err, dead);
                     if (lane == 0) {
                         const int nqt = (w.ntok + TQ - 1) / TQ;
                         mbar_arrive_expect_tx(bar(Q_FULL), (uint32_t)(nqt * HALVES * TQ * G * 128));
@@ -474,7 +482,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 // are rows with a NaN or an infinity, which are noted
                 PrNotes &nb = notes[k & 1];
                 int n_masked = 0;
-                if (k >= 2) wait_phase(bar(NOTE_FREE + (k & 1)), (uint32_t)((k >> 1) - 1) & 1u, a.err, dead);
+                if (k >= 2) pr_wait(bar(NOTE_FREE + (k & 1)), (uint32_t)((k >> 1) - 1) & 1u, a.err, dead);
                 for (int t = 0; t < w.nt; ++t, ++cnt) {
                     const int k0 = w.key0(t), st = cnt % kPrStages;
                     if (!w.masked(a, k0)) {
@@ -486,7 +494,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                         }
                         continue;
                     }
-                    wait_phase(bar(V_RAW + st), vn >> st & 1u, a.err, dead);
+                    pr_wait(bar(V_RAW + st), vn >> st & 1u, a.err, dead);
                     vn ^= 1u << st;
                     uint8_t *vt = smem + L::ST_OFF + st * L::STAGE + L::KV_TILE;
 #pragma unroll 1
@@ -558,7 +566,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                     const uint32_t n = __popc(__ballot_sync(0xffffffffu, y >= 0));
                     const uint32_t full = bar(is_v && w.masked(a, w.key0(t)) ? V_RAW + st : full0 + st);
                     if (cnt >= kPrStages)
-                        wait_phase(bar(empty0 + st), (uint32_t)(cnt / kPrStages - 1) & 1u, a.err, dead);
+                        pr_wait(bar(empty0 + st), (uint32_t)(cnt / kPrStages - 1) & 1u, a.err, dead);
                     if (lane == 0) {
                         if (bad || n == 0) {
                             if (bad) report(a.err, KV_ERR_DEVICE_BOUNDS);
@@ -579,7 +587,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             // drain: the last stages' loads have landed
             if (lane == 0)
                 for (int c = max(0, cnt - kPrStages); c < cnt; ++c)
-                    wait_phase(bar(full0 + c % kPrStages), (uint32_t)(c / kPrStages) & 1u, a.err, dead);
+                    pr_wait(bar(full0 + c % kPrStages), (uint32_t)(c / kPrStages) & 1u, a.err, dead);
         } else {
             // ---- MMA issuer: S_0(0) S_1(0) | PV_0(t) S_0(t+1) PV_1(t) S_1(t+1) | ... (SEP:
             // S_0(t+1) S_1(t+1) PV_0(t) PV_1(t)); the pipe runs one thread's MMAs in issue order, so S_a(t+1), or S_a(0) of
@@ -603,7 +611,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             };
             auto issue_pv = [&](int q, int c, int half, bool more) {
                 const uint32_t va = sbase + L::ST_OFF + (c % kPrStages) * L::STAGE + L::KV_TILE;
-                constexpr int STEPS = kPrKeys / 16, FIRST = kPrFirst / 16;
+                constexpr int STEPS = kPrKeys / 16, FIRST = kPrFirst<D> / 16;
 #pragma unroll
                 for (int kk = half ? FIRST : 0; kk < (half ? STEPS : FIRST); ++kk) {
                     umma_bf16_tmem_a(tbase + C::o(q), tbase + C::p(q) + kk * 8,
@@ -611,21 +619,21 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 }
             };
             auto wait_k = [&](int c) {
-                wait_phase(bar(FULL_K + c % kPrStages), (uint32_t)(c / kPrStages) & 1u, a.err, dead);
+                pr_wait(bar(FULL_K + c % kPrStages), (uint32_t)(c / kPrStages) & 1u, a.err, dead);
             };
             for (int k = 0;; ++k) {
                 const PrItem w = item(k);
                 if (w.s < 0) break;
                 if (w.nt == 0) continue;
                 const int nqt = (w.ntok + TQ - 1) / TQ;
-                wait_phase(bar(Q_FULL), (uint32_t)qn & 1u, a.err, dead);
+                pr_wait(bar(Q_FULL), (uint32_t)qn & 1u, a.err, dead);
                 ++qn;
                 wait_k(cnt);
                 // S of tile c for Q tile q; with SEP once the softmax has read the one before
                 auto next_s = [&](int q, int c) {
                     if (SEP) {
                         if (used >> q & 1u) {
-                            wait_phase(bar(S_FREE + q), sn >> q & 1u, a.err, dead);
+                            pr_wait(bar(S_FREE + q), sn >> q & 1u, a.err, dead);
                             sn ^= 1u << q;
                         }
                         used |= 1u << q;
@@ -648,15 +656,17 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                         for (int q = 0; q < nqt; ++q) next_s(q, cnt + 1);
                         k_used();
                     }
-                    wait_phase(bar(FULL_V + st), (uint32_t)(cnt / kPrStages) & 1u, a.err, dead);
+                    pr_wait(bar(FULL_V + st), (uint32_t)(cnt / kPrStages) & 1u, a.err, dead);
                     for (int q = 0; q < nqt; ++q) {
-                        wait_phase(bar(P_FULL + 2 * q), pn >> q & 1u, a.err, dead);
+                        pr_wait(bar(P_FULL + 2 * q), pn >> q & 1u, a.err, dead);
                         tc_fence_after();
                         issue_pv(q, cnt, 0, t > 0);
-                        wait_phase(bar(P_FULL + 2 * q + 1), pn >> q & 1u, a.err, dead);
+                        if (kPrFirst<D> < kPrKeys) {
+                            pr_wait(bar(P_FULL + 2 * q + 1), pn >> q & 1u, a.err, dead);
+                            tc_fence_after();
+                            issue_pv(q, cnt, 1, true);
+                        }
                         pn ^= 1u << q;
-                        tc_fence_after();
-                        issue_pv(q, cnt, 1, true);
                         if (SEP || !next) umma_commit(bar(O_DONE + q), el);
                         if (q == nqt - 1) umma_commit(bar(EMPTY_V + st), el);
                         if (!SEP && next) {
@@ -669,7 +679,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             }
             // every MMA has completed before TMEM is released
             umma_commit(bar(FIN), el);
-            wait_phase(bar(FIN), 0u, a.err, dead);
+            pr_wait(bar(FIN), 0u, a.err, dead);
         }
     } else {
         // ---- softmax: thread r of Q tile qa owns its row r ----
@@ -685,7 +695,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             // read where needed: its fields and a row's scores together are more
             // than the registers
             const PrItem &w = items[k % kPrSlots];
-            wait_phase(bar(ITEM_FULL + k % kPrSlots), (uint32_t)(k / kPrSlots) & 1u, a.err, dead);
+            pr_wait(bar(ITEM_FULL + k % kPrSlots), (uint32_t)(k / kPrSlots) & 1u, a.err, dead);
             if (w.s < 0) break;
             auto give_back = [&]() {  // the item and its notes
                 __syncwarp();
@@ -695,7 +705,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 }
             };
             if (qa * TQ >= w.ntok) {  // no tokens in this Q tile
-                wait_phase(bar(NOTED + (k & 1)), (uint32_t)(k >> 1) & 1u, a.err, dead);
+                pr_wait(bar(NOTED + (k & 1)), (uint32_t)(k >> 1) & 1u, a.err, dead);
                 give_back();
                 continue;
             }
@@ -712,47 +722,42 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             };
             tile_of(0);
             for (int t = 0; t < w.nt; ++t, ++pn) {
-                wait_phase(bar(S_FULL + qa), (uint32_t)pn & 1u, a.err, dead);
+                pr_wait(bar(S_FULL + qa), (uint32_t)pn & 1u, a.err, dead);
                 __syncwarp();
                 tc_fence_after();
                 uint32_t v[4][32];  // the row's scores
                 tmem_ld32(ts, v[0]);
                 tmem_ld32(ts + 32, v[1]);
-                tmem_wait_ld();
                 tmem_ld32(ts + 64, v[2]);
                 tmem_ld32(ts + 96, v[3]);
-                if (mk) {
-                    const int wl = a.window > 0 ? hi - a.window : -1;
-                    if (a.sign != 1.f) pr_times(v[0], a.sign), pr_times(v[1], a.sign);
-                    pr_mask(v[0], hi, wl, sk);
-                    pr_mask(v[1], hi - 32, wl - 32, sk - 32);
-                    tmem_wait_ld();
-                    if (a.sign != 1.f) pr_times(v[2], a.sign), pr_times(v[3], a.sign);
-                    pr_mask(v[2], hi - 64, wl - 64, sk - 64);
-                    pr_mask(v[3], hi - 96, wl - 96, sk - 96);
-                }
-                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                pr_max(v[0], mx);
-                pr_max(v[1], mx);
                 tmem_wait_ld();
                 if (SEP) {
                     tc_fence_before();
                     mbar_arrive(bar(S_FREE + qa));
-                    if (t > 0) {  // the tile before: its P read, its O there
-                        wait_phase(bar(O_DONE + qa), (uint32_t)on++ & 1u, a.err, dead);
-                        __syncwarp();
-                        tc_fence_after();
+                }
+                if (__builtin_expect(mk, 0)) {
+                    const int wl = a.window > 0 ? hi - a.window : -1;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        if (a.sign != 1.f) pr_times(v[c], a.sign);
+                        pr_mask(v[c], hi - 32 * c, wl - 32 * c, sk - 32 * c);
                     }
                 }
-                pr_max(v[2], mx);
-                pr_max(v[3], mx);
+                float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) pr_max(v[c], mx);
+                if (SEP && t > 0) {  // the tile before: its P read, its O there
+                    pr_wait(bar(O_DONE + qa), (uint32_t)on++ & 1u, a.err, dead);
+                    __syncwarp();
+                    tc_fence_after();
+                }
                 const float cmax = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
                 // The reference m_run moves only when a tile exceeds it by 2^8 (o and l
                 // share it, so the ratio is exact).  A warp's lanes read and write
                 // TMEM together: all rows of a warp are scaled when one of them asks
                 // for it, the others by 1
                 const bool rise = cmax > m_run + 8.f;
-                if (__any_sync(0xffffffffu, rise)) {
+                if (__builtin_expect(__any_sync(0xffffffffu, rise), 0)) {
                     const float al = rise ? fast_exp2(m_run - cmax) : 1.f;  // 0 when nothing came before
                     l_run *= al;
                     if (t >= 1) {
@@ -777,15 +782,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 tmem_st16(tp, pw[0]);
                 pr_weights(v[1], pw[1], r2, scale, m_run, false);
                 tmem_st16(tp + 16, pw[1]);
-                if (kPrFirst == 64) {
-                    tmem_wait_st();
-                    tc_fence_before();
-                    mbar_arrive(bar(P_FULL + 2 * qa));
-                }
                 tile_of(t + 1);  // (the loads it needs, before they are waited for)
                 pr_weights(v[2], pw[0], r2, scale, m_run, false);
                 tmem_st16(tp + 32, pw[0]);
-                if (kPrFirst == 96) {
+                if (kPrFirst<D> == 96) {
                     tmem_wait_st();
                     tc_fence_before();
                     mbar_arrive(bar(P_FULL + 2 * qa));
@@ -794,13 +794,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 tmem_st16(tp + 48, pw[1]);
                 tmem_wait_st();
                 tc_fence_before();
-                mbar_arrive(bar(P_FULL + 2 * qa + 1));
+                mbar_arrive(bar(P_FULL + 2 * qa + (kPrFirst<D> == 96 ? 1 : 0)));
                 const float2 r1 = __fadd2_rn(__fadd2_rn(r2[0], r2[1]), __fadd2_rn(r2[2], r2[3]));
                 l_run += r1.x + r1.y;
             }
             // ---- the rows' outputs, or this split's records (rolled: it runs once an item) ----
-            if (w.nt > 0) wait_phase(bar(O_DONE + qa), (uint32_t)on++ & 1u, a.err, dead);
-            wait_phase(bar(NOTED + (k & 1)), (uint32_t)(k >> 1) & 1u, a.err, dead);
+            if (w.nt > 0) pr_wait(bar(O_DONE + qa), (uint32_t)on++ & 1u, a.err, dead);
+            pr_wait(bar(NOTED + (k & 1)), (uint32_t)(k >> 1) & 1u, a.err, dead);
             __syncwarp();
             tc_fence_after();
             const bool row_ok = r < TQ * G && itok < w.ntok;

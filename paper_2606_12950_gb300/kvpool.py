@@ -270,6 +270,10 @@ def _i32(a) -> np.ndarray:
     return np.ascontiguousarray(a, dtype=np.int32)
 
 
+def _data(a: np.ndarray) -> int:
+    return a.__array_interface__["data"][0]  # 0.2 us; a.ctypes.data 0.7
+
+
 def kv_version() -> str:
     return lib().kv_version().decode()
 
@@ -357,8 +361,8 @@ def kv_copy_blocks(pool, layout: int, src, dst, tokens=None, stream=None) -> Non
     if src.ndim != 1 or src.shape != dst.shape or (tokens is not None and tokens.shape != src.shape):
         raise ValueError("src, dst and tokens must be 1-D and of one length")
     _check("kv_copy_blocks",
-           lib().kv_copy_blocks(pool, layout, int(src.size), src.ctypes.data, dst.ctypes.data,
-                                None if tokens is None else tokens.ctypes.data, _stream(stream)))
+           lib().kv_copy_blocks(pool, layout, src.size, _data(src), _data(dst), None if tokens is None else _data(tokens),
+                                _stream(stream)))
 
 
 def kv_budget_create(limit_bytes: int):
