@@ -46,6 +46,8 @@ int prompt_shape(const kv_pool *p, int layout, int S, int Hq, int T, int max_q, 
     if (rc) return rc;
     if (T < 0 || max_q < 0 || max_q > T || window < 0 || sinks < 0) return KV_ERR_INVALID_ARG;
     if (T > 0 && (S == 0 || max_q == 0)) return KV_ERR_INVALID_ARG;
+    // (positions of whole key tiles and boxes past the last token stay in 32 bits)
+    if ((int64_t)max_blocks * p->desc.block_size > INT32_MAX - 4 * kvp::kPrKeys) return KV_ERR_INVALID_ARG;
     const kv_layout &L = p->desc.layouts[layout];
     s->D = L.head_dim;
     s->Hkv = L.num_kv_heads;

@@ -211,20 +211,27 @@ __device__ __forceinline__ PrOrder pr_order(const PromptArgs &a, int TT, int lan
         o.ctx = max(0, min(o.n, a.max_blocks * a.bs) - o.nq);
     }
     o.reach = (int32_t)__reduce_max_sync(0xffffffffu, (unsigned)(o.ctx + o.nq)) / PrOrder::kUnits;
-    if (a.window > 0) o.reach = min(o.reach, (a.window + TT) / PrOrder::kUnits);
+    if (a.window > 0) o.reach = min(o.reach, a.window / PrOrder::kUnits + TT / PrOrder::kUnits);
     return o;
 }
 
+// Where the last item was found, of more sequences than PrOrder takes: items
+// are asked for in ascending order, so that the search goes on from there.
+struct PrCursor {
+    int32_t s0 = 0, before = 0;  // sequences [s0, s0 + 32), row tiles of those before
+};
+
 // Item i (a converged warp); ntok = 0 where there is none.  `order`: the row
-// tiles by their key ranges, or null: in sequence order, the last first.
-__device__ __forceinline__ PrItem pr_item(const PromptArgs &a, int i, int TT, int lane, const PrOrder *order)
+// tiles by their key ranges, or null: in sequence order.
+__device__ __forceinline__ PrItem pr_item(const PromptArgs &a, int i, int TT, int lane, const PrOrder *order,
+                                          PrCursor &cur)
 {
     PrItem w{};
     w.ks = i % a.KS;
     i /= a.KS;
     w.g = i % a.Hkv;
     const int rank = i / a.Hkv;
-    int tile = a.tiles - 1 - rank, st = 0, nq = 0;
+    int tile = rank, st = 0, nq = 0;
     int32_t n = 0;
     if (order) {
         const int l = order->find(rank, TT, lane, tile);
@@ -235,8 +242,8 @@ __device__ __forceinline__ PrItem pr_item(const PromptArgs &a, int i, int TT, in
         n = __shfl_sync(0xffffffffu, order->n, l);
     } else {
         int l = -1;
-        for (int s0 = 0, before = 0; s0 < a.S; s0 += 32) {  // before: row tiles of the sequences before
-            const int s = s0 + lane;
+        for (; cur.s0 < a.S; cur.s0 += 32) {
+            const int s = cur.s0 + lane;
             int first = 0, cnt = 0;
             if (s < a.S) {
                 first = a.starts[s];
@@ -249,16 +256,16 @@ __device__ __forceinline__ PrItem pr_item(const PromptArgs &a, int i, int TT, in
                 const int v = __shfl_up_sync(0xffffffffu, incl, off);
                 if (lane >= off) incl += v;
             }
-            const unsigned hit = __ballot_sync(0xffffffffu, before + incl > tile);
+            const unsigned hit = __ballot_sync(0xffffffffu, cur.before + incl > tile);
             if (hit) {
                 l = __ffs((int)hit) - 1;
-                tile -= before + __shfl_sync(0xffffffffu, incl - nt, l);
+                tile -= cur.before + __shfl_sync(0xffffffffu, incl - nt, l);
                 st = __shfl_sync(0xffffffffu, first, l);
                 nq = __shfl_sync(0xffffffffu, cnt, l);
-                w.s = s0 + l;
+                w.s = cur.s0 + l;
                 break;
             }
-            before += __shfl_sync(0xffffffffu, incl, 31);
+            cur.before += __shfl_sync(0xffffffffu, incl, 31);
         }
         if (l < 0) return w;
         n = a.ctx_lens[w.s];
@@ -418,6 +425,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             // (with an item a CTA the order is worth nothing)
             const bool sorted = a.S <= 32 && a.n_items > (int)gridDim.x;
             PrOrder order{};
+            PrCursor cursor;
             if (sorted) order = pr_order(a, TT, lane);
             auto look_up = [&]() {   // the next item that has tokens, or the end
                 PrItem w{};
@@ -427,7 +435,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                     const int64_t i = (int64_t)turn * P + (turn & 1 ? P - 1 - b : b);
                     ++turn;
                     if (i >= a.n_items) continue;
-                    w = pr_item(a, (int)i, TT, lane, sorted ? &order : nullptr);
+                    w = pr_item(a, (int)i, TT, lane, sorted ? &order : nullptr, cursor);
                     if (w.ntok > 0) break;
                     w.s = -1;
                 }

@@ -256,7 +256,7 @@ int kv_append_rotary(kv_pool *p, int layout, const kv_rotary *rot, const uint16_
                      int max_blocks, int S, int Hq, void *stream)
 {
     if (!p || !rot || layout < 0 || layout >= p->desc.num_layouts) return KV_ERR_INVALID_ARG;
-    if (S < 0 || T < 0 || max_blocks < 1 || Hq < 0) return KV_ERR_INVALID_ARG;
+    if (S < 0 || T < 0 || max_blocks < 1 || Hq < 0 || Hq > 65536) return KV_ERR_INVALID_ARG;
     if (!dev_q_starts && T != S) return KV_ERR_INVALID_ARG;
     if (T > 0 && S == 0) return KV_ERR_INVALID_ARG;
     const kv_layout &L = p->desc.layouts[layout];

@@ -1,0 +1,124 @@
+"""One attention layer of a server whose chats outgrow their window: rotary
+positions, a sliding window with sinks, forks, and a page cache that gives back
+what the window has left behind.
+
+PyTorch supplies device memory and the stream; every step of the path runs in
+libkvpool's kernels: the rotary append, prompt and decode attention over the
+window, the copies of forked and moved pages.
+"""
+from __future__ import annotations
+
+import numpy as np
+import torch
+
+from . import kvpool as K
+from .runner import DevicePool
+
+
+class WindowedLayer:
+    """Slots of one layer over a pool of pages.
+
+    n_pages blocks of bs tokens; Hq query and Hkv KV heads of d columns;
+    max_seqs slots of at most max_tokens tokens; a query sees the last `window`
+    tokens and the first `sinks` (window 0: all).  freqs: the rotated pairs'
+    frequencies (kvpool.kv_rotary_freqs), radians a position.  pool: a pool of
+    the caller's with this layout as its first (e.g. runner.VmmPool, which gives
+    physical memory back) in place of one of n_pages.
+    """
+
+    def __init__(self, n_pages: int, Hq: int, Hkv: int, d: int, bs: int, max_seqs: int, max_tokens: int, window: int,
+                 sinks: int, freqs, interleaved: bool = False, magnitude: float = 1.0, scale: float | None = None, pool=None):
+        self.Hq, self.Hkv, self.d, self.bs, self.S = Hq, Hkv, d, bs, max_seqs
+        self.window, self.sinks = window, sinks
+        self.scale = d ** -0.5 if scale is None else scale
+        self.own = pool is None
+        self.pool = DevicePool(n_pages, 2 * Hkv * bs * d * 2, bs, [(Hkv, d)]) if pool is None else pool
+        dev = self.pool.device
+        self.tab = K.SeqTab(self.pool.handle, 0, max_seqs, -(-max_tokens // bs))
+        self.table = torch.empty((max_seqs, self.tab.max_blocks), dtype=torch.int32, device=dev)
+        self.lens = torch.empty(max_seqs, dtype=torch.int32, device=dev)
+        steps = torch.from_numpy(K.kv_rotary_steps(freqs).view(np.int64)).to(dev)
+        self.rotary = K.Rotary(2 * len(freqs), steps, interleaved=interleaved, magnitude=magnitude)
+        n = K.kv_workspace_bytes(self.pool.handle, 0, max_seqs, Hq, self.tab.max_blocks)
+        self.ws = torch.empty(max(256, n), dtype=torch.uint8, device=dev)
+
+    def _workspace(self, n: int) -> torch.Tensor:
+        if n > self.ws.numel():
+            self.ws = torch.empty(n, dtype=torch.uint8, device=self.ws.device)
+        return self.ws
+
+    def _append(self, q, k, v, starts, T, stream):
+        """q rotated into a new tensor; k rotated, k and v written to the pages."""
+        q_out = torch.empty((T, self.Hq, self.d), dtype=torch.bfloat16, device=q.device)
+        K.kv_append_rotary(self.pool.handle, 0, self.rotary, q, q.stride(0), q_out, k, k.stride(0), v, v.stride(0),
+                           None, starts, T, self.table, self.lens, self.tab.max_blocks, self.S, self.Hq, stream)
+        return q_out
+
+    def prompt(self, counts, q, k, v, stream=None) -> torch.Tensor:
+        """Append counts[s] new tokens to each slot s and attend: q, k, v hold
+        their rows, slot after slot ([T, heads * d] bf16, any row stride).
+        Returns [T, Hq, d].  KVError (KV_ERR_OUT_OF_BLOCKS) where the pool cannot
+        hold a slot's tokens; slots before it keep their reservation."""
+        counts = np.asarray(counts, dtype=np.int64)
+        lens, T = self.tab.lens(), int(counts.sum())
+        if counts.shape != (self.S,) or counts.min() < 0 or q.shape[0] != T:
+            raise ValueError("counts must have a number for each slot, and q a row for each new token")
+        for s in np.nonzero(counts)[0]:
+            self.tab.reserve(int(s), int(lens[s] + counts[s]))
+        for s in np.nonzero(counts)[0]:
+            self.tab.set_len(int(s), int(lens[s] + counts[s]))
+        out = torch.empty((T, self.Hq, self.d), dtype=torch.bfloat16, device=q.device)
+        if T == 0:
+            return out
+        starts = torch.from_numpy(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)).to(q.device)
+        self.tab.sync(self.table, self.lens, stream)
+        x = self._append(q, k, v, starts, T, stream)
+        n = K.kv_prompt_workspace_bytes(self.pool.handle, 0, self.S, self.Hq, T, int(counts.max()),
+                                        self.tab.max_blocks, self.window, self.sinks)
+        K.paged_prompt_attn(self.pool.handle, 0, x, out, starts, T, int(counts.max()), self.table, self.lens,
+                            self.tab.max_blocks, self.S, self.Hq, self.scale, self.window, self.sinks,
+                            self._workspace(n), n, stream)
+        self._evict(np.nonzero(counts)[0])
+        return out
+
+    def step(self, q, k, v, stream=None) -> torch.Tensor:
+        """One decode step: a new token for every slot that holds a context (rows
+        of the others are passed over).  q, k, v: a row per slot.  Returns
+        [max_seqs, Hq, d], zeros for empty slots."""
+        self.tab.advance()
+        self.tab.sync(self.table, self.lens, stream)
+        x = self._append(q, k, v, None, self.S, stream)
+        out = torch.empty_like(x)
+        K.paged_decode_attn_window(self.pool.handle, 0, x, None, None, out, self.table, self.lens, self.tab.max_blocks,
+                                   self.S, self.Hq, self.scale, self.window, self.sinks, 0, self.ws, self.ws.numel(),
+                                   stream)
+        self._evict(np.nonzero(self.tab.lens())[0])
+        return out
+
+    def _evict(self, slots) -> None:
+        if self.window:
+            for s in slots:
+                self.tab.evict(int(s), self.window, self.sinks)
+
+    def fork(self, src: int, dsts, stream=None) -> None:
+        self.tab.fork(src, dsts, stream)
+
+    def release(self, s: int) -> None:
+        self.tab.release(s)
+
+    def compact(self, stream=None) -> int:
+        """Pages moved together and whole free chunks given back; returns the
+        number of pages moved.  (The next prompt or step sends the changed
+        entries.)"""
+        moved = K.kv_pool_compact(self.pool.handle, stream=stream)
+        K.kv_pool_trim(self.pool.handle)
+        return moved
+
+    def pages_used(self) -> int:
+        return K.kv_pool_stats(self.pool.handle)["blocks_used"][0]
+
+    def close(self) -> None:
+        torch.cuda.synchronize()
+        self.tab.close()
+        if self.own:
+            self.pool.close()
