@@ -54,6 +54,13 @@
 //   column slices: 2.3).  8 sequences of 601-3500 tokens (40 q / 8 KV heads,
 //   67 MB, 4.5 units a warp): 20.3 us, 21.1 with the line at 4 units.
 //
+// WIN: a sliding window with sinks.  A run's units are the sinks' tiles, then
+// those from the window's first token on; rows between the two in a unit get no
+// weight and their V is cleared.  Everything else is shared, so a windowed call
+// streams as the others do: 64 sequences, window 1024 (245 MB) 44.7 us, 250 with
+// window 2048 (789 MB) 123.5 (6.4 TB/s), one of 50001 tokens, window 4096, 11.0
+// (bound by latency: two launches).
+//
 // Grid-to-grid order: the kernel is launched as a programmatic dependent.
 // Alone it releases the next grid and waits for the one before; as part of
 // a chain (beside the shared-prefix kernel, or the later batches of several

