@@ -394,14 +394,12 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
     const int G = a.G, Hq = a.Hkv * G, TQ = kPrRows / G, TT = kPrTiles * TQ;
     constexpr int K_WARP = kPrSoft / 32, V_WARP = K_WARP + 1, MMA_WARP = K_WARP + 2, PLAN_WARP = K_WARP + 3;
 
-    if (tid == 0) {
-        for (int i = 0; i < L::NBARS; ++i) {
-            int n = 1;
-            if ((i >= P_FULL && i < O_DONE) || (i >= S_FREE && i < ITEM_FULL)) n = 128;
-            if (i >= NOTE_FREE && i < S_FREE) n = kPrSoft / 32;
-            if (i >= ITEM_EMPTY && i < FIN) n = kPrSoft / 32 + 3;
-            mbar_init(bar(i), n);
-        }
+    if (tid < L::NBARS) {
+        int n = 1;
+        if ((tid >= P_FULL && tid < O_DONE) || (tid >= S_FREE && tid < ITEM_FULL)) n = 128;
+        if (tid >= NOTE_FREE && tid < S_FREE) n = kPrSoft / 32;
+        if (tid >= ITEM_EMPTY && tid < FIN) n = kPrSoft / 32 + 3;
+        mbar_init(bar(tid), n);
         fence_mbar_init();
     }
     if (warp == 0) {
