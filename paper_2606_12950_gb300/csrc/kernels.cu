@@ -410,15 +410,17 @@ int kvp_attn_shape(const kv_pool *p, int layout, int S, int Hq, int max_blocks, 
 }
 int kvp_ensure_tmap(kv_pool *p, int layout) { return ensure_tmap(p, layout); }
 
-int kvp_tmap_3d(CUtensorMap *map, const void *base, int64_t d0, int64_t d1, int64_t d2, int b0, int b1, int b2)
+int kvp_tmap_3d(CUtensorMap *map, const void *base, int elem, int64_t d0, int64_t d1, int64_t d2, int b0, int b1,
+                int b2)
 {
     auto enc = encode_fn();
     if (!enc) return KV_ERR_CUDA;
     cuuint64_t dims[3] = {(cuuint64_t)d0, (cuuint64_t)d1, (cuuint64_t)d2};
-    cuuint64_t strides[2] = {(cuuint64_t)d0 * 2, (cuuint64_t)(d0 * d1 * 2)};
+    cuuint64_t strides[2] = {(cuuint64_t)(d0 * elem), (cuuint64_t)(d0 * d1 * elem)};
     cuuint32_t box[3] = {(cuuint32_t)b0, (cuuint32_t)b1, (cuuint32_t)b2}, estr[3] = {1, 1, 1};
-    const CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
-                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+    const CUresult r = enc(map, elem == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+                           const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? KV_OK : KV_ERR_CUDA;
 }

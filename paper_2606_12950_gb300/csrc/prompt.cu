@@ -22,7 +22,10 @@ int64_t row_tiles(int S, int T, int max_q, int TT)
 }
 
 // Key splits: CTAs for every SM where the rows are few, each with at least
-// kLeastTiles key tiles.
+// kLeastTiles key tiles.  us with 1, 2, 4, 8 and up to 16 splits (32 q / 8 KV
+// heads of 128): 16 tokens on a context of 16000 158, 87, 51, 32, 26; 64 on 8000
+// 86, 52, 34, 25, 26; 256 on 8000 (4 by this rule) 90, 56, 38; 64 on 2000 (4) 30,
+// 24, 20; 4 x 100, window 1024 (2) 28, 25.
 constexpr int kLeastTiles = 4;
 int key_splits(int64_t ctas, int sm_count, int64_t reach, int TT, int window, int sinks)
 {
@@ -56,7 +59,8 @@ int prompt_shape(const kv_pool *p, int layout, int S, int Hq, int T, int max_q, 
     if (p->sm_count <= 0) return KV_ERR_CUDA;
     s->KS = key_splits(s->tiles * s->Hkv, p->sm_count, (int64_t)max_blocks * p->desc.block_size, s->TT, window, sinks);
     if (s->tiles * s->Hkv * s->KS > INT32_MAX) return KV_ERR_INVALID_ARG;
-    s->ws_bytes = s->KS > 1 ? (size_t)s->KS * T * Hq * (s->D + 4) * sizeof(float) : 0;
+    if ((int64_t)s->KS * T > INT32_MAX) return KV_ERR_INVALID_ARG;
+    s->ws_bytes = s->KS > 1 ? (size_t)s->KS * T * Hq * (s->D + 2) * sizeof(float) : 0;
     return KV_OK;
 }
 
@@ -156,11 +160,12 @@ int paged_prompt_attn(kv_pool *p, int layout, const uint16_t *q, uint16_t *out, 
     a.sign = scale > 0.f ? 1.f : scale < 0.f ? -1.f : 0.f;
     a.qk_scale = scale == 0.f ? 1.f : std::fabs(scale) * 1.4426950408889634f;
     const cudaStream_t st = (cudaStream_t)stream;
-    // q and out as [T][Hq][d]: boxes of 64 columns of G heads, a Q tile's tokens
-    // of q, a warp's rows of out
+    // q and out as [T][Hq][d], or the splits' records as [KS T][Hq][d]: boxes of
+    // 128 bytes of G heads, a Q tile's tokens of q, a warp's rows of the other
     CUtensorMap qmap, omap;
-    rc = kvp_tmap_3d(&qmap, q, s.D, Hq, T, 64, s.G, kvp::kPrRows / s.G);
-    if (rc == KV_OK) rc = kvp_tmap_3d(&omap, out, s.D, Hq, T, 64, s.G, 32 / s.G);
+    rc = kvp_tmap_3d(&qmap, q, 2, s.D, Hq, T, 64, s.G, kvp::kPrRows / s.G);
+    if (rc == KV_OK && s.KS == 1) rc = kvp_tmap_3d(&omap, out, 2, s.D, Hq, T, 64, s.G, 32 / s.G);
+    if (rc == KV_OK && s.KS > 1) rc = kvp_tmap_3d(&omap, workspace, 4, s.D, Hq, (int64_t)s.KS * T, 32, s.G, 32 / s.G);
     if (rc) return rc;
     return s.D == 64 ? prompt_run<64>(&p->tmap[layout], qmap, omap, a, p->sm_count, st)
                      : prompt_run<128>(&p->tmap[layout], qmap, omap, a, p->sm_count, st);

@@ -89,7 +89,7 @@ struct PromptArgs {
     const int32_t *table;
     const int32_t *ctx_lens;
     int32_t *err;
-    float *ws;             // KS > 1: records [KS][T][Hq], pr_record<D>() floats each
+    float *ws;             // KS > 1: the splits' o [KS][T][Hq][D], unnormalised, then (m, l) [KS][T][Hq]
     int64_t rows_per_page;
     int64_t pool_pages;
     int32_t pages_per_block;
@@ -102,10 +102,6 @@ struct PromptArgs {
     float sign;            // 1, or what the scores are multiplied by first: -1 or 0 with the scale's sign
     float qk_scale;        // |scale| * log2(e) (1 where the scale is 0)
 };
-
-// a record: o[D] unnormalised, m, l, padded to 16 bytes
-template <int D>
-__host__ __device__ constexpr uint32_t pr_record() { return D + 4; }
 
 // An item: tokens [row0, row0 + ntok) of q, positions p0 .. p1 of sequence s,
 // KV head g, and its key tiles.
@@ -858,17 +854,17 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
             const bool blind = p < 0;  // the row sees nothing: zeros
             const float inv = blind || nt == 0 ? 0.f : 1.f / l_run;
             const bool rec = a.KS > 1;
-            float *recp = a.ws + (((int64_t)w.ks * a.T + w.row0 + itok) * Hq + w.g * G + hrow) * pr_record<D>();
+            const int64_t rec_row = ((int64_t)w.ks * a.T + w.row0 + itok) * Hq + w.g * G + hrow;
             const unsigned long long orow =
                 !row_ok || dead ? 0ull
-                                : rec ? reinterpret_cast<unsigned long long>(recp)
+                                : rec ? reinterpret_cast<unsigned long long>(a.ws + rec_row * D)
                                       : reinterpret_cast<unsigned long long>(a.out + qrow_off);
-            const int g_out = w.g * G, tok_out = w.row0 + itok;  // (of lane 0: the box's corner)
+            const int g_out = w.g * G, tok_out = w.row0 + itok + (rec ? w.ks * a.T : 0);  // (of lane 0: the box's corner)
             give_back();
             // 128 bytes of each row through shared memory.  A warp whose 32 rows are
             // whole tokens of the chunk sends them as one TMA box; otherwise eight
             // lanes write 128 consecutive bytes.
-            const bool box = !rec && 32 % G == 0 && __all_sync(0xffffffffu, orow != 0ull);
+            const bool box = 32 % G == 0 && __all_sync(0xffffffffu, orow != 0ull);
             auto send = [&](int part, const uint4 (&x)[8]) {
                 if (lane == 0) bulk_wait_read();  // a box before has been read
                 __syncwarp();
@@ -879,7 +875,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) {
-                        tma_store_3d(&omap, smem_u32(xb), part * 64, g_out, tok_out);
+                        tma_store_3d(&omap, smem_u32(xb), part * (rec ? 32 : 64), g_out, tok_out);
                         bulk_commit();
                     }
                     return;
@@ -910,10 +906,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                     for (int i = 0; i < 8; ++i) x[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                     send(cb, x);
                 }
-                if (orow) {
-                    recp[D] = blind || nt == 0 ? -INFINITY : m_run;
-                    recp[D + 1] = l_run;
-                }
+                if (orow)
+                    reinterpret_cast<float2 *>(a.ws + (int64_t)a.KS * a.T * Hq * D)[rec_row] =
+                        make_float2(blind || nt == 0 ? -INFINITY : m_run, l_run);
             } else {
 #pragma unroll 1
                 for (int cb = 0; cb < D / 64; ++cb) {
@@ -948,36 +943,60 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
 }
 
 // Merge of the KS records of each (row, query head): a warp each, D / 32
-// columns a lane.  A row without records (no split saw anything) is zero.
+// columns a lane.  The records' maxima and sums first, a record a lane, then
+// their outputs with the weights known, so that no load waits for another (16
+// records one after another: 20 us for 512 rows).  A row without records (no
+// split saw anything) is zero.
 template <int D>
 __global__ void __launch_bounds__(256) prompt_merge_kernel(const float *ws, uint16_t *out, int64_t n_rows, int KS)
 {
     grid_dependency_wait();
     grid_launch_dependents();
     constexpr int C = D / 32;
+    static_assert(kPrMaxSplits <= 32, "a record a lane");
     const int64_t i = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
     const int lane = threadIdx.x & 31;
     if (i >= n_rows) return;
-    float M = -INFINITY, L = 0.f, O[C];
+    const int64_t next = n_rows * D;
+    const float *rec = ws + i * D;
+    const float2 ml = lane < KS ? reinterpret_cast<const float2 *>(ws + KS * next)[lane * n_rows + i]
+                                : make_float2(-INFINITY, 0.f);
+    const float m = ml.x, l = ml.y;
+    float M = m;
 #pragma unroll
-    for (int c = 0; c < C; ++c) O[c] = 0.f;
+    for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+    const float wgt = m == -INFINITY ? 0.f : fast_exp2(m - M);
+    float L = m == -INFINITY ? 0.f : wgt * l;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) L += __shfl_xor_sync(0xffffffffu, L, off);
+    const unsigned there = __ballot_sync(0xffffffffu, m != -INFINITY);
+    float O[C] = {};
+#pragma unroll 8
     for (int k = 0; k < KS; ++k) {
-        const float *rec = ws + ((int64_t)k * n_rows + i) * pr_record<D>();
-        const float m = rec[D], l = rec[D + 1];
-        if (m == -INFINITY) continue;
-        const float Mn = fmaxf(M, m), sa = fast_exp2(M - Mn), sb = fast_exp2(m - Mn);
-        L = fmaf(L, sa, l * sb);
-#pragma unroll
-        for (int c = 0; c < C; ++c) O[c] = fmaf(O[c], sa, rec[lane * C + c] * sb);
-        M = Mn;
+        const float w = __shfl_sync(0xffffffffu, wgt, k);
+        if (!(there >> k & 1u)) continue;
+        const float *o = rec + k * next + lane * C;
+        if constexpr (C == 4) {
+            const float4 x = *reinterpret_cast<const float4 *>(o);
+            O[0] = fmaf(x.x, w, O[0]);
+            O[1] = fmaf(x.y, w, O[1]);
+            O[2] = fmaf(x.z, w, O[2]);
+            O[3] = fmaf(x.w, w, O[3]);
+        } else {
+            const float2 x = *reinterpret_cast<const float2 *>(o);
+            O[0] = fmaf(x.x, w, O[0]);
+            O[1] = fmaf(x.y, w, O[1]);
+        }
     }
-    const float inv = M == -INFINITY ? 0.f : 1.f / L;
+    const float inv = there ? 1.f / L : 0.f;
     uint32_t y[C / 2];
 #pragma unroll
     for (int c = 0; c < C / 2; ++c) y[c] = pr_pack(O[2 * c] * inv, O[2 * c + 1] * inv);
     uint32_t *dst = reinterpret_cast<uint32_t *>(out + i * D + lane * C);
-#pragma unroll
-    for (int c = 0; c < C / 2; ++c) dst[c] = y[c];
+    if constexpr (C == 4)
+        *reinterpret_cast<uint2 *>(dst) = make_uint2(y[0], y[1]);
+    else
+        *dst = y[0];
 }
 
 template <int D>
