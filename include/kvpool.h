@@ -346,7 +346,8 @@ int kv_seq_trim(kv_seqtab *t, int s);
  * entries; the whole-context calls (paged_decode_attn and its forms) must not
  * be given the slot any more, and kv_seq_share_prefix over such an entry is
  * KV_ERR_INVALID_ARG.  *n_freed (may be null) receives the number of blocks
- * given up.  window < 1 or sinks < 0 is KV_ERR_INVALID_ARG.
+ * given up.  window < 1 or sinks < 0 is KV_ERR_INVALID_ARG; no host memory for
+ * the change list KV_ERR_OUT_OF_BLOCKS (nothing changed).
  */
 int kv_seq_evict(kv_seqtab *t, int s, int window, int sinks, int32_t *n_freed);
 
@@ -697,8 +698,8 @@ int paged_decode_attn_window(kv_pool *pool, int layout, const uint16_t *q, const
  * over the tokens j <= p with j > p - window or j < sinks (window = 0: all
  * j <= p).  Chunks of one token are fine (a batch may mix decode steps and
  * prompts), empty ones too.
- *   q, out      bf16 [T][Hq][d], 16-byte aligned device arrays, T = starts[S];
- *               max_q: the longest chunk, at least
+ *   q, out      bf16 [T][Hq][d], 16-byte aligned device arrays that do not
+ *               overlap, T = starts[S]; max_q: the longest chunk, at least
  *   dev_q_starts device int32[S + 1]
  *   workspace   kv_prompt_workspace_bytes, 256-byte aligned; not initialised;
  *               0 bytes (NULL) where that says so

@@ -182,7 +182,7 @@ int kv_seq_fork(kv_seqtab *t, int src, int n, const int32_t *dsts, void *stream)
         if (std::adjacent_find(seen.begin(), seen.end()) != seen.end()) return KV_ERR_INVALID_ARG;
         for (int i = 0; i < full; ++i)
             if (row[i] >= 0) shared.push_back(row[i]);
-        t->changed.reserve(t->changed.size() + (size_t)n * (full + 1));
+        kvp_seqtab_make_room(t, (size_t)n * (full + 1));
         int rc = KV_OK;
         if (tail > 0) {
             rc = kv_alloc_blocks(t->pool, t->layout, n, own.data());
@@ -321,7 +321,7 @@ int kv_pool_compact(kv_pool *p, int max_moves, void *stream, int *n_moves)
         for (int l = 0; l < nl; ++l)
             for (size_t i = 0; i < src[l].size(); ++i) to[(size_t)src[l][i]] = dst[l][i];
         // room for every change first, so that nothing below can fail but the copies
-        for (kv_seqtab *t : p->seqtabs) t->changed.reserve(t->table.size());
+        for (kv_seqtab *t : p->seqtabs) kvp_seqtab_make_room(t, t->table.size() - t->changed.size());
         std::vector<int32_t> keep[KV_MAX_LAYOUTS], cut_all;
         for (int l = 0; l < nl; ++l) {
             std::vector<int32_t> taken = dst[l];

@@ -2,6 +2,7 @@
 // them (not part of the ABI).
 #pragma once
 
+#include <cstddef>
 #include <cstdint>
 
 #include "kvpool.h"
@@ -14,3 +15,5 @@ int kvp_copy_pages(const kv_pool *p, int layout, int n, const int32_t *src, cons
 
 // Set entry i of slot s and mark it changed for the next sync (seqtab.cpp).
 void kvp_seqtab_set_entry(kv_seqtab *t, int s, int i, int32_t v);
+// Room for n such changes: set_entry does not throw for them (this may).
+void kvp_seqtab_make_room(kv_seqtab *t, size_t n);

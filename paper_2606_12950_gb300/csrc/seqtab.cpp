@@ -8,6 +8,7 @@
 // end of a stage or sequence (§III-C).
 #include <algorithm>
 #include <cstring>
+#include <new>
 #include <vector>
 
 #include "pages_internal.h"
@@ -29,6 +30,14 @@ void set_entry(kv_seqtab *t, int s, int i, int32_t v)
     }
 }
 
+// Room for n more changes, so that set_entry cannot fail (may throw, nothing
+// changed).
+void make_room(kv_seqtab *t, size_t n)
+{
+    const size_t need = t->changed.size() + n;
+    if (t->changed.capacity() < need) t->changed.reserve(std::max(need, 2 * t->changed.capacity()));
+}
+
 // Give up the blocks of entries [lo, hi) of slot s: one reference each, the
 // entries -1.  Entries that kv_seq_evict has given up already are -1 and
 // passed over.  *n_given (may be null) receives how many were not.
@@ -36,6 +45,7 @@ int give_up(kv_seqtab *t, int s, int lo, int hi, int32_t *n_given)
 {
     const int32_t *row = &t->table[(size_t)s * t->max_blocks];
     int32_t n = 0;
+    make_room(t, (size_t)(hi - lo));
     if (std::find(row + lo, row + hi, -1) == row + hi) {
         int rc = kv_free_blocks(t->pool, t->layout, hi - lo, row + lo);
         if (rc) return rc;
@@ -58,6 +68,7 @@ int give_up(kv_seqtab *t, int s, int lo, int hi, int32_t *n_given)
 }  // namespace
 
 void kvp_seqtab_set_entry(kv_seqtab *t, int s, int i, int32_t v) { set_entry(t, s, i, v); }
+void kvp_seqtab_make_room(kv_seqtab *t, size_t n) { make_room(t, n); }
 
 void kvp_seqtab_detach(kv_seqtab *t) { t->pool = nullptr; }
 
@@ -222,7 +233,11 @@ int kv_seq_evict(kv_seqtab *t, int s, int window, int sinks, int32_t *n_freed)
     const int first = (int)(((int64_t)sinks + t->bs - 1) / t->bs);
     const int last = (int)std::max<int64_t>(0, ((int64_t)t->lens[(size_t)s] - window) / t->bs);
     if (first >= last) return KV_OK;
-    return give_up(t, s, first, last, n_freed);
+    try {
+        return give_up(t, s, first, last, n_freed);
+    } catch (const std::bad_alloc &) {
+        return KV_ERR_OUT_OF_BLOCKS;  // no host memory: nothing changed
+    }
 }
 
 int kv_seq_replace(kv_seqtab *t, int n, const int32_t *slots, const int64_t *reserve_tokens,
