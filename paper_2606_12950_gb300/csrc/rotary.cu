@@ -14,8 +14,8 @@
 // position: two integer multiplies, and sincospif on 31 bits of the result.
 //
 // Bound by HBM for prompts (each row read and written once) and by latency for
-// a decode step.  A CTA takes one token: its cos and sin are computed once,
-// into shared memory, for all heads.
+// a decode step.  A token's cos and sin are computed once, into shared memory,
+// for all heads.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -31,6 +31,7 @@
 namespace {
 
 constexpr int kRotThreads = 256;
+constexpr int kRotShared = 3;     // CTAs an SM holds of those that tokens share
 constexpr int kMaxHeadDim = 512;  // kv_pool_create's limit
 
 struct RotaryArgs {
@@ -49,6 +50,7 @@ struct RotaryArgs {
     int32_t pages_per_block, max_blocks;
     int32_t S, Hq, Hkv, D, bs, rot;
     int32_t items;              // of a row (see rotary_kernel)
+    int32_t run, longer;        // tokens of a group; the first `longer` groups have one more
 };
 
 // largest s with starts[s] <= t (starts ascending, starts[0] <= t): 32 probes a
@@ -104,102 +106,134 @@ __device__ __forceinline__ void turn_adjacent(uint4 &a, const float2 (&c)[4], co
     }
 }
 
-constexpr int kRotBatch = 4;  // rows a thread loads before it needs the token's position
-
-// One CTA per token.  Its Hq + 2 Hkv rows (q, k, v) are cut alike into items: a
-// pair of chunks that turn together (half layout), a chunk that turns (adjacent
-// pairs) or one that passes through; a thread keeps its item and goes from row
-// to row.  The rows' addresses need the token alone, so each thread loads its
-// first kRotBatch rows before the position, the angles and the slot, four
-// dependent loads away, are known.  16000 tokens of 40 q and 8 KV heads, half of
-// each head turned (460 MB): 98.7 us with the loads after the position, 81.0
-// with them before, 73.4 with an item a thread (issue slots had been 79% taken; 6.27 TB/s).
+// A token's threads are a GROUP of a CTA's.  Its Hq + 2 Hkv rows (q, k, v) are
+// cut alike into items: a pair of chunks that turn together (half layout), a
+// chunk that turns (adjacent pairs) or one that passes through; a thread keeps
+// its item and goes from row to row.  The rows' addresses need the token alone,
+// so each thread loads its first kRotBatch rows before the position, the angles
+// and the slot, four dependent loads away, are known.
+//
+// Tokens of many items have a CTA of their own, the whole of it their group:
+// 16000 tokens of 40 q and 8 KV heads, half of each head turned (460 MB): 98.7 us
+// with the loads after the position, 81.0 with them before, 74.8 with an item a
+// thread (issue slots had been 79% taken; 6.15 TB/s).
+//
+// Tokens whose items are fewer than a smaller group's batches, where there are
+// enough of them to fill the GPU, share CTAs that stay: a group takes a run of
+// adjacent tokens, looks its sequence up once, and has the next token's rows on
+// their way after the last's are stored.  Before, a CTA each / now: 32000 tokens
+// of 16 and 4 heads of 128: 184 us / 65.7; of 2 and 1 heads of 64 (21500 tokens):
+// 114 / 13.3; 16000 of 32 and 8 of 128: 110 / 65.8 (5.97 TB/s); 1600 of 16 and 4 of 64: 11.0 / 6.5.
+// Batches and CTAs an SM holds are the most that the registers allow; runs for
+// the large tokens too measured 84 us where a CTA each measured 73.
+//
 // Pointers are not __restrict__: the kernel may be resident while the grid
 // before it still writes what it reads, and a const __restrict__ pointer may be
 // read through the non-coherent path, which the wait below does not order.
-template <bool INTERLEAVED>
-__global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_constant__ RotaryArgs a)
+template <bool INTERLEAVED, int GROUP>
+constexpr int kRotBatch = GROUP == kRotThreads ? 4 : INTERLEAVED ? 6 : 3;
+template <bool INTERLEAVED, int GROUP>
+constexpr int kRotResident = GROUP == kRotThreads && INTERLEAVED ? 5 : kRotShared;
+
+template <bool INTERLEAVED, int GROUP>
+__global__ void __launch_bounds__(kRotThreads, kRotResident<INTERLEAVED, GROUP>) rotary_kernel(const __grid_constant__ RotaryArgs a)
 {
-    __shared__ __align__(16) float cosines[kMaxHeadDim / 2], sines[kMaxHeadDim / 2];  // times the magnitude
-    const int tid = threadIdx.x, lane = tid & 31, t = blockIdx.x;
+    constexpr int PER = kRotThreads / GROUP, BATCH = kRotBatch<INTERLEAVED, GROUP>;
+    // times the magnitude; of a group's token, and of the one before it
+    __shared__ __align__(16) float cosines[2][PER][kMaxHeadDim / 2], sines[2][PER][kMaxHeadDim / 2];
+    const int lane = threadIdx.x & 31, tid = threadIdx.x & (GROUP - 1), sub = threadIdx.x / GROUP;
+    const int group = blockIdx.x * PER + sub;
+    int t = GROUP == kRotThreads ? blockIdx.x : group * a.run + min(group, a.longer);
+    const int t_end = GROUP == kRotThreads ? t + 1 : t + a.run + (group < a.longer);
     const int turned = INTERLEAVED ? a.rot / 8 : a.rot / 16;
     const int items = a.items;  // of a row: those that turn, then the others
-    const int step = kRotThreads / items;  // rows at a time
+    const int step = GROUP / items;  // rows at a time
     const int item = tid % items, r0 = tid / items;
     const bool turns = item < turned, pair = !INTERLEAVED && turns;
     const int at = turns ? item : item + a.rot / 8 - turned;  // the item's (first) chunk
     const int q_rows = a.q ? a.Hq : 0, rows = r0 < step ? q_rows + (a.k ? 2 * a.Hkv : 0) : 0;
-    const uint16_t *qs = a.q + (int64_t)t * a.q_stride + at * 8, *ks = a.k + (int64_t)t * a.k_stride + at * 8,
-                   *vs = a.v + (int64_t)t * a.v_stride + at * 8;
     auto load = [&](int r, uint4 &x, uint4 &y) {
         const int g = r - q_rows;
-        const uint16_t *src = g < 0 ? qs + r * a.D : g < a.Hkv ? ks + g * a.D : vs + (g - a.Hkv) * a.D;
+        const uint16_t *src = g < 0          ? a.q + t * a.q_stride + r * a.D
+                              : g < a.Hkv ? a.k + t * a.k_stride + g * a.D
+                                          : a.v + t * a.v_stride + (g - a.Hkv) * a.D;
+        src += at * 8;
         x = *reinterpret_cast<const uint4 *>(src);
         if (pair) y = *reinterpret_cast<const uint4 *>(src + a.rot / 2);
     };
-    uint4 x[kRotBatch], y[kRotBatch];
+    uint4 x[BATCH], y[BATCH];
     kvp::grid_dependency_wait();
     kvp::grid_launch_dependents();
+    int32_t s = 0, n = 0, end = 0;  // the token's sequence, its context, the token past it
+    for (int buf = 0; t < t_end; ++t, buf ^= 1) {
 #pragma unroll
-    for (int b = 0; b < kRotBatch; ++b)
-        if (r0 + b * step < rows) load(r0 + b * step, x[b], y[b]);
-    const int s = a.starts ? seq_of_token(a.starts, a.S, t, lane) : t;
-    const int32_t n = a.ctx_lens[s];
-    const int32_t end = a.starts ? a.starts[s + 1] : t + 1;  // past the sequence's tokens; t past it: a bad array
-    const int32_t pos = n - (end - t);
-    // the token's slot: a sequence without a context (n <= 0) keeps its pages as
-    // they are, a position outside the table or a page outside the pool is reported
-    uint8_t *slot = nullptr;
-    if (a.k && n > 0) {
-        bool ok = t < end && pos >= 0 && pos < a.max_blocks * a.bs;
-        if (ok) {
-            const int32_t phys = a.table[(int64_t)s * a.max_blocks + pos / a.bs];
-            ok = phys >= 0 && (int64_t)phys + a.pages_per_block <= a.n_pages;
-            if (ok) slot = a.pool + (int64_t)phys * a.page_bytes + (int64_t)(pos % a.bs) * a.D * 2;
+        for (int b = 0; b < BATCH; ++b)
+            if (r0 + b * step < rows) load(r0 + b * step, x[b], y[b]);
+        if (t >= end) {
+            s = a.starts ? seq_of_token(a.starts, a.S, t, lane) : t;
+            n = a.ctx_lens[s];
+            end = a.starts ? a.starts[s + 1] : t + 1;
         }
-        if (!ok && tid == 0) atomicCAS(a.err, 0, KV_ERR_DEVICE_BOUNDS);
-    }
-    {
+        const int32_t pos = n - (end - t);
+        // the token's slot: a sequence without a context (n <= 0) keeps its pages as
+        // they are, a position outside the table or a page outside the pool is reported
+        // (as is t >= end: a bad array)
+        uint8_t *slot = nullptr;
+        if (a.k && n > 0) {
+            bool ok = t < end && pos >= 0 && pos < a.max_blocks * a.bs;
+            if (ok) {
+                const int32_t phys = a.table[(int64_t)s * a.max_blocks + pos / a.bs];
+                ok = phys >= 0 && (int64_t)phys + a.pages_per_block <= a.n_pages;
+                if (ok) slot = a.pool + (int64_t)phys * a.page_bytes + (int64_t)(pos % a.bs) * a.D * 2 + at * 16;
+            }
+            if (!ok && tid == 0) atomicCAS(a.err, 0, KV_ERR_DEVICE_BOUNDS);
+        }
         const int32_t by = a.positions ? a.positions[t] : pos;
-        for (int i = tid; i < a.rot / 2; i += kRotThreads) {
+        for (int i = tid; i < a.rot / 2; i += GROUP) {
             const uint64_t turn = (uint64_t)(int64_t)by * a.steps[i] + (1ull << 31);
             float sn, cn;
             sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &sn, &cn);
-            cosines[i] = cn * a.magnitude;
-            sines[i] = sn * a.magnitude;
+            cosines[buf][sub][i] = cn * a.magnitude;
+            sines[buf][sub][i] = sn * a.magnitude;
         }
-    }
-    __syncthreads();
-    float2 c[4] = {}, sn[4] = {};  // of the item's pairs
-    if (turns) {
+        // (the other buffer was read before this barrier, and is written after it)
+        if (GROUP == 32)
+            __syncwarp();
+        else
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + sub), "n"(GROUP) : "memory");
+        float2 c[4] = {}, sn[4] = {};  // of the item's pairs
+        if (turns) {
 #pragma unroll
-        for (int e = 0; e < (INTERLEAVED ? 2 : 4); ++e) {
-            c[e] = *reinterpret_cast<const float2 *>(cosines + item * (INTERLEAVED ? 4 : 8) + 2 * e);
-            sn[e] = *reinterpret_cast<const float2 *>(sines + item * (INTERLEAVED ? 4 : 8) + 2 * e);
+            for (int e = 0; e < (INTERLEAVED ? 2 : 4); ++e) {
+                c[e] = *reinterpret_cast<const float2 *>(cosines[buf][sub] + item * (INTERLEAVED ? 4 : 8) + 2 * e);
+                sn[e] = *reinterpret_cast<const float2 *>(sines[buf][sub] + item * (INTERLEAVED ? 4 : 8) + 2 * e);
+            }
         }
-    }
-    const int64_t head_bytes = (int64_t)a.bs * a.D * 2;  // of one KV head in a block
-    uint8_t *q_dst = reinterpret_cast<uint8_t *>(a.q_out + (int64_t)t * a.Hq * a.D) + at * 16;
-    if (slot) slot += at * 16;
-    auto finish = [&](int r, uint4 &x0, uint4 &y0) {
-        const int g = r - q_rows;
-        if (g >= 0 && !slot) return;
-        uint8_t *dst = g < 0 ? q_dst + r * a.D * 2 : slot + g * head_bytes;  // v's heads follow k's
-        if (turns && g < a.Hkv) {
-            if constexpr (INTERLEAVED)
-                turn_adjacent(x0, c, sn);
-            else
-                turn_halves(x0, y0, c, sn);
-        }
-        *reinterpret_cast<uint4 *>(dst) = x0;
-        if (pair) *reinterpret_cast<uint4 *>(dst + a.rot) = y0;
-    };
+        const int64_t head_bytes = (int64_t)a.bs * a.D * 2;  // of one KV head in a block
+        uint8_t *q_dst = reinterpret_cast<uint8_t *>(a.q_out + (int64_t)t * a.Hq * a.D) + at * 16;
+        auto finish = [&](int r, uint4 &x0, uint4 &y0) {
+            const int g = r - q_rows;
+            if (g >= 0 && !slot) return;
+            uint8_t *dst = g < 0 ? q_dst + r * a.D * 2 : slot + g * head_bytes;  // v's heads follow k's
+            if (turns && g < a.Hkv) {
+                if constexpr (INTERLEAVED)
+                    turn_adjacent(x0, c, sn);
+                else
+                    turn_halves(x0, y0, c, sn);
+            }
+            *reinterpret_cast<uint4 *>(dst) = x0;
+            if (pair) *reinterpret_cast<uint4 *>(dst + a.rot) = y0;
+        };
+        for (int r = r0;;) {
 #pragma unroll
-    for (int b = 0; b < kRotBatch; ++b)
-        if (r0 + b * step < rows) finish(r0 + b * step, x[b], y[b]);
-    for (int r = r0 + kRotBatch * step; r < rows; r += step) {
-        load(r, x[0], y[0]);
-        finish(r, x[0], y[0]);
+            for (int b = 0; b < BATCH; ++b)
+                if (r + b * step < rows) finish(r + b * step, x[b], y[b]);
+            r += BATCH * step;
+            if (r >= rows) break;
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b)
+                if (r + b * step < rows) load(r + b * step, x[b], y[b]);
+        }
     }
 }
 
@@ -302,16 +336,32 @@ int kv_append_rotary(kv_pool *p, int layout, const kv_rotary *rot, const uint16_
     a.bs = p->desc.block_size;
     a.rot = rot->rot_dim;
     a.items = (rot->interleaved ? a.rot / 8 : a.rot / 16) + (a.D - a.rot) / 8;
+    const int64_t token_items = (int64_t)a.items * ((q ? Hq : 0) + (k ? 2 * Hkv : 0));
+    const int64_t resident = (int64_t)kRotShared * std::max(1, p->sm_count);
+    const int batch = rot->interleaved ? kRotBatch<true, 32> : kRotBatch<false, 32>;
+    int per = 1;  // groups of a CTA (see rotary_kernel)
+    while (kRotThreads / per > 32 && kRotThreads / (2 * per) >= a.items && T >= 2 * per * resident &&
+           token_items <= batch * (kRotThreads / (2 * per)))
+        per *= 2;
+    a.run = (int32_t)(T / (per * resident));
+    a.longer = (int32_t)(T % (per * resident));
+    void (*kernel)(RotaryArgs) = nullptr;
+    switch (kRotThreads / per) {
+    case 256: kernel = rot->interleaved ? rotary_kernel<true, 256> : rotary_kernel<false, 256>; break;
+    case 128: kernel = rot->interleaved ? rotary_kernel<true, 128> : rotary_kernel<false, 128>; break;
+    case 64: kernel = rot->interleaved ? rotary_kernel<true, 64> : rotary_kernel<false, 64>; break;
+    default: kernel = rot->interleaved ? rotary_kernel<true, 32> : rotary_kernel<false, 32>; break;
+    }
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)T);
+    cfg.gridDim = dim3((unsigned)(per == 1 ? T : resident));  // (T >= per * resident)
     cfg.blockDim = dim3(kRotThreads);
     cfg.stream = (cudaStream_t)stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, rot->interleaved ? rotary_kernel<true> : rotary_kernel<false>, a) != cudaSuccess)
+    if (cudaLaunchKernelEx(&cfg, kernel, a) != cudaSuccess)
         return KV_ERR_CUDA;
     kvp_note_stream(stream, false);
     return KV_OK;

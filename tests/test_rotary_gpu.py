@@ -161,3 +161,45 @@ def test_refusals():
         call(rot=24)
     assert e.value.code == K.KV_ERR_UNSUPPORTED
     c.close()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("Hq,Hkv,d,rot", [(2, 1, 64, 64), (16, 4, 64, 32), (8, 2, 128, 128), (1, 1, 128, 48), (5, 1, 256, 0),
+                                          (40, 8, 128, 64)])
+@pytest.mark.parametrize("T", [1000, 2000, 7001])
+def test_runs_of_tokens(T, Hq, Hkv, d, rot, interleaved):
+    """Many tokens: small ones share CTAs, each group of threads takes a run of
+    them, over the ends of sequences and over sequences without new tokens."""
+    rng = np.random.default_rng(T)
+    nq = rng.integers(0, 40, T)
+    nq[5:9] = 0
+    nq = nq[: int(np.searchsorted(np.cumsum(nq), T)) + 1]
+    nq[-1] -= nq.sum() - T
+    c = paged(nq + rng.integers(0, 50, len(nq)), nq, Hq, Hkv, d, 16)
+    assert c.T == T
+    verify(c, rot, K.kv_rotary_freqs(rot) if rot else np.zeros(0), interleaved=interleaved)
+    c.close()
+
+
+def test_runs_of_single_tokens():
+    rng = np.random.default_rng(5)
+    c = paged(rng.integers(1, 60, 4001), [1] * 4001, 4, 2, 64, 16)
+    verify(c, 64, K.kv_rotary_freqs(64), ragged=False, pad=8)
+    verify(c, 64, K.kv_rotary_freqs(64), ragged=False, q=False)
+    verify(c, 64, K.kv_rotary_freqs(64), kv=False, positions=rng.integers(-9, 10 ** 6, 4001))
+    c.close()
+
+
+def test_bounds_within_runs():
+    c = paged([20] * 1000, [4] * 1000, 4, 2, 64, 16)  # the new tokens at 16 .. 19
+    before = c.pool.clone()
+    c.lens[10:20] = 0          # no context: nothing is written
+    c.lens[30:40] = 2          # two of four tokens before position 0
+    c.table[50:60, 1] = -1     # no block
+    c.table[70:80, 1] = 10 ** 6
+    run(c, 64, K.kv_rotary_freqs(64))
+    assert c.error() == K.KV_ERR_DEVICE_BOUNDS
+    changed = (c.pool.view(torch.int16) != before.view(torch.int16)).flatten(1).any(1).nonzero().flatten().tolist()
+    want = {int(c.host_table[s, 1]) for s in range(1000) if not any(a <= s < a + 10 for a in (10, 30, 50, 70))}
+    assert set(changed) == want | {int(c.host_table[s, 0]) for s in range(30, 40)}
+    c.close()
