@@ -318,13 +318,14 @@ __device__ __forceinline__ void pr_wait(uint32_t bar, uint32_t parity, int32_t *
 }
 // bits 0 .. n of a word (none for n < 0, all from 31 on)
 __device__ __forceinline__ uint32_t pr_bits(int n) { return n < 0 ? 0u : 0xffffffffu >> (31 - min(n, 31)); }
-// 32 scores of a row: those of unseen tokens to -inf (column k is seen when
-// k <= hi and not wl >= k >= sk).  The columns' bits first, then a select each:
-// what a masked tile executes is rarely in the instruction caches, and with the
-// comparisons per column it took 16000 clocks, 2500 unmasked.
-__device__ __forceinline__ void pr_mask(uint32_t (&x)[32], int hi, int wl, int sk)
+// The columns that a row sees of 32 (column k is seen when k <= hi and not wl >=
+// k >= sk), and its scores of the others to -inf.
+__device__ __forceinline__ uint32_t pr_seen(int hi, int wl, int sk)
 {
-    const uint32_t seen = pr_bits(hi) & ~(pr_bits(wl) & ~pr_bits(sk - 1));
+    return pr_bits(hi) & ~(pr_bits(wl) & ~pr_bits(sk - 1));
+}
+__device__ __forceinline__ void pr_mask(uint32_t (&x)[32], uint32_t seen)
+{
 #pragma unroll
     for (int k = 0; k < 32; ++k)
         if (!(seen >> k & 1u)) x[k] = 0xff800000u;
@@ -517,21 +518,23 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                         // x * 0 + acc: acc stays 0 while every value is finite
                         __nv_bfloat162 acc[2] = {__floats2bfloat162_rn(0.f, 0.f), __floats2bfloat162_rn(0.f, 0.f)};
                         const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+                        if (__any_sync(0xffffffffu, any)) {
 #pragma unroll
-                        for (int c = 0; c < D / 8; ++c) {
-                            const uint4 x =
-                                *reinterpret_cast<const uint4 *>(vt + r * 128 + (c / 8) * L::KV_HALF + ((c ^ r) & 7) * 16);
-                            acc[0] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.x), zero, acc[0]);
-                            acc[1] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.y), zero, acc[1]);
-                            acc[0] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.z), zero, acc[0]);
-                            acc[1] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.w), zero, acc[1]);
+                            for (int c = 0; c < D / 8; ++c) {
+                                const uint4 x = *reinterpret_cast<const uint4 *>(vt + r * 128 + (c / 8) * L::KV_HALF +
+                                                                                 ((c ^ r) & 7) * 16);
+                                acc[0] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.x), zero, acc[0]);
+                                acc[1] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.y), zero, acc[1]);
+                                acc[0] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.z), zero, acc[0]);
+                                acc[1] = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&x.w), zero, acc[1]);
+                            }
                         }
                         const bool odd = ((*reinterpret_cast<uint32_t *>(&acc[0]) | *reinterpret_cast<uint32_t *>(&acc[1])) &
                                           0x7fff7fffu) != 0;
                         if (!any || odd)
-#pragma unroll 1
-                            for (int c = 0; c < D / 8; ++c)
-                                *reinterpret_cast<uint4 *>(vt + r * 128 + (c / 8) * L::KV_HALF + c % 8 * 16) =
+#pragma unroll
+                            for (int c = 0; c < D / 8; ++c)  // (the order that spreads the lanes over the banks)
+                                *reinterpret_cast<uint4 *>(vt + r * 128 + (c / 8) * L::KV_HALF + ((c ^ r) & 7) * 16) =
                                     make_uint4(0u, 0u, 0u, 0u);
                         __syncwarp();
                         const uint32_t bits = __ballot_sync(0xffffffffu, any && odd);
@@ -738,6 +741,28 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 pr_wait(bar(S_FULL + qa), (uint32_t)pn & 1u, a.err, dead);
                 __syncwarp();
                 tc_fence_after();
+                // A masked tile: its scores masked in TMEM, 32 columns at a time, and
+                // read like any other's.  Rolled, because what runs now and then is
+                // rarely in the instruction caches: with the masks unrolled over the
+                // 128 scores a tile took 700 clocks more, and skipping the weights of
+                // unseen columns in a second copy of that code cost more than it
+                // saved (6 sequences of 64 / 16 heads, window 68: 96 us unrolled, 111
+                // with the copy, 93 so).
+                if (__builtin_expect(mk, 0)) {
+                    const int wl = a.window > 0 ? hi - a.window : -1;
+#pragma unroll 1
+                    for (int c = 0; c < 128; c += 32) {
+                        const uint32_t seen = pr_seen(hi - c, wl - c, sk - c);
+                        if (a.sign == 1.f && __all_sync(0xffffffffu, seen == 0xffffffffu)) continue;
+                        uint32_t x[32];
+                        tmem_ld32(ts + c, x);
+                        tmem_wait_ld();
+                        if (a.sign != 1.f) pr_times(x, a.sign);
+                        pr_mask(x, seen);
+                        tmem_st32(ts + c, x);
+                    }
+                    tmem_wait_st();
+                }
                 uint32_t v[4][32];  // the row's scores
                 tmem_ld32(ts, v[0]);
                 tmem_ld32(ts + 32, v[1]);
@@ -747,14 +772,6 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tmap, const __grid_consta
                 if (SEP) {
                     tc_fence_before();
                     mbar_arrive(bar(S_FREE + qa));
-                }
-                if (__builtin_expect(mk, 0)) {
-                    const int wl = a.window > 0 ? hi - a.window : -1;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        if (a.sign != 1.f) pr_times(v[c], a.sign);
-                        pr_mask(v[c], hi - 32 * c, wl - 32 * c, sk - 32 * c);
-                    }
                 }
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
