@@ -53,16 +53,18 @@ struct RotaryArgs {
     int32_t run, longer;        // tokens of a group; the first `longer` groups have one more
 };
 
-// largest s with starts[s] <= t (starts ascending, starts[0] <= t): 32 probes a
-// round trip; the whole warp, converged
+// largest s with starts[s] <= t (starts ascending, starts[0] <= t): N probes a
+// round trip by the N lanes that share t; the whole warp, converged
+template <int N>
 __device__ __forceinline__ int seq_of_token(const int32_t *starts, int S, int t, int lane)
 {
+    const int own = lane & (N - 1);
     int lo = 0, n = S;  // the answer is in [lo, lo + n)
-    while (n > 1) {
-        const int step = (n + 31) / 32;
-        const int i = lo + lane * step;
-        const unsigned le = __ballot_sync(0xffffffffu, lane * step < n && starts[i] <= t);
-        const int k = 31 - __clz((int)(le | 1u));
+    while (__any_sync(0xffffffffu, n > 1)) {
+        const int step = (n + N - 1) / N;
+        const int i = lo + own * step;
+        const unsigned le = __ballot_sync(0xffffffffu, own * step < n && starts[i] <= t) >> (lane - own);
+        const int k = 31 - __clz((int)((N < 32 ? le & ((1u << (N & 31)) - 1u) : le) | 1u));
         n = min(step, n - k * step);
         lo += k * step;
     }
@@ -119,11 +121,12 @@ __device__ __forceinline__ void turn_adjacent(uint4 &a, const float2 (&c)[4], co
 // thread (issue slots had been 79% taken; 6.15 TB/s).
 //
 // Tokens whose items are fewer than a smaller group's batches, where there are
-// enough of them to fill the GPU, share CTAs that stay: a group takes a run of
-// adjacent tokens, looks its sequence up once, and has the next token's rows on
-// their way after the last's are stored.  Before, a CTA each / now: 32000 tokens
-// of 16 and 4 heads of 128: 184 us / 65.7; of 2 and 1 heads of 64 (21500 tokens):
-// 114 / 13.3; 16000 of 32 and 8 of 128: 110 / 65.8 (5.97 TB/s); 1600 of 16 and 4 of 64: 11.0 / 6.5.
+// enough of them to fill the GPU, share CTAs that stay: a group of 128 to 8
+// threads takes a run of adjacent tokens, looks its sequence up once, and has the
+// next token's rows on their way after the last's are stored.  A CTA each / so:
+// 32000 tokens of 16 and 4 heads of 128 184 us / 65.7; 16000 of 32 and 8 of 128
+// 110 / 65.8 (5.97 TB/s); 1600 of 16 and 4 of 64 11.0 / 6.5; 21500 of 2 and 1
+// heads of 64 114 / 7.8 (13.3 with no groups below a warp).
 // Batches and CTAs an SM holds are the most that the registers allow; runs for
 // the large tokens too measured 84 us where a CTA each measured 73.
 //
@@ -139,19 +142,23 @@ template <bool INTERLEAVED, int GROUP>
 __global__ void __launch_bounds__(kRotThreads, kRotResident<INTERLEAVED, GROUP>) rotary_kernel(const __grid_constant__ RotaryArgs a)
 {
     constexpr int PER = kRotThreads / GROUP, BATCH = kRotBatch<INTERLEAVED, GROUP>;
+    constexpr int PAIRS = GROUP < 32 ? 8 * GROUP : kMaxHeadDim / 2;  // (no more, with an item of a row a thread)
     // times the magnitude; of a group's token, and of the one before it
-    __shared__ __align__(16) float cosines[2][PER][kMaxHeadDim / 2], sines[2][PER][kMaxHeadDim / 2];
+    __shared__ __align__(16) float cosines[2][PER][PAIRS], sines[2][PER][PAIRS];
     const int lane = threadIdx.x & 31, tid = threadIdx.x & (GROUP - 1), sub = threadIdx.x / GROUP;
     const int group = blockIdx.x * PER + sub;
-    int t = GROUP == kRotThreads ? blockIdx.x : group * a.run + min(group, a.longer);
-    const int t_end = GROUP == kRotThreads ? t + 1 : t + a.run + (group < a.longer);
+    const int t0 = GROUP == kRotThreads ? blockIdx.x : group * a.run + min(group, a.longer);
+    const int t_end = GROUP == kRotThreads ? t0 + 1 : t0 + a.run + (group < a.longer);
+    // (a warp's groups take turns together)
+    const int turns_end = GROUP < 32 ? t0 + a.run + (a.longer > 0) : t_end;
     const int turned = INTERLEAVED ? a.rot / 8 : a.rot / 16;
     const int items = a.items;  // of a row: those that turn, then the others
     const int step = GROUP / items;  // rows at a time
     const int item = tid % items, r0 = tid / items;
     const bool turns = item < turned, pair = !INTERLEAVED && turns;
     const int at = turns ? item : item + a.rot / 8 - turned;  // the item's (first) chunk
-    const int q_rows = a.q ? a.Hq : 0, rows = r0 < step ? q_rows + (a.k ? 2 * a.Hkv : 0) : 0;
+    const int q_rows = a.q ? a.Hq : 0, all_rows = r0 < step ? q_rows + (a.k ? 2 * a.Hkv : 0) : 0;
+    int t = t0;
     auto load = [&](int r, uint4 &x, uint4 &y) {
         const int g = r - q_rows;
         const uint16_t *src = g < 0          ? a.q + t * a.q_stride + r * a.D
@@ -165,12 +172,15 @@ __global__ void __launch_bounds__(kRotThreads, kRotResident<INTERLEAVED, GROUP>)
     kvp::grid_dependency_wait();
     kvp::grid_launch_dependents();
     int32_t s = 0, n = 0, end = 0;  // the token's sequence, its context, the token past it
-    for (int buf = 0; t < t_end; ++t, buf ^= 1) {
+    for (int i = t0, buf = 0; i < turns_end; ++i, buf ^= 1) {
+        const bool live = GROUP >= 32 || i < t_end;  // else: the last token once more, without rows
+        t = live ? i : t_end - 1;
+        const int rows = live ? all_rows : 0;
 #pragma unroll
         for (int b = 0; b < BATCH; ++b)
             if (r0 + b * step < rows) load(r0 + b * step, x[b], y[b]);
-        if (t >= end) {
-            s = a.starts ? seq_of_token(a.starts, a.S, t, lane) : t;
+        if (GROUP < 32 ? __any_sync(0xffffffffu, t >= end) : t >= end) {
+            s = a.starts ? seq_of_token<GROUP < 32 ? GROUP : 32>(a.starts, a.S, t, lane) : t;
             n = a.ctx_lens[s];
             end = a.starts ? a.starts[s + 1] : t + 1;
         }
@@ -197,7 +207,7 @@ __global__ void __launch_bounds__(kRotThreads, kRotResident<INTERLEAVED, GROUP>)
             sines[buf][sub][i] = sn * a.magnitude;
         }
         // (the other buffer was read before this barrier, and is written after it)
-        if (GROUP == 32)
+        if (GROUP <= 32)
             __syncwarp();
         else
             asm volatile("bar.sync %0, %1;" ::"r"(1 + sub), "n"(GROUP) : "memory");
@@ -340,7 +350,7 @@ int kv_append_rotary(kv_pool *p, int layout, const kv_rotary *rot, const uint16_
     const int64_t resident = (int64_t)kRotShared * std::max(1, p->sm_count);
     const int batch = rot->interleaved ? kRotBatch<true, 32> : kRotBatch<false, 32>;
     int per = 1;  // groups of a CTA (see rotary_kernel)
-    while (kRotThreads / per > 32 && kRotThreads / (2 * per) >= a.items && T >= 2 * per * resident &&
+    while (kRotThreads / per > 8 && kRotThreads / (2 * per) >= a.items && T >= 2 * per * resident &&
            token_items <= batch * (kRotThreads / (2 * per)))
         per *= 2;
     a.run = (int32_t)(T / (per * resident));
@@ -350,7 +360,9 @@ int kv_append_rotary(kv_pool *p, int layout, const kv_rotary *rot, const uint16_
     case 256: kernel = rot->interleaved ? rotary_kernel<true, 256> : rotary_kernel<false, 256>; break;
     case 128: kernel = rot->interleaved ? rotary_kernel<true, 128> : rotary_kernel<false, 128>; break;
     case 64: kernel = rot->interleaved ? rotary_kernel<true, 64> : rotary_kernel<false, 64>; break;
-    default: kernel = rot->interleaved ? rotary_kernel<true, 32> : rotary_kernel<false, 32>; break;
+    case 32: kernel = rot->interleaved ? rotary_kernel<true, 32> : rotary_kernel<false, 32>; break;
+    case 16: kernel = rot->interleaved ? rotary_kernel<true, 16> : rotary_kernel<false, 16>; break;
+    default: kernel = rot->interleaved ? rotary_kernel<true, 8> : rotary_kernel<false, 8>; break;
     }
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

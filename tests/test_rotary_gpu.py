@@ -203,3 +203,35 @@ def test_bounds_within_runs():
     want = {int(c.host_table[s, 1]) for s in range(1000) if not any(a <= s < a + 10 for a in (10, 30, 50, 70))}
     assert set(changed) == want | {int(c.host_table[s, 0]) for s in range(30, 40)}
     c.close()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("Hq,Hkv,d,rot", [(2, 1, 64, 64), (5, 1, 64, 32), (1, 1, 128, 128), (1, 1, 128, 48), (3, 1, 80, 16)])
+@pytest.mark.parametrize("T", [8000, 15013])
+def test_groups_below_a_warp(T, Hq, Hkv, d, rot, interleaved):
+    """So many small tokens that a warp's threads are two or four tokens'."""
+    rng = np.random.default_rng(T)
+    nq = rng.integers(0, 90, T)
+    nq[3:8] = 0
+    nq = nq[: int(np.searchsorted(np.cumsum(nq), T)) + 1]
+    nq[-1] -= nq.sum() - T
+    c = paged(nq + rng.integers(0, 50, len(nq)), nq, Hq, Hkv, d, 16)
+    assert c.T == T
+    verify(c, rot, K.kv_rotary_freqs(rot), interleaved=interleaved, pad=8)
+    c.close()
+
+
+def test_groups_below_a_warp_single_tokens_and_bounds():
+    rng = np.random.default_rng(6)
+    c = paged(rng.integers(1, 40, 15000), [1] * 15000, 2, 1, 64, 16)
+    verify(c, 64, K.kv_rotary_freqs(64), ragged=False)
+    verify(c, 64, K.kv_rotary_freqs(64), q=False)
+    before = c.pool.clone()
+    c.lens[100:111] = 0       # no context: nothing is written
+    c.table[200:213] = -1     # no block
+    run(c, 64, K.kv_rotary_freqs(64))
+    assert c.error() == K.KV_ERR_DEVICE_BOUNDS
+    changed = (c.pool.view(torch.int16) != before.view(torch.int16)).flatten(1).any(1).nonzero().flatten().tolist()
+    want = {int(c.host_table[s, (c.n[s] - 1) // 16]) for s in range(15000) if not (100 <= s < 111 or 200 <= s < 213)}
+    assert set(changed) == want
+    c.close()
