@@ -699,7 +699,9 @@ int paged_decode_attn_window(kv_pool *pool, int layout, const uint16_t *q, const
  * j <= p).  Chunks of one token are fine (a batch may mix decode steps and
  * prompts), empty ones too.
  *   q, out      bf16 [T][Hq][d], 16-byte aligned device arrays that do not
- *               overlap, T = starts[S]; max_q: the longest chunk, at least
+ *               overlap, T = starts[S]; max_q: the longest chunk, at least (a
+ *               longer one sets the error word, and any rows of out may then
+ *               stay unwritten)
  *   dev_q_starts device int32[S + 1]
  *   workspace   kv_prompt_workspace_bytes, 256-byte aligned; not initialised;
  *               0 bytes (NULL) where that says so

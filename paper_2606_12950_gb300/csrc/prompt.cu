@@ -151,7 +151,7 @@ int paged_prompt_attn(kv_pool *p, int layout, const uint16_t *q, uint16_t *out, 
     a.G = s.G;
     a.bs = p->desc.block_size;
     a.T = T;
-    a.tiles = (int32_t)s.tiles;
+    a.max_q = max_q;
     a.KS = s.KS;
     const int32_t reach = max_blocks * a.bs;
     a.window = window < reach ? window : 0;  // one that no context outgrows is the whole context

@@ -95,7 +95,7 @@ struct PromptArgs {
     int32_t pages_per_block;
     int32_t max_blocks;
     int32_t S, Hkv, G, bs, T;
-    int32_t tiles;         // row tiles, at least those there are
+    int32_t max_q;         // the longest chunk by the caller's word: n_items goes by it
     int32_t n_items;       // tiles * Hkv * KS
     int32_t KS;
     int32_t window, sinks; // window 0: the whole context
@@ -283,6 +283,10 @@ __device__ __forceinline__ PrItem pr_item(const PromptArgs &a, int i, int TT, in
         report(a.err, KV_ERR_DEVICE_BOUNDS);
         return w;
     }
+    // a chunk longer than the caller's bound: the last row tiles, of any sequence,
+    // may have no items.  (Where some have none, a chunk with an item is longer:
+    // were none, n_items would be enough.)
+    if (nq > a.max_q) report(a.err, KV_ERR_DEVICE_BOUNDS);
     w.ntok = min(TT, nq - i0);
     const int32_t cap = a.max_blocks * a.bs;
     if (n < nq || n > cap) {
