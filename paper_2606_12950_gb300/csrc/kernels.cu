@@ -515,7 +515,8 @@ struct CascadePlan {
 int attn_call(kv_pool *p, int layout, const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new,
               uint16_t *out, const int32_t *dev_table, const int32_t *dev_ctx_lens, int max_blocks, int S, int Hq,
               float scale, int num_splits, void *workspace, size_t ws_bytes, void *stream,
-              const CascadePlan *cas = nullptr, const FusedSync *sync = nullptr, int window = 0, int sinks = 0)
+              const CascadePlan *cas = nullptr, const FusedSync *sync = nullptr, int window = 0, int sinks = 0,
+              bool window_call = false)
 {
     int G = 0;
     if (num_splits < 0 || !std::isfinite(scale) || window < 0 || sinks < 0) return KV_ERR_INVALID_ARG;
@@ -526,7 +527,8 @@ int attn_call(kv_pool *p, int layout, const uint16_t *q, const uint16_t *k_new, 
     if ((k_new || v_new) && (!k_new || !v_new || !aligned16(k_new) || !aligned16(v_new))) return KV_ERR_INVALID_ARG;
     if (p->sm_count <= 0) return KV_ERR_CUDA;
     const kv_layout &L = p->desc.layouts[layout];
-    const int variant = pick_variant(p, G);
+    // the windowed call has the tensor-core kernel alone, whatever its window is
+    const int variant = window_call ? 2 : pick_variant(p, G);
     kvp::AttnArgs a{};
     a.q = q;
     a.out = out;
@@ -553,12 +555,13 @@ int attn_call(kv_pool *p, int layout, const uint16_t *q, const uint16_t *k_new, 
         a.sink_units = (a.sinks + unit - 1) / unit;
     }
     int P = 0;
-    if (a.window > 0 && num_splits == 0 && variant == 1) {
-        // the workspace is sized for the pool's variant, with fewer CTAs an SM
-        rc = L.head_dim == 64 ? kvp_attn_d64(variant, G, nullptr, &a, 0, p->sm_count, nullptr, kvp::kLaunchQuery, &P)
-                              : kvp_attn_d128(variant, G, nullptr, &a, 0, p->sm_count, nullptr, kvp::kLaunchQuery, &P);
-        if (rc) return rc;
-        num_splits = P;
+    if (window_call && num_splits == 0 && pick_variant(p, G) == 1) {
+        // the workspace is sized for the pool's variant, with fewer CTAs an SM (or,
+        // where that variant has no kernel for this group, before it was set)
+        rc = L.head_dim == 64 ? kvp_attn_d64(1, G, nullptr, &a, 0, p->sm_count, nullptr, kvp::kLaunchQuery, &P)
+                              : kvp_attn_d128(1, G, nullptr, &a, 0, p->sm_count, nullptr, kvp::kLaunchQuery, &P);
+        if (rc && rc != KV_ERR_UNSUPPORTED) return rc;
+        if (rc == KV_OK) num_splits = P;
     }
     rc = dispatch(variant, L.head_dim, G, nullptr, &a, num_splits, p->sm_count, nullptr, kvp::kLaunchQuery, &P);
     if (rc) return rc;
@@ -805,7 +808,7 @@ int paged_decode_attn_window(kv_pool *p, int layout, const uint16_t *q, const ui
                              size_t ws_bytes, void *stream)
 {
     return attn_call(p, layout, q, k_new, v_new, out, dev_table, dev_ctx_lens, max_blocks, S, Hq, scale, num_splits,
-                     workspace, ws_bytes, stream, nullptr, nullptr, window, sinks);
+                     workspace, ws_bytes, stream, nullptr, nullptr, window, sinks, true);
 }
 
 int paged_decode_attn_seqtab(kv_pool *p, kv_seqtab *t, const uint16_t *q, const uint16_t *k_new,
