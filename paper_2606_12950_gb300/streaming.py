@@ -47,6 +47,26 @@ class WindowedLayer:
             self.ws = torch.empty(n, dtype=torch.uint8, device=self.ws.device)
         return self.ws
 
+    def _check_rows(self, T: int, q, k, v) -> None:
+        """ValueError unless q, k and v are T rows each as the kernels read them
+        (bf16 on the pool's device, a row's heads packed, rows 16 bytes apart or a
+        multiple, from such an address; a row may hold more columns than are read)."""
+        for name, x, heads in (("q", q, self.Hq), ("k", k, self.Hkv), ("v", v, self.Hkv)):
+            shape, stride, row = x.shape, x.stride(), heads * self.d
+            width = 1  # columns of a row that follow one another
+            for i in range(len(shape) - 1, 0, -1):
+                if shape[i] != 1 and stride[i] != width:
+                    width = 0
+                    break
+                width *= shape[i]
+            if x.dtype != torch.bfloat16 or x.device != self.table.device:
+                raise ValueError(f"{name} must be bfloat16 on {self.table.device}, not {x.dtype} on {x.device}")
+            if len(shape) < 2 or shape[0] != T or width < row:
+                raise ValueError(f"{name} must hold {T} rows of {row} packed columns, not {tuple(shape)} with strides "
+                                 f"{stride}")
+            if x.data_ptr() % 16 or stride[0] % 8 or stride[0] < row:
+                raise ValueError(f"{name}'s rows must lie apart, each at a multiple of 16 bytes")
+
     def _append(self, q, k, v, starts, T, stream):
         """q rotated into a new tensor; k rotated, k and v written to the pages."""
         q_out = torch.empty((T, self.Hq, self.d), dtype=torch.bfloat16, device=q.device)
@@ -57,12 +77,15 @@ class WindowedLayer:
     def prompt(self, counts, q, k, v, stream=None) -> torch.Tensor:
         """Append counts[s] new tokens to each slot s and attend: q, k, v hold
         their rows, slot after slot ([T, heads * d] bf16, any row stride).
-        Returns [T, Hq, d].  KVError (KV_ERR_OUT_OF_BLOCKS) where the pool cannot
+        Returns [T, Hq, d].  ValueError where the rows do not fit (nothing has
+        changed then); KVError (KV_ERR_OUT_OF_BLOCKS) where the pool cannot
         hold a slot's tokens; slots before it keep their reservation."""
         counts = np.asarray(counts, dtype=np.int64)
         lens, T = self.tab.lens(), int(counts.sum())
         if counts.shape != (self.S,) or counts.min() < 0 or q.shape[0] != T:
             raise ValueError("counts must have a number for each slot, and q a row for each new token")
+        if T:
+            self._check_rows(T, q, k, v)
         for s in np.nonzero(counts)[0]:
             self.tab.reserve(int(s), int(lens[s] + counts[s]))
         for s in np.nonzero(counts)[0]:
@@ -84,7 +107,9 @@ class WindowedLayer:
     def step(self, q, k, v, stream=None) -> torch.Tensor:
         """One decode step: a new token for every slot that holds a context (rows
         of the others are passed over).  q, k, v: a row per slot.  Returns
-        [max_seqs, Hq, d], zeros for empty slots."""
+        [max_seqs, Hq, d], zeros for empty slots.  ValueError where the rows do
+        not fit (nothing has changed then)."""
+        self._check_rows(self.S, q, k, v)
         self.tab.advance()
         self.tab.sync(self.table, self.lens, stream)
         x = self._append(q, k, v, None, self.S, stream)
