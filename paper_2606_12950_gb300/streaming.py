@@ -83,7 +83,7 @@ class WindowedLayer:
 
     @contextlib.contextmanager
     def _go_to(self, st, here, rows):
-        if st.cuda_stream != self.last.cuda_stream:
+        if st.cuda_stream != self.handle:  # (a stream that is not torch's may be a new one by an old handle)
             if self.done is self.last:
                 st.wait_stream(self.last)
             else:

@@ -262,3 +262,11 @@ def test_an_error_leaves_the_current_stream_as_it_was(layer, streams, monkeypatc
     with pytest.raises(K.KVError):  # more tokens than a slot holds
         layer.prompt([300, 0, 0], **good(300), stream=streams.new(55))
     assert streams.current[-1].cuda_stream == 100
+
+
+def test_a_handle_may_name_a_new_stream(layer, streams, monkeypatch):
+    launched_on(layer, streams, monkeypatch)
+    for i in range(2):
+        streams.log.clear()
+        layer.step(**good(S), stream=4096)
+        assert (("wait", 4096, "event of 4096") in streams.log) == (i == 1)
