@@ -296,7 +296,8 @@ typedef struct kv_seqtab_counters {
     int64_t sync_launches;
 } kv_seqtab_counters;
 
-/* Create an empty table (all lengths 0, all entries -1).  KV_ERR_INVALID_ARG. */
+/* Create an empty table (all lengths 0, all entries -1).  KV_ERR_INVALID_ARG;
+ * KV_ERR_OUT_OF_BLOCKS (no host memory). */
 int kv_seqtab_create(kv_pool *pool, int layout, int max_seqs, int max_blocks, kv_seqtab **out);
 
 /* Release every block reference the table holds, then the table. */
@@ -346,8 +347,7 @@ int kv_seq_trim(kv_seqtab *t, int s);
  * entries; the whole-context calls (paged_decode_attn and its forms) must not
  * be given the slot any more, and kv_seq_share_prefix over such an entry is
  * KV_ERR_INVALID_ARG.  *n_freed (may be null) receives the number of blocks
- * given up.  window < 1 or sinks < 0 is KV_ERR_INVALID_ARG; no host memory for
- * the change list KV_ERR_OUT_OF_BLOCKS (nothing changed).
+ * given up.  window < 1 or sinks < 0 is KV_ERR_INVALID_ARG.
  */
 int kv_seq_evict(kv_seqtab *t, int s, int window, int sinks, int32_t *n_freed);
 

@@ -182,7 +182,6 @@ int kv_seq_fork(kv_seqtab *t, int src, int n, const int32_t *dsts, void *stream)
         if (std::adjacent_find(seen.begin(), seen.end()) != seen.end()) return KV_ERR_INVALID_ARG;
         for (int i = 0; i < full; ++i)
             if (row[i] >= 0) shared.push_back(row[i]);
-        kvp_seqtab_make_room(t, (size_t)n * (full + 1));
         int rc = KV_OK;
         if (tail > 0) {
             rc = kv_alloc_blocks(t->pool, t->layout, n, own.data());
@@ -320,8 +319,7 @@ int kv_pool_compact(kv_pool *p, int max_moves, void *stream, int *n_moves)
         std::vector<int32_t> to((size_t)p->n_pages, -1);
         for (int l = 0; l < nl; ++l)
             for (size_t i = 0; i < src[l].size(); ++i) to[(size_t)src[l][i]] = dst[l][i];
-        // room for every change first, so that nothing below can fail but the copies
-        for (kv_seqtab *t : p->seqtabs) kvp_seqtab_make_room(t, t->table.size() - t->changed.size());
+        // (what is needed below first, so that nothing there can fail but the copies)
         std::vector<int32_t> keep[KV_MAX_LAYOUTS], cut_all;
         for (int l = 0; l < nl; ++l) {
             std::vector<int32_t> taken = dst[l];
@@ -350,7 +348,7 @@ int kv_pool_compact(kv_pool *p, int max_moves, void *stream, int *n_moves)
                 p->refcnt[a] = 0;
                 p->owner[a] = -1;
             }
-            p->free_blocks[l].swap(keep[l]);
+            p->free_blocks[l].assign(keep[l].begin(), keep[l].end());  // (within its room)
             p->carved_blocks[l] += (int64_t)cut[l].size() * (p->super_pages / p->pages_per_block[l]);
             if (p->vmm.active)
                 for (int32_t sp : cut[l]) p->vmm.free_supers[(size_t)(sp / p->vmm.supers_per_chunk)] -= 1;

@@ -13,7 +13,6 @@
 int kvp_copy_pages(const kv_pool *p, int layout, int n, const int32_t *src, const int32_t *dst, const int32_t *tokens,
                    void *stream);
 
-// Set entry i of slot s and mark it changed for the next sync (seqtab.cpp).
+// Set entry i of slot s and mark it changed for the next sync (seqtab.cpp;
+// does not throw).
 void kvp_seqtab_set_entry(kv_seqtab *t, int s, int i, int32_t v);
-// Room for n such changes: set_entry does not throw for them (this may).
-void kvp_seqtab_make_room(kv_seqtab *t, size_t n);

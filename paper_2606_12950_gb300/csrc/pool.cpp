@@ -90,6 +90,7 @@ int kv_pool_create(const kv_pool_desc *desc, kv_pool **out_pool)
         if (K % p->pages_per_block[l]) { delete p; return KV_ERR_INVALID_ARG; }
         p->used_blocks[l] = 0;
         p->carved_blocks[l] = 0;
+        p->free_blocks[l].reserve((size_t)(p->n_pages / p->pages_per_block[l]));  // giving blocks back needs no memory
     }
     p->super_pages = K;
     int64_t n_super = p->n_pages / K;
@@ -264,11 +265,11 @@ int kv_pool_trim(kv_pool *p, uint64_t *released_bytes)
             if (kv.second == per_super) whole.push_back(kv.first);
         if (whole.empty()) continue;
         std::sort(whole.begin(), whole.end());
-        std::vector<int32_t> keep;
-        keep.reserve(fl.size());
-        for (int32_t id : fl)
-            if (!std::binary_search(whole.begin(), whole.end(), (int32_t)(id / K))) keep.push_back(id);
-        fl.swap(keep);
+        fl.erase(std::remove_if(fl.begin(), fl.end(),
+                                [&](int32_t id) {
+                                    return std::binary_search(whole.begin(), whole.end(), (int32_t)(id / K));
+                                }),
+                 fl.end());
         p->carved_blocks[l] -= (int64_t)whole.size() * per_super;
         for (auto it = whole.rbegin(); it != whole.rend(); ++it) {
             p->super_free.push_back(*it);

@@ -8,6 +8,7 @@
 // end of a stage or sequence (§III-C).
 #include <algorithm>
 #include <cstring>
+#include <memory>
 #include <new>
 #include <vector>
 
@@ -30,14 +31,6 @@ void set_entry(kv_seqtab *t, int s, int i, int32_t v)
     }
 }
 
-// Room for n more changes, so that set_entry cannot fail (may throw, nothing
-// changed).
-void make_room(kv_seqtab *t, size_t n)
-{
-    const size_t need = t->changed.size() + n;
-    if (t->changed.capacity() < need) t->changed.reserve(std::max(need, 2 * t->changed.capacity()));
-}
-
 // Give up the blocks of entries [lo, hi) of slot s: one reference each, the
 // entries -1.  Entries that kv_seq_evict has given up already are -1 and
 // passed over.  *n_given (may be null) receives how many were not.
@@ -45,17 +38,16 @@ int give_up(kv_seqtab *t, int s, int lo, int hi, int32_t *n_given)
 {
     const int32_t *row = &t->table[(size_t)s * t->max_blocks];
     int32_t n = 0;
-    make_room(t, (size_t)(hi - lo));
     if (std::find(row + lo, row + hi, -1) == row + hi) {
         int rc = kv_free_blocks(t->pool, t->layout, hi - lo, row + lo);
         if (rc) return rc;
         n = hi - lo;
     } else {
-        std::vector<int32_t> ids;
+        t->ids.clear();
         for (int i = lo; i < hi; ++i)
-            if (row[i] >= 0) ids.push_back(row[i]);
-        n = (int32_t)ids.size();
-        int rc = n ? kv_free_blocks(t->pool, t->layout, n, ids.data()) : KV_OK;
+            if (row[i] >= 0) t->ids.push_back(row[i]);
+        n = (int32_t)t->ids.size();
+        int rc = n ? kv_free_blocks(t->pool, t->layout, n, t->ids.data()) : KV_OK;
         if (rc) return rc;
     }
     for (int i = lo; i < hi; ++i)
@@ -68,7 +60,6 @@ int give_up(kv_seqtab *t, int s, int lo, int hi, int32_t *n_given)
 }  // namespace
 
 void kvp_seqtab_set_entry(kv_seqtab *t, int s, int i, int32_t v) { set_entry(t, s, i, v); }
-void kvp_seqtab_make_room(kv_seqtab *t, size_t n) { make_room(t, n); }
 
 void kvp_seqtab_detach(kv_seqtab *t) { t->pool = nullptr; }
 
@@ -80,23 +71,27 @@ int kv_seqtab_create(kv_pool *pool, int layout, int max_seqs, int max_blocks, kv
     if (max_seqs < 1 || max_blocks < 1) return KV_ERR_INVALID_ARG;
     if ((int64_t)max_seqs * max_blocks >= INT32_MAX) return KV_ERR_INVALID_ARG;
     if ((int64_t)max_blocks * pool->desc.block_size >= INT32_MAX) return KV_ERR_INVALID_ARG;
-    kv_seqtab *t = new kv_seqtab();
-    t->pool = pool;
-    t->layout = layout;
-    t->S = max_seqs;
-    t->max_blocks = max_blocks;
-    t->bs = pool->desc.block_size;
-    t->table.assign((size_t)max_seqs * max_blocks, -1);
-    t->lens.assign((size_t)max_seqs, 0);
-    t->held.assign((size_t)max_seqs, 0);
-    t->pending.assign((size_t)max_seqs * max_blocks, 0);
-    t->full_dirty = true;
-    std::memset(&t->counters, 0, sizeof t->counters);
-    {
+    try {
+        auto t = std::make_unique<kv_seqtab>();
+        t->pool = pool;
+        t->layout = layout;
+        t->S = max_seqs;
+        t->max_blocks = max_blocks;
+        t->bs = pool->desc.block_size;
+        t->table.assign((size_t)max_seqs * max_blocks, -1);
+        t->lens.assign((size_t)max_seqs, 0);
+        t->held.assign((size_t)max_seqs, 0);
+        t->pending.assign((size_t)max_seqs * max_blocks, 0);
+        t->changed.reserve((size_t)max_seqs * max_blocks);
+        t->ids.reserve((size_t)max_blocks);
+        t->full_dirty = true;
+        std::memset(&t->counters, 0, sizeof t->counters);
         std::lock_guard<std::mutex> g(pool->mu);
-        pool->seqtabs.push_back(t);
+        pool->seqtabs.push_back(t.get());
+        *out = t.release();
+    } catch (const std::bad_alloc &) {
+        return KV_ERR_OUT_OF_BLOCKS;
     }
-    *out = t;
     return KV_OK;
 }
 
@@ -173,7 +168,7 @@ int kv_seq_set_len(kv_seqtab *t, int s, int32_t len)
 }
 
 int kv_seq_advance(kv_seqtab *t, int n, const int32_t *seqs, int32_t *n_grown)
-{
+try {
     if (!t || !t->pool || (seqs && n < 0)) return KV_ERR_INVALID_ARG;
     std::vector<int32_t> list;
     if (seqs) {
@@ -211,6 +206,8 @@ int kv_seq_advance(kv_seqtab *t, int n, const int32_t *seqs, int32_t *n_grown)
     for (int32_t s : list) t->lens[(size_t)s] += 1;
     if (n_grown) *n_grown = (int32_t)grow.size();
     return KV_OK;
+} catch (const std::bad_alloc &) {
+    return KV_ERR_OUT_OF_BLOCKS;  // (nothing has changed)
 }
 
 int kv_seq_trim(kv_seqtab *t, int s)
@@ -233,16 +230,12 @@ int kv_seq_evict(kv_seqtab *t, int s, int window, int sinks, int32_t *n_freed)
     const int first = (int)(((int64_t)sinks + t->bs - 1) / t->bs);
     const int last = (int)std::max<int64_t>(0, ((int64_t)t->lens[(size_t)s] - window) / t->bs);
     if (first >= last) return KV_OK;
-    try {
-        return give_up(t, s, first, last, n_freed);
-    } catch (const std::bad_alloc &) {
-        return KV_ERR_OUT_OF_BLOCKS;  // no host memory: nothing changed
-    }
+    return give_up(t, s, first, last, n_freed);
 }
 
 int kv_seq_replace(kv_seqtab *t, int n, const int32_t *slots, const int64_t *reserve_tokens,
                    const int32_t *lens, int32_t *status)
-{
+try {
     if (!t || !t->pool || n < 0) return KV_ERR_INVALID_ARG;
     if (n == 0) return KV_OK;
     if (!slots || !reserve_tokens || !lens || !status) return KV_ERR_INVALID_ARG;
@@ -270,6 +263,8 @@ int kv_seq_replace(kv_seqtab *t, int n, const int32_t *slots, const int64_t *res
         status[i] = KV_OK;
     }
     return KV_OK;
+} catch (const std::bad_alloc &) {
+    return KV_ERR_OUT_OF_BLOCKS;  // (nothing has changed)
 }
 
 int kv_seqtab_host(const kv_seqtab *t, const int32_t **table, const int32_t **ctx_lens)

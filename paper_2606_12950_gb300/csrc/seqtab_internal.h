@@ -16,7 +16,8 @@ struct kv_seqtab {
     std::vector<int32_t> lens;     // [S]
     std::vector<int32_t> held;     // blocks held per slot (a prefix of the row)
     std::vector<uint8_t> pending;  // entry changed since the last sync
-    std::vector<int32_t> changed;  // flat indices of pending entries
+    std::vector<int32_t> changed;  // flat indices of pending entries (room for all: a change needs no memory)
+    std::vector<int32_t> ids;      // blocks being given up (room for a row)
     bool full_dirty = true;        // the device copy has never been written
     kv_seqtab_counters counters;
 };
