@@ -7,6 +7,7 @@
 #include <atomic>
 
 #include "cascade_impl.cuh"
+#include "device_flags.h"
 #include "stream_order.h"
 
 namespace kvp {
@@ -81,13 +82,15 @@ int attn_run(const CUtensorMap *tmap, AttnArgs a, int P_req, int sm_count, cudaS
     auto fn = paged_attn_kernel<D, G, Comp, kRecWarps>;
     auto fn_merge = paged_attn_kernel<D, G, Comp, kRecCtas>;
     auto fn_by_part = paged_attn_kernel<D, G, Comp, kRecCtasByPart>;
-    static std::atomic<bool> attr_set{false};
-    if (!attr_set.load()) {
+    static DeviceFlags attr_set;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return KV_ERR_CUDA;
+    if (!attr_set.has(dev)) {
         if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax) != cudaSuccess ||
             cudaFuncSetAttribute(fn_merge, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax) != cudaSuccess ||
             cudaFuncSetAttribute(fn_by_part, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax) != cudaSuccess)
             return KV_ERR_CUDA;
-        attr_set.store(true);
+        attr_set.set(dev);
     }
     // six warps a CTA, eight beside the shared-prefix kernel (kPlainWarps)
     const int most_warps = a.skip != nullptr ? kWarps : kPlainWarps;
@@ -208,11 +211,13 @@ int cascade_run(const CUtensorMap *tmap, const CascadeArgs *c, int grid, int sm_
 {
     auto fn = cascade_prefix_kernel<D, G>;
     const size_t smem = cascade_smem_bytes<D>();
-    static std::atomic<bool> attr_set{false};
-    if (!attr_set.load()) {
+    static DeviceFlags attr_set;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return KV_ERR_CUDA;
+    if (!attr_set.has(dev)) {
         if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
             return KV_ERR_CUDA;
-        attr_set.store(true);
+        attr_set.set(dev);
     }
     if (!launch) {
         int occ = 0;

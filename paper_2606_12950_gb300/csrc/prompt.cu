@@ -1,7 +1,6 @@
 // prompt.cu -- causal attention of prompt chunks over the paged pool
 // (paged_prompt_attn): argument checks, the split of the key range, launches.
 #include <algorithm>
-#include <atomic>
 #include <climits>
 #include <cmath>
 #include <cstdint>
@@ -9,6 +8,7 @@
 #include <cuda_runtime.h>
 
 #include "attn_host.h"
+#include "device_flags.h"
 #include "pool_internal.h"
 #include "prompt_impl.cuh"
 #include "stream_order.h"
@@ -68,9 +68,11 @@ template <int D>
 int prompt_run(const CUtensorMap *tmap, const CUtensorMap &qmap, const CUtensorMap &omap, const kvp::PromptArgs &a,
                int sm_count, cudaStream_t st)
 {
-    static std::atomic<bool> attr_set{false};
+    static kvp::DeviceFlags attr_set;
     const size_t smem = kvp::prompt_smem_bytes<D>();
-    if (!attr_set.load()) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return KV_ERR_CUDA;
+    if (!attr_set.has(dev)) {
         if (cudaFuncSetAttribute(kvp::prompt_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
             cudaSuccess)
             return KV_ERR_CUDA;
@@ -79,7 +81,7 @@ int prompt_run(const CUtensorMap *tmap, const CUtensorMap &qmap, const CUtensorM
         cudaFuncAttributes at;
         if (cudaFuncGetAttributes(&at, kvp::prompt_attn_kernel<D>) != cudaSuccess || at.numRegs != kvp::kPrRegsLaunch)
             return KV_ERR_CUDA;
-        attr_set.store(true);
+        attr_set.set(dev);
     }
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
