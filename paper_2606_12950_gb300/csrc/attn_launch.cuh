@@ -192,7 +192,7 @@ int attn_run(const CUtensorMap *tmap, AttnArgs a, int P_req, int sm_count, cudaS
     // shared-prefix mode
     const int runs = a.S * a.Hkv;
     const double per_run = (double)P * (merge && small ? 1 : a.nwarps) / std::max(1, runs) + 1.0 + (a.skip ? a.KS : 0);
-    if constexpr (G * D / 4 >= 128) {
+    if constexpr (!Comp::WIN && G * D / 4 >= 128) {  // (no windowed call has a shared prefix)
         // one group in shared-prefix mode: two columns a thread, so that
         // every member run fits in one wave
         if (a.skip != nullptr && combine_groups<D, G, 1>(per_run) == 1)
