@@ -543,7 +543,9 @@ int kv_append(kv_pool *pool, int layout, const uint16_t *k_new, const uint16_t *
  *     frequency makes over the trained context (NTK-by-parts; Peng et al.,
  *     2023): f / factor up to low_turns, f from high_turns on, between them
  *     mixed in proportion.  Those authors' magnitude is 0.1 ln(factor) + 1.
- * A caller with other frequencies fills the array itself.
+ * A caller with other frequencies fills the array itself, e.g. with a mix that
+ * goes linearly by the pair's index between two bounds, not by its turns, as some
+ * checkpoints' configurations ask.
  * Errors: KV_ERR_INVALID_ARG (rot_dim odd or not in [2, 512], base <= 1,
  * factor < 1, high_turns <= low_turns, original_len < 1).
  *

@@ -57,9 +57,9 @@
 // WIN: a sliding window with sinks.  A run's units are the sinks' tiles, then
 // those from the window's first token on; rows between the two in a unit get no
 // weight and their V is cleared.  Everything else is shared, so a windowed call
-// streams as the others do: 64 sequences, window 1024 (245 MB) 44.7 us, 250 with
-// window 2048 (789 MB) 123.5 (6.4 TB/s), one of 50001 tokens, window 4096, 11.0
-// (bound by latency: two launches).
+// streams as the others do: 64 sequences, window 1024 (245 MB) 45 us, 250 with
+// window 2048 (789 MB) 124 (6.35 TB/s), one of 50001 tokens, window 4096, 10.9
+// (two launches, not told apart yet from the host's call).
 //
 // Grid-to-grid order: the kernel is launched as a programmatic dependent.
 // Alone it releases the next grid and waits for the one before; as part of

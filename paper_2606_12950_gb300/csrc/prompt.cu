@@ -26,6 +26,13 @@ int64_t row_tiles(int S, int T, int max_q, int TT)
 // heads of 128): 16 tokens on a context of 16000 158, 87, 51, 32, 26; 64 on 8000
 // 86, 52, 34, 25, 26; 256 on 8000 (4 by this rule) 90, 56, 38; 64 on 2000 (4) 30,
 // 24, 20; 4 x 100, window 1024 (2) 28, 25.
+// The lengths are on the device, so the rule takes the table's width for them: in
+// a table much wider than its sequences a call pays for splits without keys and
+// for a merge.  us in a table as wide as the context and in one of 32768 tokens
+// (splits): 33 tokens, 4 q / 2 KV heads of 64, 6.4 (1) and 9.2 (16); 100 tokens,
+// 32 / 8 of 128, 8.4 (1) and 13.6 (9); chunks of 60, 90 and 100 tokens, window
+// 1024, 12.6 (1) and 15.2 (2); 16 tokens on 1000 13.4 (2) and 12.4 (16); 128 on
+// 4000 20.7 (8) and 21.1 (9).
 constexpr int kLeastTiles = 4;
 int key_splits(int64_t ctas, int sm_count, int64_t reach, int TT, int window, int sinks)
 {

@@ -34,12 +34,12 @@
 // What bounds it, and what it measured.  At d = 128 (32 q / 8 KV heads): the
 // chain S -> softmax -> P.V -> S of a Q tile, 2450 clocks for two 128 x 128
 // tiles where the tensor core's own time is 2048, and the power limit: 16384
-// tokens with a window of 4096 (963 GFLOP) 622 to 661 us, 1460 to 1550 TFLOP/s
-// (a plain library product 1705 sustained).  At d = 64: the softmax warps, 2440
+// tokens with a window of 4096 (963 GFLOP) 658 us, 1460 TFLOP/s (a plain library
+// product 1705 sustained; the lowest seen on any GPU 600 us).  At d = 64: the softmax warps, 2440
 // clocks where the exponentials are 1100 (each warp's own latencies; two Q tiles
 // leave a sub-partition two warps): 5 causal prompts of 700 to 2500 tokens, 16
-// heads, 70 to 78 us.  Short items pay 5 us for a CTA's start and about 8000
-// clocks an item (masked tiles, output): 9 ragged chunks, window 1024, 73 to 83
+// heads, 69 to 78 us.  Short items pay 5 us for a CTA's start and about 8000
+// clocks an item (masked tiles, output): 9 ragged chunks, window 1024, 67 to 74
 // us for 52 GFLOP.
 //
 // Few rows (KS > 1): an item's key tiles are split over KS items, each leaving
