@@ -72,10 +72,27 @@ typedef enum kv_status {
 
 #define KV_MAX_LAYOUTS 4
 
-/* Geometry of one model's layer KV in the pool. */
+/*
+ * Geometry of one model's layer KV in the pool.
+ *
+ * KV_Q4, added to head_dim (64 or 128; block sizes that are multiples of 16),
+ * makes a layout whose blocks are held in 4 bits: kv_pack_blocks fills them
+ * from bf16 blocks of the same geometry, kv_unpack_blocks reads them back and
+ * paged_decode_attn_q4 attends over them; the bf16 calls refuse such a layout
+ * (KV_ERR_UNSUPPORTED).  Groups of 64 columns of a token's K or V row share a
+ * scale s and a least value z (bf16); a code c in 0..15 stands for s c + z:
+ *     z = min x,  s = bf16((max x - z) / 15),  c = the code nearest to (x - z) / s
+ * (ties to even; s = 0, and c = 0, where (max x - z) / 15 is below 2^-100).  A
+ * group whose span max x - z is not below 2^80, or that holds a NaN, is NaN
+ * throughout.  4.5 bits a value: a block takes 9/32 of its bf16 form,
+ * [Hkv][bs / 16] tiles of 16 tokens, K and V side by side (csrc/q4_format.h).
+ * In a pool of bf16 and 4-bit blocks of one geometry, page_bytes is a 32nd of
+ * the bf16 block; a superpage then holds one bf16 block or three 4-bit ones.
+ */
+#define KV_Q4 0x10000
 typedef struct kv_layout {
     int32_t num_kv_heads; /* Hkv >= 1 */
-    int32_t head_dim;     /* d: 64 or 128 */
+    int32_t head_dim;     /* d: 64 or 128; | KV_Q4 */
 } kv_layout;
 
 typedef struct kv_pool_desc {
@@ -85,7 +102,10 @@ typedef struct kv_pool_desc {
     int32_t num_layouts;   /* 1..KV_MAX_LAYOUTS */
     kv_layout layouts[KV_MAX_LAYOUTS];
     uint64_t page_bytes;   /* 0 = smallest layout block; every layout's block
-                              bytes must be a multiple of it, and it a multiple of 256 */
+                              bytes must be a multiple of it, and it a multiple of 256
+                              (with a 4-bit layout: of 128); without a 4-bit layout
+                              the largest block must be a multiple of each (with one
+                              a superpage's rest is unused) */
     int32_t *device_error; /* caller-owned device int32, zero-initialised */
     uint64_t shuffle_seed; /* 0: free list hands out ascending ids; otherwise the
                               initial free order is a seeded permutation
@@ -201,12 +221,32 @@ int kv_pool_compact(kv_pool *pool, int max_moves, void *stream, int *n_moves);
  * block) of block src[i] to block dst[i], for i < n (host arrays), on
  * `stream`.  The copies run side by side.  Checked before anything is
  * launched, else KV_ERR_INVALID_ARG: every id names a live block of `layout`,
- * no destination appears twice or is also a source, 0 <= tokens[i] <= bs.
+ * no destination appears twice or is also a source, 0 <= tokens[i] <= bs.  Of
+ * a 4-bit layout only whole blocks are copied: KV_ERR_UNSUPPORTED for others.
  * The triples travel as kernel parameters (1360 a launch): the arrays may
  * change right after the call.
  */
 int kv_copy_blocks(kv_pool *pool, int layout, int n, const int32_t *src, const int32_t *dst, const int32_t *tokens,
                    void *stream);
+
+/*
+ * Pack: block src[i] of the bf16 layout `layout` into block dst[i] of the
+ * 4-bit layout `q4_layout` (KV_Q4), for i < n (host arrays), on `stream`; and
+ * the way back: kv_unpack_blocks writes bf16(s c + z) for every value of block
+ * src[i] of `q4_layout` into block dst[i] of `layout` (e.g. for
+ * paged_prompt_attn, when a chat goes on with a new prompt).  The layouts have
+ * the same heads and columns.  Blocks run side by side.  Checked before
+ * anything is launched, else KV_ERR_INVALID_ARG: every id names a live block
+ * of its layout, no destination appears twice.  A source may appear again.
+ * Packing what was unpacked gives the same values where bf16 holds s c + z.
+ * The pairs travel as kernel parameters (2040 a launch): the arrays may change
+ * right after the call.  Errors also: KV_ERR_UNSUPPORTED (a layout that is
+ * not of that kind), KV_ERR_CUDA.
+ */
+int kv_pack_blocks(kv_pool *pool, int layout, int q4_layout, int n, const int32_t *src, const int32_t *dst,
+                   void *stream);
+int kv_unpack_blocks(kv_pool *pool, int q4_layout, int layout, int n, const int32_t *src, const int32_t *dst,
+                     void *stream);
 
 /* A physical-memory budget shared by VMM pools (e.g. M_total - M_res of the
  * node, §III-C).  Destroy it after every pool that uses it. */
@@ -360,9 +400,32 @@ int kv_seq_evict(kv_seqtab *t, int s, int window, int sinks, int32_t *n_freed);
  * its own; entries it has given up (kv_seq_evict) stay -1.  All-or-nothing:
  * KV_ERR_OUT_OF_BLOCKS (a block per fork is needed where the length is no
  * multiple of the block size), KV_ERR_INVALID_ARG (a slot that is not empty,
- * given twice, or src itself) and KV_ERR_CUDA leave every slot as it was.
+ * given twice, or src itself), KV_ERR_UNSUPPORTED (a 4-bit layout, whose
+ * blocks are copied whole, and a partial last block) and KV_ERR_CUDA leave
+ * every slot as it was.
  */
 int kv_seq_fork(kv_seqtab *t, int src, int n, const int32_t *dsts, void *stream);
+
+/*
+ * Move old tokens of n distinct slots into 4 bits: t is a table over a bf16
+ * layout, t4 one over a KV_Q4 layout of the same pool and geometry, slot s of
+ * both one chat.  t4's length of a slot is its packed tokens, a multiple of
+ * the block size.  For each slot, every full block of t after those, but for
+ * the ones that the last `keep` tokens reach (keep >= 1), is packed on
+ * `stream` (kv_pack_blocks) into a new block of t4; t4's length grows, one
+ * reference to the bf16 block is dropped and its entry in t becomes -1, as
+ * kv_seq_evict's do (t's length stays; paged_decode_attn_q4 reads both).
+ * *n_packed (may be null) receives the number of blocks.  Sync both tables
+ * afterwards.  A block given up here is free at once: work on other streams
+ * that reads it has to be ordered before `stream`, and later writers after it.
+ * All-or-nothing: KV_ERR_OUT_OF_BLOCKS (4-bit blocks, or no host memory),
+ * KV_ERR_INVALID_ARG (tables of different pools or slot counts, keep < 1, a
+ * slot out of range or given twice, t4 shorter than a slot needs, a packed
+ * length that is not what t4 holds, or is past t's, an entry that
+ * kv_seq_evict has given up), KV_ERR_UNSUPPORTED and KV_ERR_CUDA leave both
+ * tables as they were.
+ */
+int kv_seq_pack(kv_seqtab *t, kv_seqtab *t4, int n, const int32_t *slots, int keep, void *stream, int32_t *n_packed);
 
 /*
  * A step's finished sequences replaced by new admissions, in one call: for
@@ -612,6 +675,32 @@ int kv_append_rotary(kv_pool *pool, int layout, const kv_rotary *rot, const uint
                      const int32_t *dev_ctx_lens, int max_blocks, int S, int Hq, void *stream);
 
 /*
+ * kv_append_rotary with each head of q and k normed first (RMSNorm over its d
+ * columns):
+ *     x / sqrt(mean(x^2) + eps) * (weight + offset)
+ * and then rotated; v is copied.  q_weight, k_weight: bf16 [d], shared by all
+ * heads, 16-byte aligned device arrays; NULL: those heads are not normed.
+ * offset: 0, or 1 where the checkpoint holds weights about 0.  Everything is
+ * in fp32, the sum of squares too, with one rounding to bf16 at the end, also
+ * for the columns past rot_dim.  A row of zeros with eps = 0 gives NaN; a row
+ * with an infinity or a NaN gives NaN.  All else, the strides, q == q_out,
+ * ragged chunks and errors, is as there; KV_ERR_INVALID_ARG also for eps < 0
+ * or not finite, KV_ERR_UNSUPPORTED for head dims above 256.
+ */
+typedef struct kv_head_norm {
+    const uint16_t *q_weight;
+    const uint16_t *k_weight;
+    float eps;
+    float offset;
+} kv_head_norm;
+
+int kv_append_rotary_norm(kv_pool *pool, int layout, const kv_rotary *rot, const kv_head_norm *norm, const uint16_t *q,
+                          int64_t q_stride, uint16_t *q_out, const uint16_t *k, int64_t k_stride, const uint16_t *v,
+                          int64_t v_stride, const int32_t *positions, const int32_t *dev_q_starts, int T,
+                          const int32_t *dev_table, const int32_t *dev_ctx_lens, int max_blocks, int S, int Hq,
+                          void *stream);
+
+/*
  * Bytes of device workspace paged_decode_attn needs for these sizes and this
  * num_splits: a run table, two int32 per (sequence, KV head) run that say
  * where its records are, followed by fp32 split partials, one record of
@@ -689,6 +778,35 @@ int paged_decode_attn_window(kv_pool *pool, int layout, const uint16_t *q, const
                              const uint16_t *v_new, uint16_t *out, const int32_t *dev_table,
                              const int32_t *dev_ctx_lens, int max_blocks, int S, int Hq, float scale, int window,
                              int sinks, int num_splits, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * paged_decode_attn (k_new, v_new NULL) or paged_decode_attn_append over a
+ * context whose first tokens are held in 4 bits: token j of sequence s is
+ *     j < p: token j % bs of block dev_table4[s][j / bs] of `q4_layout`
+ *     p <= j < n: token j % bs of block dev_table[s][j / bs] of `layout`
+ * with n = dev_ctx_lens[s] (post-append) and p = dev_packed_lens[s], a
+ * multiple of 16 from 0 to n (to n - 1 where a row is appended: it goes to a
+ * bf16 block).  Entries of dev_table before p / bs are never looked at
+ * (kv_seq_pack makes them -1).  The codes' values s c + z are used as they
+ * are, not rounded to bf16.  A p that is none of those, or past
+ * max_blocks4 * bs, sets the error word.
+ * Arithmetic: q scaled by a power of two to fp16, products with the codes on
+ * the tensor cores, scales and least values applied in fp32 to the scores and
+ * to the weights, which are rounded to fp16 with the scale (to bf16 before
+ * rows in bf16); sums and softmax statistics in fp32.  Where |scale * q . K|
+ * is near fp32's range, or q holds an infinity or a NaN, the output is NaN.
+ * V groups with s below 2^-60 count as constant.
+ * The result of a call does not depend on where its blocks lie.
+ * Workspace: kv_q4_workspace_bytes (256-byte aligned, not initialised).
+ * Errors: those of paged_decode_attn; layout and q4_layout have the same heads
+ * and columns, else KV_ERR_INVALID_ARG.
+ */
+int kv_q4_workspace_bytes(const kv_pool *pool, int q4_layout, int S, int Hq, int max_blocks, size_t *out_bytes);
+
+int paged_decode_attn_q4(kv_pool *pool, int layout, int q4_layout, const uint16_t *q, const uint16_t *k_new,
+                         const uint16_t *v_new, uint16_t *out, const int32_t *dev_table, const int32_t *dev_ctx_lens,
+                         int max_blocks, const int32_t *dev_table4, const int32_t *dev_packed_lens, int max_blocks4,
+                         int S, int Hq, float scale, void *workspace, size_t ws_bytes, void *stream);
 
 /*
  * Causal attention of prompt chunks over the paged pool: sequence s's queries

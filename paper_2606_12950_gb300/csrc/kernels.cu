@@ -435,7 +435,7 @@ int kv_append(kv_pool *p, int layout, const uint16_t *k_new, const uint16_t *v_n
     if (!k_new || !v_new || !dev_table || !dev_ctx_lens) return KV_ERR_INVALID_ARG;
     if (!aligned16(k_new) || !aligned16(v_new)) return KV_ERR_INVALID_ARG;
     const kv_layout &L = p->desc.layouts[layout];
-    if (L.head_dim % 8) return KV_ERR_UNSUPPORTED;
+    if (L.head_dim % 8 || (L.head_dim & KV_Q4)) return KV_ERR_UNSUPPORTED;
     const int64_t total = (int64_t)S * L.num_kv_heads * 2 * (L.head_dim / 8);
     const int threads = 256;
     const int64_t want = (total + threads - 1) / threads;

@@ -18,6 +18,7 @@
 
 #include "pages_internal.h"
 #include "pool_internal.h"
+#include "q4_format.h"
 #include "ptx.cuh"
 #include "seqtab_internal.h"
 #include "stream_order.h"
@@ -84,6 +85,11 @@ int copy_launch(const kv_pool *p, int layout, int n, const int32_t *src, const i
     c.row_bytes = 2 * L.head_dim;
     c.seg_stride = (int64_t)p->desc.block_size * c.row_bytes;
     c.segs = 2 * L.num_kv_heads;
+    if (kvp_is_q4(L)) {  // copied whole, or (no tokens) not at all
+        c.row_bytes = 0;
+        c.seg_stride = (int64_t)p->block_bytes[layout];
+        c.segs = 1;
+    }
     c.bs = p->desc.block_size;
     for (int i = 0; i < n; ++i) {
         c.at[i][0] = src[i];
@@ -137,6 +143,9 @@ int kv_copy_blocks(kv_pool *p, int layout, int n, const int32_t *src, const int3
     if (!p || layout < 0 || layout >= p->desc.num_layouts || n < 0) return KV_ERR_INVALID_ARG;
     if (n == 0) return KV_OK;
     if (!src || !dst) return KV_ERR_INVALID_ARG;
+    if (tokens && kvp_is_q4(p->desc.layouts[layout]))
+        for (int i = 0; i < n; ++i)
+            if (tokens[i] > 0 && tokens[i] < p->desc.block_size) return KV_ERR_UNSUPPORTED;
     {
         // every id a live block; no destination twice, none that is also a
         // source: the copies run side by side.  Marks go to the pool's tally,
@@ -176,6 +185,7 @@ int kv_seq_fork(kv_seqtab *t, int src, int n, const int32_t *dsts, void *stream)
     const int full = len / t->bs, tail = len % t->bs;
     const int32_t *row = &t->table[(size_t)src * t->max_blocks];
     if (tail > 0 && row[full] < 0) return KV_ERR_INVALID_ARG;  // the last token's page was given up
+    if (tail > 0 && kvp_is_q4(t->pool->desc.layouts[t->layout])) return KV_ERR_UNSUPPORTED;
     try {
         std::vector<int32_t> seen(dsts, dsts + n), shared, own((size_t)n), from((size_t)n), rows((size_t)n);
         std::sort(seen.begin(), seen.end());
@@ -297,7 +307,7 @@ int kv_pool_compact(kv_pool *p, int max_moves, void *stream, int *n_moves)
                     while (supers[(size_t)order[super_from - 1]].empty()) --super_from;
                     std::vector<int32_t> &f = supers[(size_t)order[super_from - 1]];
                     const int32_t step = p->pages_per_block[l];
-                    for (int32_t off = 0; off < p->super_pages; off += step)
+                    for (int32_t off = 0; off + step <= p->super_pages; off += step)
                         room[l][(size_t)order[super_from - 1]].push_back(f.back() * p->super_pages + off);
                     spare[l] += p->super_pages / step;
                     cut[l].push_back(f.back());
@@ -329,7 +339,7 @@ int kv_pool_compact(kv_pool *p, int max_moves, void *stream, int *n_moves)
             };
             for (int32_t id : p->free_blocks[l]) take(id);
             for (int32_t sp : cut[l])
-                for (int32_t off = 0; off < p->super_pages; off += p->pages_per_block[l]) take(sp * p->super_pages + off);
+                for (int32_t off = 0; off + p->pages_per_block[l] <= p->super_pages; off += p->pages_per_block[l]) take(sp * p->super_pages + off);
             keep[l].insert(keep[l].end(), src[l].begin(), src[l].end());
             cut_all.insert(cut_all.end(), cut[l].begin(), cut[l].end());
         }

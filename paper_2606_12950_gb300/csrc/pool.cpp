@@ -14,6 +14,7 @@
 #include <cuda_runtime.h>
 
 #include "pool_internal.h"
+#include "q4_format.h"
 #include "stream_order.h"
 
 namespace {
@@ -62,16 +63,23 @@ int kv_pool_create(const kv_pool_desc *desc, kv_pool **out_pool)
     if (desc->num_layouts < 1 || desc->num_layouts > KV_MAX_LAYOUTS) return KV_ERR_INVALID_ARG;
     if (desc->block_size < 1 || desc->block_size > 256) return KV_ERR_INVALID_ARG;
     uint64_t min_block = UINT64_MAX, max_block = 0;
+    bool any_q4 = false;
     for (int l = 0; l < desc->num_layouts; ++l) {
         const kv_layout &L = desc->layouts[l];
         if (L.num_kv_heads < 1 || L.num_kv_heads > 1024) return KV_ERR_INVALID_ARG;
-        if (L.head_dim < 8 || L.head_dim > 512 || (L.head_dim % 8)) return KV_ERR_INVALID_ARG;
-        uint64_t bb = 2ull * L.num_kv_heads * desc->block_size * L.head_dim * 2ull;
+        if (kvp_is_q4(L)) {
+            if (kvp_head_dim(L) != 64 && kvp_head_dim(L) != 128) return KV_ERR_INVALID_ARG;
+            if (desc->block_size % kQ4Tile) return KV_ERR_INVALID_ARG;
+            any_q4 = true;
+        } else if (L.head_dim < 8 || L.head_dim > 512 || (L.head_dim % 8)) {
+            return KV_ERR_INVALID_ARG;
+        }
+        const uint64_t bb = kvp_layout_block_bytes(L, desc->block_size);
         min_block = std::min(min_block, bb);
         max_block = std::max(max_block, bb);
     }
     uint64_t page = desc->page_bytes ? desc->page_bytes : min_block;
-    if (page == 0 || (page % 256)) return KV_ERR_INVALID_ARG;
+    if (page == 0 || (page % (any_q4 ? 128 : 256))) return KV_ERR_INVALID_ARG;
     kv_pool *p = new kv_pool();
     p->desc = *desc;
     p->page_bytes = page;
@@ -79,15 +87,15 @@ int kv_pool_create(const kv_pool_desc *desc, kv_pool **out_pool)
     if (p->n_pages > INT32_MAX) { delete p; return KV_ERR_INVALID_ARG; }
     int32_t K = 1;
     for (int l = 0; l < desc->num_layouts; ++l) {
-        const kv_layout &L = desc->layouts[l];
-        uint64_t bb = 2ull * L.num_kv_heads * desc->block_size * L.head_dim * 2ull;
+        const uint64_t bb = kvp_layout_block_bytes(desc->layouts[l], desc->block_size);
         if (bb % page) { delete p; return KV_ERR_INVALID_ARG; }
         p->block_bytes[l] = bb;
         p->pages_per_block[l] = (int32_t)(bb / page);
         K = std::max<int32_t>(K, p->pages_per_block[l]);
     }
     for (int l = 0; l < desc->num_layouts; ++l) {
-        if (K % p->pages_per_block[l]) { delete p; return KV_ERR_INVALID_ARG; }
+        // (9 pages of 4 bits beside 32 of bf16: a superpage's last 5 are not used)
+        if (K % p->pages_per_block[l] && !any_q4) { delete p; return KV_ERR_INVALID_ARG; }
         p->used_blocks[l] = 0;
         p->carved_blocks[l] = 0;
         p->free_blocks[l].reserve((size_t)(p->n_pages / p->pages_per_block[l]));  // giving blocks back needs no memory

@@ -24,6 +24,7 @@ KV_ERR_UNSUPPORTED = -5
 KV_ERR_WORKSPACE = -6
 KV_ERR_DEVICE_TIMEOUT = -7
 KV_MAX_LAYOUTS = 4
+KV_Q4 = 0x10000  # added to a layout's head dim: its blocks are held in 4 bits
 
 _NAMES = {
     0: "KV_OK", -1: "KV_ERR_INVALID_ARG", -2: "KV_ERR_OUT_OF_BLOCKS", -3: "KV_ERR_CUDA",
@@ -155,6 +156,11 @@ class kv_rotary(ctypes.Structure):
                 ("magnitude", ctypes.c_float), ("reserved", ctypes.c_int32)]
 
 
+class kv_head_norm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("offset", ctypes.c_float)]
+
+
 KV_ROTARY_PLAIN, KV_ROTARY_LINEAR, KV_ROTARY_BY_PARTS = 0, 1, 2
 KV_ENGINE_IDLE, KV_ENGINE_SLEEPING, KV_ENGINE_SLEEP_PENDING, KV_ENGINE_ACTIVE, KV_ENGINE_COLD = 0, 1, 2, 3, 4
 KV_ACT_SLEEP, KV_ACT_EVICT, KV_ACT_STOP, KV_ACT_PREEMPT, KV_ACT_ABORT = 1, 2, 3, 4, 5
@@ -208,6 +214,12 @@ def lib() -> ctypes.CDLL:
             "kv_rotary_freqs": [ctypes.POINTER(kv_rotary_desc), P],
             "kv_rotary_steps": [P, I, P],
             "kv_append_rotary": [P, I, P, P, I64, P, P, I64, P, I64, P, P, I, P, P, I, I, I, P],
+            "kv_append_rotary_norm": [P, I, P, P, P, I64, P, P, I64, P, I64, P, P, I, P, P, I, I, I, P],
+            "kv_pack_blocks": [P, I, I, I, P, P, P],
+            "kv_unpack_blocks": [P, I, I, I, P, P, P],
+            "kv_seq_pack": [P, P, I, P, I, P, ctypes.POINTER(I32)],
+            "kv_q4_workspace_bytes": [P, I, I, I, I, ctypes.POINTER(SZ)],
+            "paged_decode_attn_q4": [P, I, I, P, P, P, P, P, P, I, P, P, I, I, I, F, P, SZ, P],
             "paged_decode_attn_window": [P, I, P, P, P, P, P, P, I, I, I, F, I, I, I, P, SZ, P],
             "kv_prompt_workspace_bytes": [P, I, I, I, I, I, I, I, I, ctypes.POINTER(SZ)],
             "paged_prompt_attn": [P, I, P, P, P, I, I, P, P, I, I, I, F, I, I, P, SZ, P],
@@ -378,6 +390,25 @@ def kv_copy_blocks(pool, layout: int, src, dst, tokens=None, stream=None) -> Non
                                 _stream(stream)))
 
 
+def _pairs(name: str, pool, first: int, second: int, src, dst, stream) -> None:
+    src, dst = _i32(src), _i32(dst)
+    if src.ndim != 1 or src.shape != dst.shape:
+        raise ValueError("src and dst must be 1-D and of one length")
+    _check(name, getattr(lib(), name)(pool, first, second, src.size, _data(src), _data(dst), _stream(stream)))
+
+
+def kv_pack_blocks(pool, layout: int, q4_layout: int, src, dst, stream=None) -> None:
+    """Pack bf16 block src[i] of `layout` into 4-bit block dst[i] of
+    `q4_layout`; host arrays of one length."""
+    _pairs("kv_pack_blocks", pool, layout, q4_layout, src, dst, stream)
+
+
+def kv_unpack_blocks(pool, q4_layout: int, layout: int, src, dst, stream=None) -> None:
+    """Write 4-bit block src[i] of `q4_layout` out as bf16 block dst[i] of
+    `layout`; host arrays of one length."""
+    _pairs("kv_unpack_blocks", pool, q4_layout, layout, src, dst, stream)
+
+
 def kv_budget_create(limit_bytes: int):
     out = ctypes.c_void_p()
     _check("kv_budget_create", lib().kv_budget_create(int(limit_bytes), ctypes.byref(out)))
@@ -504,6 +535,25 @@ def kv_append_rotary(pool, layout: int, rotary: Rotary, q, q_stride: int, q_out,
           S, Hq, _stream(stream))
 
 
+class HeadNorm:
+    """The norms of kv_append_rotary_norm, marshalled once: bf16 [d] device
+    weights of q and k (None: not normed), eps, and the weights' offset."""
+
+    def __init__(self, q_weight, k_weight, eps: float = 1e-6, offset: float = 0.0):
+        self.weights = (q_weight, k_weight)  # kept alive
+        self.struct = kv_head_norm(_addr(q_weight), _addr(k_weight), float(eps), float(offset))
+        self.address = ctypes.addressof(self.struct)
+
+
+def kv_append_rotary_norm(pool, layout: int, rotary: Rotary, norm: HeadNorm, q, q_stride: int, q_out, k, k_stride: int, v,
+                          v_stride: int, positions, q_starts, T: int, dev_table, dev_ctx_lens, max_blocks: int, S: int,
+                          Hq: int, stream=None) -> None:
+    """kv_append_rotary with each head of q and k normed first."""
+    _call("kv_append_rotary_norm", pool, layout, rotary.address, norm.address, _addr(q), q_stride, _addr(q_out),
+          _addr(k), k_stride, _addr(v), v_stride, _addr(positions), _addr(q_starts), T, _addr(dev_table),
+          _addr(dev_ctx_lens), max_blocks, S, Hq, _stream(stream))
+
+
 def kv_workspace_bytes(pool, layout: int, S: int, Hq: int, max_blocks: int, num_splits: int = 0) -> int:
     n = ctypes.c_size_t(0)
     _check("kv_workspace_bytes", lib().kv_workspace_bytes(pool, layout, int(S), int(Hq), int(max_blocks),
@@ -543,6 +593,24 @@ def paged_decode_attn_window(pool, layout: int, q, k_new, v_new, out, dev_table,
     _call("paged_decode_attn_window", pool, layout, _addr(q), _addr(k_new), _addr(v_new), _addr(out),
           _addr(dev_table), _addr(dev_ctx_lens), max_blocks, S, Hq, scale, window, sinks, num_splits,
           _addr(workspace), ws_bytes, _stream(stream))
+
+
+def kv_q4_workspace_bytes(pool, q4_layout: int, S: int, Hq: int, max_blocks: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check("kv_q4_workspace_bytes",
+           lib().kv_q4_workspace_bytes(pool, q4_layout, int(S), int(Hq), int(max_blocks), ctypes.byref(n)))
+    return int(n.value)
+
+
+def paged_decode_attn_q4(pool, layout: int, q4_layout: int, q, k_new, v_new, out, dev_table, dev_ctx_lens,
+                         max_blocks: int, dev_table4, dev_packed_lens, max_blocks4: int, S: int, Hq: int, scale: float,
+                         workspace, ws_bytes: int, stream=None) -> None:
+    """Decode attention over contexts whose first dev_packed_lens[s] tokens are
+    in 4-bit blocks (dev_table4) and whose others are in bf16 blocks
+    (dev_table); k_new and v_new may be None."""
+    _call("paged_decode_attn_q4", pool, layout, q4_layout, _addr(q), _addr(k_new), _addr(v_new), _addr(out),
+          _addr(dev_table), _addr(dev_ctx_lens), max_blocks, _addr(dev_table4), _addr(dev_packed_lens), max_blocks4, S,
+          Hq, scale, _addr(workspace), ws_bytes, _stream(stream))
 
 
 def kv_prompt_workspace_bytes(pool, layout: int, S: int, Hq: int, T: int, max_q: int, max_blocks: int, window: int,
@@ -717,6 +785,14 @@ class SeqTab:
         reference, a partial last one as its own copy on `stream`."""
         a = _i32(dsts)
         _check("kv_seq_fork", lib().kv_seq_fork(self.handle, int(src), int(a.size), a.ctypes.data, _stream(stream)))
+
+    def pack(self, packed: "SeqTab", slots, keep: int, stream=None) -> int:
+        """Move each slot's full blocks but those that its last `keep` tokens
+        reach into 4-bit blocks of the table `packed`; returns how many."""
+        a, n = _i32(slots), ctypes.c_int32(0)
+        _check("kv_seq_pack", lib().kv_seq_pack(self.handle, packed.handle, int(a.size), a.ctypes.data, int(keep),
+                                                _stream(stream), ctypes.byref(n)))
+        return int(n.value)
 
     def replace(self, slots, reserve_tokens, lens) -> np.ndarray:
         """Release each listed slot, then reserve and set the length of its
