@@ -14,7 +14,7 @@ bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 size_t q4_ws_layout(int S, int Hkv, int G, int D, int P, size_t *part_off)
 {
     *part_off = ((size_t)S * Hkv * sizeof(int2) + 255) / 256 * 256;
-    return *part_off + ((size_t)S * Hkv + (size_t)P * kvp::kQ4Warps) * (size_t)((G * D + 2 * G + 3) / 4 * 4) * 4;
+    return *part_off + ((size_t)S * Hkv + (size_t)P) * (size_t)kvp::q4_record_floats(D, G) * 4;
 }
 
 int q4_shape(const kv_pool *p, int q4_layout, int S, int Hq, int max_blocks, int *G, int *D)
@@ -27,8 +27,10 @@ int q4_shape(const kv_pool *p, int q4_layout, int S, int Hq, int max_blocks, int
     *G = Hq / L.num_kv_heads;
     *D = kvp_head_dim(L);
     if (!(*G == 1 || *G == 2 || *G == 4 || *G == 5 || *G == 8)) return KV_ERR_UNSUPPORTED;
-    // token and run numbers, and a run's cost, are 32-bit on the device
-    if ((int64_t)max_blocks * p->desc.block_size / kQ4Tile * kvp::kBf16Cost >= INT32_MAX) return KV_ERR_INVALID_ARG;
+    // token and run numbers, and a sequence's cost, are 32-bit on the device
+    if ((int64_t)max_blocks * p->desc.block_size >= INT32_MAX - kQ4Tile) return KV_ERR_INVALID_ARG;
+    const int64_t tiles = ((int64_t)max_blocks * p->desc.block_size + kQ4Tile - 1) / kQ4Tile;
+    if (tiles * L.num_kv_heads * kvp::kBf16Cost >= INT32_MAX) return KV_ERR_INVALID_ARG;
     if ((int64_t)S * L.num_kv_heads >= INT32_MAX) return KV_ERR_INVALID_ARG;
     return KV_OK;
 }

@@ -11,7 +11,7 @@ template <int D, int G>
 int q4_combine(const Q4Args &a, int sm_count, const cudaLaunchConfig_t &cfg)
 {
     const CombineArgs c{a.out, a.ws_run, a.ws_part, a.S, a.Hkv, nullptr, nullptr, 0};
-    const double per_run = (double)a.P * kQ4Warps / std::max(1, a.S * a.Hkv) + 1.0;
+    const double per_run = (double)a.P / std::max(1, a.S * a.Hkv) + 1.0;
     return combine_run<D, G, kRecCtas>(c, per_run, sm_count, cfg);
 }
 
@@ -19,12 +19,12 @@ template <int D>
 int q4_attn_run(int G, const Q4Args *args, int sm_count, cudaStream_t st, bool launch, int *P_out)
 {
     auto fn = q4_attn_kernel<D>;
-    const size_t smem = q4_smem_bytes<D>();
+    const size_t smem = q4_smem_bytes<D>(G);
     static DeviceFlags attr_set;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return KV_ERR_CUDA;
     if (!attr_set.has(dev)) {
-        if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+        if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)q4_smem_bytes<D>(8)) != cudaSuccess)
             return KV_ERR_CUDA;
         attr_set.set(dev);
     }

@@ -5,8 +5,8 @@
 // each (d columns, NG = d / 64 groups of 64):
 //     8 d    K codes
 //     8 d    V codes
-//     64 NG  K parameters, [16 tokens][NG] of (s, z) bf16 pairs, s in the low half
-//     64 NG  V parameters, the same
+//     128 NG parameters, [16 tokens][K, V][NG] of (s, z) bf16 pairs, s in the
+//            low half
 // so that one copy of a tile brings all that a warp needs of 16 tokens, and each
 // value lies where the lane that multiplies it reads it: with lane = 4 g + t (g
 // in 0..7, t in 0..3),

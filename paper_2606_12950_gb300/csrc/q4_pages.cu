@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_blocks_kernel(const __grid_
             *reinterpret_cast<uint4 *>(row) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
         else
             *reinterpret_cast<uint2 *>(row) = make_uint2(codes[0], codes[1]);
-        uint32_t *par = reinterpret_cast<uint32_t *>(dst + 16 * D) + (gid + 8 * r) * NG;
+        uint32_t *par = reinterpret_cast<uint32_t *>(dst + 16 * D) + (gid + 8 * r) * 2 * NG;
         if (tig == r) {
 #pragma unroll
             for (int c = 0; c < NG; ++c) par[c] = params[c];
@@ -169,8 +169,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_blocks_kernel(const __grid_
             }
             const Group g = group_of(mn, mx);
             if (gid == r)
-                *(reinterpret_cast<uint32_t *>(dst + 16 * D + 64 * NG) + (2 * tig + (r & 1) + 4 * (r & 2)) * NG + c) =
-                    g.word;
+                *(reinterpret_cast<uint32_t *>(dst + 16 * D) + (2 * tig + (r & 1) + 4 * (r & 2)) * 2 * NG + NG + c) = g.word;
             // tokens a, a + 1, a + 8, a + 9: nibbles 0, 4, 2, 6 and those after
             const int nib = 4 * (r & 1) + (r & 2);
             const uint32_t *w = reinterpret_cast<const uint32_t *>(&v[r][c]);
@@ -214,7 +213,7 @@ __global__ void __launch_bounds__(kPackThreads) unpack_blocks_kernel(const __gri
             k[r][j + 1] = w.y;
         }
 #pragma unroll
-        for (int c = 0; c < NG; ++c) kp[r][c] = *(reinterpret_cast<const uint32_t *>(src + 16 * D) + (gid + 8 * r) * NG + c);
+        for (int c = 0; c < NG; ++c) kp[r][c] = *(reinterpret_cast<const uint32_t *>(src + 16 * D) + (gid + 8 * r) * 2 * NG + c);
     }
 #pragma unroll
     for (int c = 0; c < NG; ++c) {
@@ -225,8 +224,8 @@ __global__ void __launch_bounds__(kPackThreads) unpack_blocks_kernel(const __gri
         v[c][3] = w.w;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            vp[r][c] = *(reinterpret_cast<const uint32_t *>(src + 16 * D + 64 * NG) +
-                         (2 * tig + (r & 1) + 4 * (r & 2)) * NG + c);
+            vp[r][c] = *(reinterpret_cast<const uint32_t *>(src + 16 * D) +
+                         (2 * tig + (r & 1) + 4 * (r & 2)) * 2 * NG + NG + c);
     }
 #pragma unroll
     for (int r = 0; r < 2; ++r)

@@ -51,8 +51,7 @@ def parse_block(raw, Hkv, bs, d):
                     for i, (tok, col) in enumerate(place):
                         codes[1, :, :, 2 * lane + tok, 64 * c + 8 * g + 2 * m + col] = (v[:, :, c, g, lane, m] >> (4 * i)) & 15
     for kv in (0, 1):
-        at = 16 * d + kv * 64 * NG
-        w = t[:, :, at : at + 64 * NG].copy().view(np.uint32).reshape(Hkv, -1, 16, NG)
+        w = t[:, :, 16 * d :].copy().view(np.uint32).reshape(Hkv, -1, 16, 2, NG)[:, :, :, kv]
         par[kv, ..., 0] = (w << 16).view(np.float32)
         par[kv, ..., 1] = (w & 0xFFFF0000).view(np.float32)
     shape = (2, Hkv, bs, NG)
