@@ -24,9 +24,9 @@
 // it is in 4 bits and 32 in bf16 (its bytes).  The batch's tiles, in order, are cut
 // into parts of equal cost, one a CTA, and those into equal ones, one a warp.  A
 // run inside a CTA leaves its output, others a record a CTA for the combine (the
-// warps' states merged in shared memory).  Each warp streams its 4-bit tiles
-// through its own ring of shared-memory stages (a bulk copy a tile) and reads its
-// bf16 tiles straight into registers.
+// warps' states merged in shared memory).  Each warp streams its tiles
+// through its own ring of shared-memory stages, a bulk copy each (of K or V, where
+// they are in bf16).
 #pragma once
 
 #include <cuda_fp16.h>
@@ -36,13 +36,13 @@
 
 namespace kvp {
 
-constexpr int kQ4Warps = 8;
+constexpr int kQ4Warps = 16;
 constexpr int kQ4Threads = kQ4Warps * 32;
 constexpr int kQ4Stages = 2;
 template <int D>
 constexpr int kQ4Unit = D == 64 ? 4 : 2;  // tiles of a stage: 4608 bytes either way
-constexpr int kQ4Cost = 9, kBf16Cost = 32;
-constexpr int kQ4MinPart = 36;            // a part's least cost: more than any tile's, so that each has one
+constexpr int kQ4Cost = 9, kBf16Cost = 32, kRunCost = 24;
+constexpr int kQ4MinPart = 64;            // a part's least cost: more than any tile's, so that each has one
 
 struct Q4Args {
     const uint16_t *q;
@@ -72,7 +72,7 @@ template <int D>
 inline size_t q4_smem_bytes(int G)
 {
     return 128 + (size_t)kQ4Warps * (kQ4Stages * (kQ4Unit<D> * kQ4TileBytes<D> + 8) + q4_record_floats(D, G) * 4 + 16) +
-           (kQ4Threads + 1) * sizeof(int64_t);
+           (kQ4Threads + kQ4Warps) * sizeof(int64_t);
 }
 
 // A sequence's lengths, clamped to what the tables can hold.
@@ -81,7 +81,12 @@ struct Q4Seq {
     bool append;     // a new row can be appended
     __device__ int32_t tiles4() const { return p >> 4; }
     __device__ int32_t tiles() const { return (p >> 4) + ((n - p + 15) >> 4); }
-    __device__ int32_t cost() const { return kQ4Cost * (p >> 4) + kBf16Cost * ((n - p + 15) >> 4); }
+    // of a run, and before its tile i
+    __device__ int32_t cost() const { return n > 0 ? cost_to(tiles()) : 0; }
+    __device__ int32_t cost_to(int32_t i) const
+    {
+        return i > 0 ? kRunCost + kQ4Cost * min(i, p >> 4) + kBf16Cost * max(0, i - (p >> 4)) : 0;
+    }
 };
 
 __device__ __forceinline__ Q4Seq q4_seq(const Q4Args &a, int s)
@@ -95,12 +100,16 @@ __device__ __forceinline__ Q4Seq q4_seq(const Q4Args &a, int s)
     return q;
 }
 
-// the tile of a run at cost position x or the first one after it
+// the first tile of a run with no less than cost x before it
 __device__ __forceinline__ int32_t q4_tile_at(const Q4Seq &q, int32_t x)
 {
+    if (x <= 0) return 0;
+    if (x >= q.cost()) return q.tiles();
+    x -= kRunCost;
     const int32_t c4 = kQ4Cost * q.tiles4();
-    return x <= c4 ? (int32_t)((uint32_t)(x + kQ4Cost - 1) / (uint32_t)kQ4Cost)
-                   : q.tiles4() + (x - c4 + kBf16Cost - 1) / kBf16Cost;
+    const int32_t i = x <= c4 ? (int32_t)((uint32_t)(max(x, 0) + kQ4Cost - 1) / (uint32_t)kQ4Cost)
+                              : q.tiles4() + (x - c4 + kBf16Cost - 1) / kBf16Cost;
+    return max(1, i);
 }
 
 // D(16x8, f32) += A(16x16, f16, row) * B(16x8, f16, col)
@@ -368,38 +377,46 @@ struct Q4State {
         }
     }
 
-    // a tile of `valid` tokens in bf16: rows k[r], r = g and g + 8, and v[r], r = 2 t,
-    // 2 t + 1, 2 t + 8, 2 t + 9 (null: none); qrow as in begin
-    __device__ __forceinline__ void tile16(const uint16_t *const (&k)[2], const uint16_t *const (&v)[4],
-                                           const uint16_t *qrow, int G, float qk_scale, int lane)
+    // A tile of bf16 rows: its K's scores (rows, their first of this lane's, and
+    // the tile's tokens with a weight, a bit each), then its V.  qrow as in begin;
+    // where token `fresh` is one of the tile's, its row is k_new or v_new.
+    __device__ __forceinline__ void scores16(float (&y)[4], const uint16_t *rows, int valid, int fresh, const uint16_t *k_new,
+                                             const uint16_t *qrow, int G, float qk_scale, int lane)
     {
         const int gid = lane >> 2, tig = lane & 3;
-        uint4 kw[2][NW], vw[4][NG];
         const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-        for (int j = 0; j < NW; ++j)
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-                kw[r][j] = k[r] ? *reinterpret_cast<const uint4 *>(k[r] + 64 * (j >> 1) + 32 * (j & 1) + 8 * tig) : none;
-#pragma unroll
-        for (int c = 0; c < NG; ++c)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                vw[r][c] = v[r] ? *reinterpret_cast<const uint4 *>(v[r] + 64 * c + 8 * gid) : none;
+        const uint16_t *k0 = gid == fresh ? k_new : rows + gid * D, *k1 = gid + 8 == fresh ? k_new : rows + (gid + 8) * D;
         float x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NW; ++j) {
-            const uint4 q = gid < G ? *reinterpret_cast<const uint4 *>(qrow + gid * D + 64 * (j >> 1) + 32 * (j & 1) + 8 * tig)
-                                    : none;
-            mma_bf16_16816(x, kw[0][j].x, kw[1][j].x, kw[0][j].y, kw[1][j].y, q.x, q.y);
-            mma_bf16_16816(x, kw[0][j].z, kw[1][j].z, kw[0][j].w, kw[1][j].w, q.z, q.w);
+            const int at = 64 * (j >> 1) + 32 * (j & 1) + 8 * tig;
+            const uint4 a = *reinterpret_cast<const uint4 *>(k0 + at), b = *reinterpret_cast<const uint4 *>(k1 + at);
+            const uint4 q = gid < G ? *reinterpret_cast<const uint4 *>(qrow + gid * D + at) : none;
+            mma_bf16_16816(x, a.x, b.x, a.y, b.y, q.x, q.y);
+            mma_bf16_16816(x, a.z, b.z, a.w, b.w, q.z, q.w);
         }
         const float no = -INFINITY;
-        const float ya = k[0] ? x[0] * qk_scale : no, yb = k[0] ? x[1] * qk_scale : no;
-        const float yc = k[1] ? x[2] * qk_scale : no, yd = k[1] ? x[3] * qk_scale : no;
-        raise(fmaxf(ya, yc), fmaxf(yb, yd));
-        const float p0 = fast_exp2(ya - m[0]), p1 = fast_exp2(yb - m[1]);
-        const float p2 = fast_exp2(yc - m[0]), p3 = fast_exp2(yd - m[1]);
+        y[0] = gid < valid ? x[0] * qk_scale : no;
+        y[1] = gid < valid ? x[1] * qk_scale : no;
+        y[2] = gid + 8 < valid ? x[2] * qk_scale : no;
+        y[3] = gid + 8 < valid ? x[3] * qk_scale : no;
+        raise(fmaxf(y[0], y[2]), fmaxf(y[1], y[3]));
+    }
+    __device__ __forceinline__ void values16(const float (&y)[4], const uint16_t *rows, int valid, int fresh,
+                                             const uint16_t *v_new, int lane)
+    {
+        const int gid = lane >> 2, tig = lane & 3;
+        uint4 vw[4][NG];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {  // (what lies past the context may be anything)
+            const int t = 2 * tig + (r & 1) + 4 * (r & 2);
+            const uint16_t *v = t == fresh ? v_new : rows + t * D;
+#pragma unroll
+            for (int c = 0; c < NG; ++c)
+                vw[r][c] = t < valid ? *reinterpret_cast<const uint4 *>(v + 64 * c + 8 * gid) : make_uint4(0u, 0u, 0u, 0u);
+        }
+        const float p0 = fast_exp2(y[0] - m[0]), p1 = fast_exp2(y[1] - m[1]);
+        const float p2 = fast_exp2(y[2] - m[0]), p3 = fast_exp2(y[3] - m[1]);
         l[0] += p0 + p2;
         l[1] += p1 + p3;
         // the accumulators' units: weights times 2^-24, odd columns times 16
@@ -471,16 +488,19 @@ struct Q4State {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kQ4Threads, 2) q4_attn_kernel(const __grid_constant__ Q4Args a)
+__global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_constant__ Q4Args a)
 {
     constexpr int TILE = kQ4TileBytes<D>, U = kQ4Unit<D>, STAGE = U * TILE;
+    constexpr int TILE16 = kQ4Tile * 2 * D;  // K or V of a tile in bf16
+    static_assert(TILE16 <= STAGE, "a unit is a stage");
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
     const int G = a.G, MF = q4_record_floats(D, G);
     float *recs = reinterpret_cast<float *>(smem + (size_t)kQ4Warps * kQ4Stages * STAGE);  // [warps][MF]
     int4 *chains = reinterpret_cast<int4 *>(recs + kQ4Warps * MF);                          // [warps]
     uint64_t *bars = reinterpret_cast<uint64_t *>(chains + kQ4Warps);
-    int64_t *base = reinterpret_cast<int64_t *>(bars + kQ4Warps * kQ4Stages);  // [threads + 1] costs before a thread's sequences
+    // costs before a thread's sequences, from its warp's on, and of a warp's
+    int64_t *base = reinterpret_cast<int64_t *>(bars + kQ4Warps * kQ4Stages), *tops = base + kQ4Threads;
     const int tid = threadIdx.x, lane = tid & 31;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const int bid = blockIdx.x, S = a.S;
@@ -515,25 +535,28 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_attn_kernel(const __grid_con
             const int64_t v = __shfl_up_sync(0xffffffffu, incl, off);
             if (lane >= off) incl += v;
         }
-        __shared__ int64_t tops[kQ4Warps];
+        base[tid] = incl - sum;
         if (lane == 31) tops[warp] = incl;
         __syncthreads();
-        int64_t before = 0;
-        for (int w = 0; w < warp; ++w) before += tops[w];
-        base[tid] = before + incl - sum;
-        if (tid == kQ4Threads - 1) base[kQ4Threads] = before + incl;
-        __syncthreads();
+    }
+    int64_t upto = lane < kQ4Warps ? tops[lane] : 0;  // the cost up to the end of warp `lane`'s sequences
+#pragma unroll
+    for (int off = 1; off < kQ4Warps; off <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, upto, off);
+        if (lane >= off) upto += v;
     }
     // Equal shares of the cost: CTAs, and in a CTA its warps; a warp's is at least
-    // kQ4MinPart.
-    const int64_t W = base[kQ4Threads];
+    // kQ4MinPart.  (64-bit divisions take 0.5 us each: there is one where W needs it.)
+    const int64_t W = __shfl_sync(0xffffffffu, upto, kQ4Warps - 1);
     const int NC = (int)min((int64_t)a.P, (W / kQ4MinPart + kQ4Warps - 1) / kQ4Warps + (W < kQ4MinPart));
     if (bid >= NC || W == 0) return;
-    auto share = [](int64_t n, int i, int parts) { return i * (n / parts) + i * (n % parts) / parts; };
-    const int64_t c0 = share(W, bid, NC);
-    const int32_t cn = (int32_t)(share(W, bid + 1, NC) - c0);  // this CTA's
+    const int64_t wq = (W >> 32) == 0 ? (int64_t)((uint32_t)W / (uint32_t)NC) : W / NC;
+    const uint32_t wr = (uint32_t)(W - wq * NC);
+    const int64_t c0 = bid * wq + (uint32_t)bid * wr / (uint32_t)NC;
+    const int32_t cn = (int32_t)(wq + (uint32_t)(bid + 1) * wr / (uint32_t)NC - (uint32_t)bid * wr / (uint32_t)NC);  // this CTA's
     const int nw = max(1, min(kQ4Warps, cn / kQ4MinPart));
-    auto warp_begin = [&](int w) { return w * (cn / nw) + w * (cn % nw) / nw; };
+    const int32_t nq = (int32_t)((uint32_t)cn / (uint32_t)nw), nr = cn - nq * nw;
+    auto warp_begin = [&](int w) { return w * nq + (int32_t)((uint32_t)(w * nr) / (uint32_t)nw); };
 
     struct Run {
         Q4Seq q;
@@ -544,10 +567,7 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_attn_kernel(const __grid_con
     if (warp < nw) {
         const int32_t w0 = warp_begin(warp), w1 = warp_begin(warp + 1);
         // a run's tiles from cost x on
-        auto tile_from = [&](const Run &r, int32_t x) {
-            x -= r.begin;
-            return x <= 0 ? 0 : x >= r.q.cost() ? r.q.tiles() : min(r.q.tiles(), q4_tile_at(r.q, x));
-        };
+        auto tile_from = [&](const Run &r, int32_t x) { return q4_tile_at(r.q, x - r.begin); };
         // the run after r that has tiles in this part; false if there is none
         auto next = [&](Run &r) {
             r.begin += r.q.cost();
@@ -566,13 +586,14 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_attn_kernel(const __grid_con
         // ---- the run at the part's start ----
         Run run;
         {
-            int lo = 0, hi = kQ4Threads;  // the last thread whose sequences start at or before w0, with any cost
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (base[mid] <= c0 + w0) lo = mid; else hi = mid;
-            }
-            int64_t x = c0 + w0 - base[lo];  // cost from the sequence's start on
-            run.s = lo * per;
+            // the last thread whose sequences start at or before w0 (with any cost)
+            int64_t x = c0 + w0;
+            const int k = __popc(__ballot_sync(0xffffffffu, lane < kQ4Warps && upto <= x));  // warps before
+            const int64_t before = __shfl_sync(0xffffffffu, upto, max(k - 1, 0));
+            x -= k > 0 ? before : 0;
+            const int t = 31 - __clz((int)__ballot_sync(0xffffffffu, base[k * 32 + lane] <= x));
+            x -= base[k * 32 + t];  // cost from the sequence's start on
+            run.s = (k * 32 + t) * per;
             run.q = q4_seq(a, run.s);
             while (x >= (int64_t)run.q.cost() * a.Hkv) {
                 x -= (int64_t)run.q.cost() * a.Hkv;
@@ -586,46 +607,53 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_attn_kernel(const __grid_con
         // (the part may start past this run's last tile; it has one of the next then)
         bool go = run.i0 < run.i1 || next(run);
 
-        // ---- the ring: this warp's 4-bit tiles, piece after piece ----
+        // ---- the ring: units of this warp's tiles, piece after piece.  A unit is up
+        // to kQ4Unit tiles in 4 bits, or the K or the V of one in bf16 ----
         uint8_t *ring = smem + (size_t)warp * kQ4Stages * STAGE;
         const uint32_t ring_addr = smem_u32(ring), bar0 = smem_u32(&bars[warp * kQ4Stages]);
         const uint64_t policy = l2_policy_evict_first();
         const int per_block = a.bs / kQ4Tile;
         Run ahead = run;
         bool more = go;          // `ahead` is a run of this part
-        int32_t at = run.i0, end = 0;  // its next tile to ask for, and the tile past its last in 4 bits
-        int32_t from = 0;        // tile of lane 0's address
+        int32_t at = run.i0;     // its next tile to ask for
+        int32_t from = at - 32;  // tile of lane 0's address
         const uint8_t *src = nullptr;  // of tile from + lane
         uint32_t good = 0;       // lanes with one
+        bool v_next = false;     // a bf16 tile's V is next
         uint32_t issue_stage = 0;
-        if (more) end = min(ahead.i1, ahead.q.tiles4());
-        bool fresh = true;
         auto issue = [&]() {     // the next unit, if there is one
-            while (at >= end) {
-                if (!more) return;
+            if (!more) return;
+            if (at >= ahead.i1) {
                 more = next(ahead);
                 if (!more) return;
-                at = 0;
-                end = min(ahead.i1, ahead.q.tiles4());
-                fresh = true;
+                at = ahead.i0;
+                from = at - 32;
             }
-            if (fresh || at + U > from + 32) {  // the next 32 tiles' places
-                fresh = false;
+            const int32_t tiles4 = ahead.q.tiles4();
+            const bool packed = at < tiles4;
+            const int32_t end = packed ? min(at + U, min(ahead.i1, tiles4)) : at + 1;
+            if (end > from + 32) {  // the next 32 tiles' places
                 from = at;
-                const int32_t i = at + lane, b = (int32_t)((uint32_t)i / (uint32_t)per_block);
-                const int32_t id = i < end ? a.table4[(int64_t)ahead.s * a.max_blocks4 + b] : -1;
-                const bool ok = id >= 0 && (int64_t)id + a.pages_per_block4 <= a.pool_pages;
-                if (i < end && !ok) report(a.err, KV_ERR_DEVICE_BOUNDS);
-                src = a.pool + (int64_t)id * a.page_bytes + ((int64_t)ahead.g * per_block + (i - b * per_block)) * TILE;
+                const int32_t i = at + lane, b = (int32_t)((uint32_t)i / (uint32_t)per_block), t = i - b * per_block;
+                const bool in4 = i < tiles4;
+                int32_t id = -1;
+                if (i < ahead.i1)
+                    id = in4 ? a.table4[(int64_t)ahead.s * a.max_blocks4 + b] : a.table[(int64_t)ahead.s * a.max_blocks + b];
+                const bool ok = id >= 0 && (int64_t)id + (in4 ? a.pages_per_block4 : a.pages_per_block) <= a.pool_pages;
+                if (i < ahead.i1 && !ok) report(a.err, KV_ERR_DEVICE_BOUNDS);
+                src = a.pool + (int64_t)id * a.page_bytes + ((int64_t)ahead.g * per_block + t) * (in4 ? TILE : TILE16);
                 good = __ballot_sync(0xffffffffu, ok);
             }
-            const int off = at - from;
+            const int off = at - from, n = end - at;
             const uint32_t bar = bar0 + issue_stage * 8;
-            if (lane == off) mbar_arrive_expect_tx(bar, __popc((good >> off) & ((1u << U) - 1u)) * TILE);
+            const uint32_t bytes = packed ? TILE : TILE16;
+            if (lane == off) mbar_arrive_expect_tx(bar, __popc((good >> off) & ((1u << n) - 1u)) * bytes);
             __syncwarp();
-            if ((uint32_t)(lane - off) < (uint32_t)U && ((good >> lane) & 1u))
-                bulk_load(ring_addr + issue_stage * STAGE + (lane - off) * TILE, src, TILE, bar, policy);
-            at += U;
+            if ((uint32_t)(lane - off) < (uint32_t)n && ((good >> lane) & 1u))
+                bulk_load(ring_addr + issue_stage * STAGE + (lane - off) * TILE,
+                          src + (v_next ? (int64_t)a.Hkv * per_block * TILE16 : 0), bytes, bar, policy);
+            if (packed || v_next) at = end;
+            v_next = !packed && !v_next;
             issue_stage = issue_stage + 1 == kQ4Stages ? 0 : issue_stage + 1;
         };
         for (int st = 0; st < kQ4Stages; ++st) issue();
@@ -639,12 +667,7 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_attn_kernel(const __grid_con
             Q4State<D> st;
             st.begin(qrow, G, a.qk_scale, lane);
             const int32_t end4 = min(run.i1, q.tiles4());
-            for (int32_t i = run.i0; i < end4; i += U) {
-                wait_phase(bar0 + stage * 8, parity, a.err, dead);
-                if (i + U <= end4)
-                    st.template unit4<true>(ring + stage * STAGE, U, lane);
-                else
-                    st.template unit4<false>(ring + stage * STAGE, end4 - i, lane);
+            auto unit_done = [&]() {
                 if (++stage == kQ4Stages) {
                     stage = 0;
                     parity ^= 1u;
@@ -653,38 +676,40 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_attn_kernel(const __grid_con
                 fence_proxy_async_smem();
                 __syncwarp();
                 issue();
+            };
+            for (int32_t i = run.i0; i < end4; i += U) {
+                wait_phase(bar0 + stage * 8, parity, a.err, dead);
+                if (i + U <= end4)
+                    st.template unit4<true>(ring + stage * STAGE, U, lane);
+                else
+                    st.template unit4<false>(ring + stage * STAGE, end4 - i, lane);
+                unit_done();
             }
             for (int32_t i = max(run.i0, q.tiles4()); i < run.i1; ++i) {
-                const int32_t tok0 = q.p + (i - q.tiles4()) * 16;
-                const int gid = lane >> 2, tig = lane & 3;
-                auto row = [&](int rr, int kv) -> const uint16_t * {
-                    const int32_t j = tok0 + rr;
-                    if (j >= q.n) return nullptr;
-                    if (a.k_new && q.append && j == q.n - 1) return (kv ? a.v_new : a.k_new) + (int64_t)r * D;
-                    const int32_t id = a.table[(int64_t)run.s * a.max_blocks + j / a.bs];
-                    if (id < 0 || (int64_t)id + a.pages_per_block > a.pool_pages) {
-                        report(a.err, KV_ERR_DEVICE_BOUNDS);
-                        return nullptr;
-                    }
-                    return reinterpret_cast<const uint16_t *>(a.pool + (int64_t)id * a.page_bytes) +
-                           ((int64_t)(kv * a.Hkv + run.g) * a.bs + j % a.bs) * D;
-                };
-                const uint16_t *const k[2] = {row(gid, 0), row(gid + 8, 0)};
-                const uint16_t *const v[4] = {row(2 * tig, 1), row(2 * tig + 1, 1), row(2 * tig + 8, 1), row(2 * tig + 9, 1)};
-                st.tile16(k, v, qrow, G, a.qk_scale, lane);
-                if (a.k_new && q.append && tok0 + 16 >= q.n && lane < D / 4) {  // the new row's place
-                    const int32_t j = q.n - 1;
-                    const int32_t id = a.table[(int64_t)run.s * a.max_blocks + j / a.bs];
+                const int32_t tok0 = i * kQ4Tile;
+                const int fresh = a.k_new && q.append ? q.n - 1 - tok0 : -1, valid = q.n - tok0;
+                float y[4];
+                wait_phase(bar0 + stage * 8, parity, a.err, dead);
+                st.scores16(y, reinterpret_cast<const uint16_t *>(ring + stage * STAGE), valid, fresh, a.k_new + (int64_t)r * D,
+                            qrow, G, a.qk_scale, lane);
+                unit_done();
+                wait_phase(bar0 + stage * 8, parity, a.err, dead);
+                st.values16(y, reinterpret_cast<const uint16_t *>(ring + stage * STAGE), valid, fresh, a.v_new + (int64_t)r * D,
+                            lane);
+                if ((uint32_t)fresh < (uint32_t)kQ4Tile && lane < D / 4) {
+                    // the new row's place: this warp's copies of the tile have landed, and
+                    // no other unit holds that row
+                    const int32_t j = q.n - 1, b = j / a.bs;
+                    const int32_t id = a.table[(int64_t)run.s * a.max_blocks + b];
                     if (id >= 0 && (int64_t)id + a.pages_per_block <= a.pool_pages) {
                         const int kv = lane / (D / 8), c = lane % (D / 8);
                         uint16_t *dst = reinterpret_cast<uint16_t *>(a.pool + (int64_t)id * a.page_bytes) +
-                                        ((int64_t)(kv * a.Hkv + run.g) * a.bs + j % a.bs) * D;
+                                        ((int64_t)(kv * a.Hkv + run.g) * a.bs + (j - b * a.bs)) * D;
                         *reinterpret_cast<uint4 *>(dst + c * 8) =
                             *reinterpret_cast<const uint4 *>((kv ? a.v_new : a.k_new) + (int64_t)r * D + c * 8);
-                    } else {
-                        report(a.err, KV_ERR_DEVICE_BOUNDS);
                     }
                 }
+                unit_done();
             }
             // ---- end of a piece: t0, t1 are the CTA's tiles of the run ----
             const int32_t t0 = tile_from(run, 0), t1 = tile_from(run, cn);
@@ -699,7 +724,7 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_attn_kernel(const __grid_con
                 st.store(nullptr, recs + warp * MF, true, G, lane);
             } else {  // goes on in the next warp: the last piece here, so the ring is free
                 st.store(nullptr, reinterpret_cast<float *>(ring), true, G, lane);
-                const int32_t last_tile = run.begin + min(t1 - 1, q.tiles4()) * kQ4Cost + max(0, t1 - 1 - q.tiles4()) * kBf16Cost;
+                const int32_t last_tile = run.begin + q.cost_to(t1 - 1);
                 int e = warp;
                 while (e + 1 < nw && warp_begin(e + 1) <= last_tile) ++e;
                 if (lane == 0) chains[warp] = make_int4(r, e - warp, (first ? 1 : 0) | (last ? 2 : 0), split ? 1 : 0);
@@ -715,22 +740,23 @@ __global__ void __launch_bounds__(kQ4Threads, 2) q4_attn_kernel(const __grid_con
         const int w = i / cols, c = i - w * cols, h = c * 4 / D;
         const int4 ch = chains[w];
         if (ch.x < 0) continue;
-        float mv[kQ4Warps], lv[kQ4Warps];
-        float4 ov[kQ4Warps];
-#pragma unroll
-        for (int k = 0; k < kQ4Warps; ++k) {
-            mv[k] = -INFINITY;
-            if (k <= ch.y) {
-                const float *rec = k == 0 ? reinterpret_cast<const float *>(smem + (size_t)w * kQ4Stages * STAGE)
-                                          : recs + (w + k) * MF;
-                mv[k] = rec[G * D + h];
-                lv[k] = rec[G * D + G + h];
-                ov[k] = *reinterpret_cast<const float4 *>(rec + c * 4);
-            }
+        auto rec = [&](int k) {
+            return k == 0 ? reinterpret_cast<const float *>(smem + (size_t)w * kQ4Stages * STAGE) : recs + (w + k) * MF;
+        };
+        float M = rec(0)[G * D + h], L = 0.f;
+        for (int k = 1; k <= ch.y; ++k) M = fmaxf(M, rec(k)[G * D + h]);
+        float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int k = 0; k <= ch.y; ++k) {
+            const float *r = rec(k);
+            const float e = fast_exp2(r[G * D + h] - M);
+            const float4 o = *reinterpret_cast<const float4 *>(r + c * 4);
+            L = __fmaf_rn(r[G * D + G + h], e, L);
+            O.x = __fmaf_rn(o.x, e, O.x);
+            O.y = __fmaf_rn(o.y, e, O.y);
+            O.z = __fmaf_rn(o.z, e, O.z);
+            O.w = __fmaf_rn(o.w, e, O.w);
         }
-        float M, L;
-        float4 O;
-        merge_group(M, L, O, mv, lv, ov);
         if (ch.w == 0) {
             store_column(a.out + (int64_t)ch.x * (G * D) + c * 4, O, L);
         } else {
