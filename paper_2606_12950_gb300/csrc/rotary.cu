@@ -26,14 +26,16 @@
 
 #include "pool_internal.h"
 #include "ptx.cuh"
+#include "rotary_impl.cuh"
 #include "stream_order.h"
 
 namespace {
 
+using namespace kvp;
+
 constexpr int kRotThreads = 256;
 constexpr int kRotShared = 3;     // CTAs an SM holds of those that tokens share
 constexpr int kMaxHeadDim = 512;  // kv_pool_create's limit
-constexpr int kMaxNormDim = 256;
 
 struct RotaryArgs {
     const uint16_t *q, *k, *v;  // rows of token t at t * stride
@@ -51,88 +53,33 @@ struct RotaryArgs {
     int32_t pages_per_block, max_blocks;
     int32_t S, Hq, Hkv, D, bs, rot;
     int32_t items;              // of a row (see rotary_kernel)
-    // norms of the heads (NORM kernels)
-    const uint16_t *q_weight, *k_weight;  // [D], or null: not normed
-    float eps, offset;
-    int32_t lanes;              // threads of a row: the items, or with norms the power of two that holds them
     int32_t run, longer;        // tokens of a group; the first `longer` groups have one more
 };
 
-// largest s with starts[s] <= t (starts ascending, starts[0] <= t): N probes a
-// round trip by the N lanes that share t; the whole warp, converged
-template <int N>
-__device__ __forceinline__ int seq_of_token(const int32_t *starts, int S, int t, int lane)
-{
-    const int own = lane & (N - 1);
-    int lo = 0, n = S;  // the answer is in [lo, lo + n)
-    while (__any_sync(0xffffffffu, n > 1)) {
-        const int step = (n + N - 1) / N;
-        const int i = lo + own * step;
-        const unsigned le = __ballot_sync(0xffffffffu, own * step < n && starts[i] <= t) >> (lane - own);
-        const int k = 31 - __clz((int)((N < 32 ? le & ((1u << (N & 31)) - 1u) : le) | 1u));
-        n = min(step, n - k * step);
-        lo += k * step;
-    }
-    return lo;
-}
-
-__device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-__device__ __forceinline__ uint32_t pack2(float lo, float hi)
-{
-    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<uint32_t *>(&v);
-}
-
-__device__ __forceinline__ float2 unpack2(uint32_t w) { return make_float2(lo_f(w), hi_f(w)); }
-
-// Two pairs of pairs of the half layout (c, s: their cos and sin)
-__device__ __forceinline__ void turn2(float2 &u, float2 &v, float2 c, float2 s)
-{
-    const float2 ns = make_float2(-s.x, -s.y);
-    const float2 p = __ffma2_rn(u, c, __fmul2_rn(v, ns)), q = __ffma2_rn(v, c, __fmul2_rn(u, s));
-    u = p;
-    v = q;
-}
-// an adjacent pair
-__device__ __forceinline__ void turn1(float2 &u, float c, float s)
-{
-    u = __ffma2_rn(u, make_float2(c, c), __fmul2_rn(make_float2(u.y, u.x), make_float2(-s, s)));
-}
-
 // Two chunks of the half layout, columns 8c .. of either half (c, s: the cos and
 // sin of the pairs, two at a time)
-__device__ __forceinline__ void turn_halves(float2 (&u)[4], float2 (&v)[4], const float2 (&c)[4], const float2 (&s)[4])
-{
-#pragma unroll
-    for (int e = 0; e < 4; ++e) turn2(u[e], v[e], c[e], s[e]);
-}
 __device__ __forceinline__ void turn_halves(uint4 &a, uint4 &b, const float2 (&c)[4], const float2 (&s)[4])
 {
     uint32_t *x = reinterpret_cast<uint32_t *>(&a), *y = reinterpret_cast<uint32_t *>(&b);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        float2 u = unpack2(x[e]), v = unpack2(y[e]);
-        turn2(u, v, c[e], s[e]);
-        x[e] = pack2(u.x, u.y);
-        y[e] = pack2(v.x, v.y);
+        const float2 u = unpack2(x[e]), v = unpack2(y[e]), ns = make_float2(-s[e].x, -s[e].y);
+        const float2 p = __ffma2_rn(u, c[e], __fmul2_rn(v, ns)), q = __ffma2_rn(v, c[e], __fmul2_rn(u, s[e]));
+        x[e] = pack2(p.x, p.y);
+        y[e] = pack2(q.x, q.y);
     }
 }
 
 // a chunk of four adjacent pairs (c, s: the first four pairs' in c[0 .. 1], s[0 .. 1])
-__device__ __forceinline__ void turn_adjacent(float2 (&u)[4], const float2 (&c)[4], const float2 (&s)[4])
-{
-#pragma unroll
-    for (int e = 0; e < 4; ++e) turn1(u[e], e & 1 ? c[e / 2].y : c[e / 2].x, e & 1 ? s[e / 2].y : s[e / 2].x);
-}
 __device__ __forceinline__ void turn_adjacent(uint4 &a, const float2 (&c)[4], const float2 (&s)[4])
 {
     uint32_t *x = reinterpret_cast<uint32_t *>(&a);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        float2 u = unpack2(x[e]);
-        turn1(u, e & 1 ? c[e / 2].y : c[e / 2].x, e & 1 ? s[e / 2].y : s[e / 2].x);
-        x[e] = pack2(u.x, u.y);
+        const float ce = e & 1 ? c[e / 2].y : c[e / 2].x, se = e & 1 ? s[e / 2].y : s[e / 2].x;
+        const float2 u = unpack2(x[e]);
+        const float2 p = __ffma2_rn(u, make_float2(ce, ce), __fmul2_rn(make_float2(u.y, u.x), make_float2(-se, se)));
+        x[e] = pack2(p.x, p.y);
     }
 }
 
@@ -161,24 +108,18 @@ __device__ __forceinline__ void turn_adjacent(uint4 &a, const float2 (&c)[4], co
 // Pointers are not __restrict__: the kernel may be resident while the grid
 // before it still writes what it reads, and a const __restrict__ pointer may be
 // read through the non-coherent path, which the wait below does not order.
-//
-// NORM: each head of q and k is normed before it turns.  A row's threads are then
-// a power of two (those past its items hold no columns), which sum its squares by
-// shuffles; the weights lie in shared memory as fp32, with the offset.
-template <bool INTERLEAVED, int GROUP, bool NORM = false>
-constexpr int kRotBatch = NORM ? (INTERLEAVED ? 4 : 2) : GROUP == kRotThreads ? 4 : INTERLEAVED ? 6 : 3;
-template <bool INTERLEAVED, int GROUP, bool NORM = false>
-constexpr int kRotResident = !NORM && GROUP == kRotThreads && INTERLEAVED ? 5 : kRotShared;
+template <bool INTERLEAVED, int GROUP>
+constexpr int kRotBatch = GROUP == kRotThreads ? 4 : INTERLEAVED ? 6 : 3;
+template <bool INTERLEAVED, int GROUP>
+constexpr int kRotResident = GROUP == kRotThreads && INTERLEAVED ? 5 : kRotShared;
 
-template <bool INTERLEAVED, int GROUP, bool NORM>
-__global__ void __launch_bounds__(kRotThreads, kRotResident<INTERLEAVED, GROUP, NORM>)
-    rotary_kernel(const __grid_constant__ RotaryArgs a)
+template <bool INTERLEAVED, int GROUP>
+__global__ void __launch_bounds__(kRotThreads, kRotResident<INTERLEAVED, GROUP>) rotary_kernel(const __grid_constant__ RotaryArgs a)
 {
-    constexpr int PER = kRotThreads / GROUP, BATCH = kRotBatch<INTERLEAVED, GROUP, NORM>;
+    constexpr int PER = kRotThreads / GROUP, BATCH = kRotBatch<INTERLEAVED, GROUP>;
     constexpr int PAIRS = GROUP < 32 ? 8 * GROUP : kMaxHeadDim / 2;  // (no more, with an item of a row a thread)
     // times the magnitude; of a group's token, and of the one before it
     __shared__ __align__(16) float cosines[2][PER][PAIRS], sines[2][PER][PAIRS];
-    __shared__ __align__(16) float norms[2][NORM ? kMaxNormDim : 4];  // weights of q and of k, with the offset
     const int lane = threadIdx.x & 31, tid = threadIdx.x & (GROUP - 1), sub = threadIdx.x / GROUP;
     const int group = blockIdx.x * PER + sub;
     const int t0 = GROUP == kRotThreads ? blockIdx.x : group * a.run + min(group, a.longer);
@@ -187,14 +128,11 @@ __global__ void __launch_bounds__(kRotThreads, kRotResident<INTERLEAVED, GROUP, 
     const int turns_end = GROUP < 32 ? t0 + a.run + (a.longer > 0) : t_end;
     const int turned = INTERLEAVED ? a.rot / 8 : a.rot / 16;
     const int items = a.items;  // of a row: those that turn, then the others
-    const int lanes = NORM ? a.lanes : items;
-    const int step = GROUP / lanes;  // rows at a time
-    const int item = tid % lanes, r0 = tid / lanes;
-    const bool holds = !NORM || item < items;
+    const int step = GROUP / items;  // rows at a time
+    const int item = tid % items, r0 = tid / items;
     const bool turns = item < turned, pair = !INTERLEAVED && turns;
     const int at = turns ? item : item + a.rot / 8 - turned;  // the item's (first) chunk
-    const int q_rows = a.q ? a.Hq : 0, token_rows = q_rows + (a.k ? 2 * a.Hkv : 0);
-    const int all_rows = r0 < step && holds ? token_rows : 0;
+    const int q_rows = a.q ? a.Hq : 0, all_rows = r0 < step ? q_rows + (a.k ? 2 * a.Hkv : 0) : 0;
     int t = t0;
     auto load = [&](int r, uint4 &x, uint4 &y) {
         const int g = r - q_rows;
@@ -208,14 +146,6 @@ __global__ void __launch_bounds__(kRotThreads, kRotResident<INTERLEAVED, GROUP, 
     uint4 x[BATCH], y[BATCH];
     kvp::grid_dependency_wait();
     kvp::grid_launch_dependents();
-    if constexpr (NORM) {
-        for (int i = threadIdx.x; i < 2 * a.D; i += kRotThreads) {
-            const uint16_t *w = i < a.D ? a.q_weight + i : a.k_weight + (i - a.D);
-            const bool normed = (i < a.D ? a.q_weight : a.k_weight) != nullptr;
-            norms[i >= a.D][i < a.D ? i : i - a.D] = normed ? __uint_as_float((uint32_t)*w << 16) + a.offset : 1.f;
-        }
-        __syncthreads();
-    }
     int32_t s = 0, n = 0, end = 0;  // the token's sequence, its context, the token past it
     for (int i = t0, buf = 0; i < turns_end; ++i, buf ^= 1) {
         const bool live = GROUP >= 32 || i < t_end;  // else: the last token once more, without rows
@@ -245,9 +175,8 @@ __global__ void __launch_bounds__(kRotThreads, kRotResident<INTERLEAVED, GROUP, 
         }
         const int32_t by = a.positions ? a.positions[t] : pos;
         for (int i = tid; i < a.rot / 2; i += GROUP) {
-            const uint64_t turn = (uint64_t)(int64_t)by * a.steps[i] + (1ull << 31);
             float sn, cn;
-            sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &sn, &cn);
+            turn_of(by, a.steps[i], sn, cn);
             cosines[buf][sub][i] = cn * a.magnitude;
             sines[buf][sub][i] = sn * a.magnitude;
         }
@@ -279,83 +208,51 @@ __global__ void __launch_bounds__(kRotThreads, kRotResident<INTERLEAVED, GROUP, 
             *reinterpret_cast<uint4 *>(dst) = x0;
             if (pair) *reinterpret_cast<uint4 *>(dst + a.rot) = y0;
         };
-        if constexpr (NORM) {
-            // (every thread of a warp goes round as often: the sums need them all)
-            for (int first = 0;;) {
+        for (int r = r0;;) {
 #pragma unroll
-                for (int b = 0; b < BATCH; ++b) {
-                    const int r = r0 + first + b * step, which = r >= q_rows;
-                    const bool mine = r < rows, normed = r < q_rows + a.Hkv && (which ? a.k_weight : a.q_weight) != nullptr;
-                    float2 u[4] = {}, v[4] = {};
-                    float sum = 0.f;
-                    if (mine) {
-                        const uint32_t *xw = reinterpret_cast<const uint32_t *>(&x[b]), *yw = reinterpret_cast<const uint32_t *>(&y[b]);
+            for (int b = 0; b < BATCH; ++b)
+                if (r + b * step < rows) finish(r + b * step, x[b], y[b]);
+            r += BATCH * step;
+            if (r >= rows) break;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            u[e] = unpack2(xw[e]);
-                            sum = __fmaf_rn(u[e].x, u[e].x, __fmaf_rn(u[e].y, u[e].y, sum));
-                            if (!INTERLEAVED && pair) {
-                                v[e] = unpack2(yw[e]);
-                                sum = __fmaf_rn(v[e].x, v[e].x, __fmaf_rn(v[e].y, v[e].y, sum));
-                            }
-                        }
-                    }
-                    for (int off = 1; off < lanes; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-                    if (!mine) continue;
-                    const int g = r - q_rows;
-                    if (g >= 0 && !slot) continue;
-                    uint8_t *dst = g < 0 ? q_dst + r * a.D * 2 : slot + g * head_bytes;
-                    if (g < a.Hkv) {
-                        if (normed) {
-                            const float by = rsqrtf(sum / (float)a.D + a.eps);
-                            const float2 by2 = make_float2(by, by);
-                            const float2 *w = reinterpret_cast<const float2 *>(norms[which] + at * 8);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                u[e] = __fmul2_rn(__fmul2_rn(u[e], by2), w[e]);
-                                if (!INTERLEAVED && pair) v[e] = __fmul2_rn(__fmul2_rn(v[e], by2), w[e + a.rot / 4]);
-                            }
-                        }
-                        if (turns) {
-                            if constexpr (INTERLEAVED)
-                                turn_adjacent(u, c, sn);
-                            else
-                                turn_halves(u, v, c, sn);
-                        }
-                        x[b] = make_uint4(pack2(u[0].x, u[0].y), pack2(u[1].x, u[1].y), pack2(u[2].x, u[2].y), pack2(u[3].x, u[3].y));
-                        if (!INTERLEAVED && pair)
-                            y[b] = make_uint4(pack2(v[0].x, v[0].y), pack2(v[1].x, v[1].y), pack2(v[2].x, v[2].y), pack2(v[3].x, v[3].y));
-                    }
-                    *reinterpret_cast<uint4 *>(dst) = x[b];
-                    if (pair) *reinterpret_cast<uint4 *>(dst + a.rot) = y[b];
-                }
-                first += BATCH * step;
-                if (first >= token_rows) break;
-#pragma unroll
-                for (int b = 0; b < BATCH; ++b)
-                    if (r0 + first + b * step < rows) load(r0 + first + b * step, x[b], y[b]);
-            }
-        } else {
-            for (int r = r0;;) {
-#pragma unroll
-                for (int b = 0; b < BATCH; ++b)
-                    if (r + b * step < rows) finish(r + b * step, x[b], y[b]);
-                r += BATCH * step;
-                if (r >= rows) break;
-#pragma unroll
-                for (int b = 0; b < BATCH; ++b)
-                    if (r + b * step < rows) load(r + b * step, x[b], y[b]);
-            }
+            for (int b = 0; b < BATCH; ++b)
+                if (r + b * step < rows) load(r + b * step, x[b], y[b]);
         }
     }
 }
 
-bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
-
-// a row stride that holds the row and keeps 16-byte chunks aligned
-bool stride_ok(int64_t stride, int64_t row) { return stride >= row && stride % 8 == 0; }
-
 }  // namespace
+
+int kvp_rotary_check(const kv_pool *p, int layout, const kv_rotary *rot, const uint16_t *q, int64_t q_stride,
+                     const uint16_t *q_out, const uint16_t *k, int64_t k_stride, const uint16_t *v, int64_t v_stride,
+                     const int32_t *dev_q_starts, int T, const int32_t *dev_table, const int32_t *dev_ctx_lens,
+                     int max_blocks, int S, int Hq, bool *go)
+{
+    *go = false;
+    if (!p || !rot || layout < 0 || layout >= p->desc.num_layouts) return KV_ERR_INVALID_ARG;
+    if (S < 0 || T < 0 || max_blocks < 1 || Hq < 0 || Hq > 65536) return KV_ERR_INVALID_ARG;
+    if (!dev_q_starts && T != S) return KV_ERR_INVALID_ARG;
+    if (T > 0 && S == 0) return KV_ERR_INVALID_ARG;
+    const kv_layout &L = p->desc.layouts[layout];
+    if (L.head_dim & KV_Q4) return KV_ERR_UNSUPPORTED;
+    const int64_t D = L.head_dim, Hkv = L.num_kv_heads;
+    if (rot->rot_dim < 0 || rot->rot_dim > D || !std::isfinite(rot->magnitude)) return KV_ERR_INVALID_ARG;
+    if (rot->interleaved < 0 || rot->interleaved > 1) return KV_ERR_INVALID_ARG;
+    if (rot->rot_dim % 16) return KV_ERR_UNSUPPORTED;  // whole 16-byte chunks of either half
+    if (rot->rot_dim > 0 && (!rot->steps || ((uintptr_t)rot->steps & 7u))) return KV_ERR_INVALID_ARG;
+    if ((int64_t)max_blocks * p->desc.block_size >= INT32_MAX) return KV_ERR_INVALID_ARG;
+    *go = T > 0;
+    if (T == 0) return KV_OK;
+    if (!dev_table || !dev_ctx_lens) return KV_ERR_INVALID_ARG;
+    if (!q && !k) return KV_ERR_INVALID_ARG;
+    if (q && (Hq < 1 || !q_out || !rotary_aligned16(q) || !rotary_aligned16(q_out) || !rotary_stride_ok(q_stride, Hq * D)))
+        return KV_ERR_INVALID_ARG;
+    if (q && q == q_out && q_stride != Hq * D) return KV_ERR_INVALID_ARG;  // in place: the same rows
+    if (!k != !v) return KV_ERR_INVALID_ARG;
+    if (k && (!rotary_aligned16(k) || !rotary_aligned16(v) || !rotary_stride_ok(k_stride, Hkv * D) || !rotary_stride_ok(v_stride, Hkv * D)))
+        return KV_ERR_INVALID_ARG;
+    return KV_OK;
+}
 
 extern "C" {
 
@@ -397,54 +294,17 @@ int kv_rotary_steps(const double *inv_freq, int n, uint64_t *steps)
     return KV_OK;
 }
 
-}  // extern "C"
-
-namespace {
-
-template <bool INTERLEAVED, bool NORM>
-void (*rotary_variant(int group))(RotaryArgs)
+int kv_append_rotary(kv_pool *p, int layout, const kv_rotary *rot, const uint16_t *q, int64_t q_stride, uint16_t *q_out,
+                     const uint16_t *k, int64_t k_stride, const uint16_t *v, int64_t v_stride, const int32_t *positions,
+                     const int32_t *dev_q_starts, int T, const int32_t *dev_table, const int32_t *dev_ctx_lens,
+                     int max_blocks, int S, int Hq, void *stream)
 {
-    switch (group) {
-    case 256: return rotary_kernel<INTERLEAVED, 256, NORM>;
-    case 128: return rotary_kernel<INTERLEAVED, 128, NORM>;
-    case 64: return rotary_kernel<INTERLEAVED, 64, NORM>;
-    case 32: return rotary_kernel<INTERLEAVED, 32, NORM>;
-    case 16: return rotary_kernel<INTERLEAVED, 16, NORM>;
-    default: return rotary_kernel<INTERLEAVED, 8, NORM>;
-    }
-}
-
-int append_rotary(kv_pool *p, int layout, const kv_rotary *rot, const kv_head_norm *norm, const uint16_t *q,
-                  int64_t q_stride, uint16_t *q_out, const uint16_t *k, int64_t k_stride, const uint16_t *v,
-                  int64_t v_stride, const int32_t *positions, const int32_t *dev_q_starts, int T,
-                  const int32_t *dev_table, const int32_t *dev_ctx_lens, int max_blocks, int S, int Hq, void *stream)
-{
-    if (!p || !rot || layout < 0 || layout >= p->desc.num_layouts) return KV_ERR_INVALID_ARG;
-    if (S < 0 || T < 0 || max_blocks < 1 || Hq < 0 || Hq > 65536) return KV_ERR_INVALID_ARG;
-    if (!dev_q_starts && T != S) return KV_ERR_INVALID_ARG;
-    if (T > 0 && S == 0) return KV_ERR_INVALID_ARG;
+    bool go;
+    const int rc = kvp_rotary_check(p, layout, rot, q, q_stride, q_out, k, k_stride, v, v_stride, dev_q_starts, T, dev_table,
+                                    dev_ctx_lens, max_blocks, S, Hq, &go);
+    if (rc || !go) return rc;
     const kv_layout &L = p->desc.layouts[layout];
-    if (L.head_dim & KV_Q4) return KV_ERR_UNSUPPORTED;
-    const int64_t D = L.head_dim, Hkv = L.num_kv_heads;
-    if (rot->rot_dim < 0 || rot->rot_dim > D || !std::isfinite(rot->magnitude)) return KV_ERR_INVALID_ARG;
-    if (rot->interleaved < 0 || rot->interleaved > 1) return KV_ERR_INVALID_ARG;
-    if (rot->rot_dim % 16) return KV_ERR_UNSUPPORTED;  // whole 16-byte chunks of either half
-    if (rot->rot_dim > 0 && (!rot->steps || ((uintptr_t)rot->steps & 7u))) return KV_ERR_INVALID_ARG;
-    if ((int64_t)max_blocks * p->desc.block_size >= INT32_MAX) return KV_ERR_INVALID_ARG;
-    if (norm) {
-        if (!(norm->eps >= 0.f) || !std::isfinite(norm->eps) || !std::isfinite(norm->offset)) return KV_ERR_INVALID_ARG;
-        if (!aligned16(norm->q_weight) || !aligned16(norm->k_weight)) return KV_ERR_INVALID_ARG;
-        if (D > kMaxNormDim) return KV_ERR_UNSUPPORTED;  // a row's threads are of one warp
-    }
-    if (T == 0) return KV_OK;
-    if (!dev_table || !dev_ctx_lens) return KV_ERR_INVALID_ARG;
-    if (!q && !k) return KV_ERR_INVALID_ARG;
-    if (q && (Hq < 1 || !q_out || !aligned16(q) || !aligned16(q_out) || !stride_ok(q_stride, Hq * D)))
-        return KV_ERR_INVALID_ARG;
-    if (q && q == q_out && q_stride != Hq * D) return KV_ERR_INVALID_ARG;  // in place: the same rows
-    if (!k != !v) return KV_ERR_INVALID_ARG;
-    if (k && (!aligned16(k) || !aligned16(v) || !stride_ok(k_stride, Hkv * D) || !stride_ok(v_stride, Hkv * D)))
-        return KV_ERR_INVALID_ARG;
+    const int64_t Hkv = L.num_kv_heads;
     RotaryArgs a{};
     a.q = q;
     a.k = k;
@@ -468,33 +328,28 @@ int append_rotary(kv_pool *p, int layout, const kv_rotary *rot, const kv_head_no
     a.S = S;
     a.Hq = Hq;
     a.Hkv = (int32_t)Hkv;
-    a.D = (int32_t)D;
+    a.D = L.head_dim;
     a.bs = p->desc.block_size;
     a.rot = rot->rot_dim;
     a.items = (rot->interleaved ? a.rot / 8 : a.rot / 16) + (a.D - a.rot) / 8;
-    a.lanes = a.items;
-    if (norm) {
-        a.q_weight = norm->q_weight;
-        a.k_weight = norm->k_weight;
-        a.eps = norm->eps;
-        a.offset = norm->offset;
-        for (a.lanes = 1; a.lanes < a.items;) a.lanes *= 2;
-    }
-    const int64_t token_items = (int64_t)a.lanes * ((q ? Hq : 0) + (k ? 2 * Hkv : 0));
+    const int64_t token_items = (int64_t)a.items * ((q ? Hq : 0) + (k ? 2 * Hkv : 0));
     const int64_t resident = (int64_t)kRotShared * std::max(1, p->sm_count);
-    const int batch = norm ? (rot->interleaved ? kRotBatch<true, 32, true> : kRotBatch<false, 32, true>)
-                      : rot->interleaved ? kRotBatch<true, 32>
-                                         : kRotBatch<false, 32>;
+    const int batch = rot->interleaved ? kRotBatch<true, 32> : kRotBatch<false, 32>;
     int per = 1;  // groups of a CTA (see rotary_kernel)
-    while (kRotThreads / per > 8 && kRotThreads / (2 * per) >= a.lanes && T >= 2 * per * resident &&
+    while (kRotThreads / per > 8 && kRotThreads / (2 * per) >= a.items && T >= 2 * per * resident &&
            token_items <= batch * (kRotThreads / (2 * per)))
         per *= 2;
     a.run = (int32_t)(T / (per * resident));
     a.longer = (int32_t)(T % (per * resident));
-    void (*kernel)(RotaryArgs) = norm ? (rot->interleaved ? rotary_variant<true, true>(kRotThreads / per)
-                                                          : rotary_variant<false, true>(kRotThreads / per))
-                                 : rot->interleaved ? rotary_variant<true, false>(kRotThreads / per)
-                                                    : rotary_variant<false, false>(kRotThreads / per);
+    void (*kernel)(RotaryArgs) = nullptr;
+    switch (kRotThreads / per) {
+    case 256: kernel = rot->interleaved ? rotary_kernel<true, 256> : rotary_kernel<false, 256>; break;
+    case 128: kernel = rot->interleaved ? rotary_kernel<true, 128> : rotary_kernel<false, 128>; break;
+    case 64: kernel = rot->interleaved ? rotary_kernel<true, 64> : rotary_kernel<false, 64>; break;
+    case 32: kernel = rot->interleaved ? rotary_kernel<true, 32> : rotary_kernel<false, 32>; break;
+    case 16: kernel = rot->interleaved ? rotary_kernel<true, 16> : rotary_kernel<false, 16>; break;
+    default: kernel = rot->interleaved ? rotary_kernel<true, 8> : rotary_kernel<false, 8>; break;
+    }
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -508,30 +363,6 @@ int append_rotary(kv_pool *p, int layout, const kv_rotary *rot, const kv_head_no
         return KV_ERR_CUDA;
     kvp_note_stream(stream, false);
     return KV_OK;
-}
-
-}  // namespace
-
-extern "C" {
-
-int kv_append_rotary(kv_pool *p, int layout, const kv_rotary *rot, const uint16_t *q, int64_t q_stride, uint16_t *q_out,
-                     const uint16_t *k, int64_t k_stride, const uint16_t *v, int64_t v_stride, const int32_t *positions,
-                     const int32_t *dev_q_starts, int T, const int32_t *dev_table, const int32_t *dev_ctx_lens,
-                     int max_blocks, int S, int Hq, void *stream)
-{
-    return append_rotary(p, layout, rot, nullptr, q, q_stride, q_out, k, k_stride, v, v_stride, positions, dev_q_starts, T,
-                         dev_table, dev_ctx_lens, max_blocks, S, Hq, stream);
-}
-
-int kv_append_rotary_norm(kv_pool *p, int layout, const kv_rotary *rot, const kv_head_norm *norm, const uint16_t *q,
-                          int64_t q_stride, uint16_t *q_out, const uint16_t *k, int64_t k_stride, const uint16_t *v,
-                          int64_t v_stride, const int32_t *positions, const int32_t *dev_q_starts, int T,
-                          const int32_t *dev_table, const int32_t *dev_ctx_lens, int max_blocks, int S, int Hq,
-                          void *stream)
-{
-    if (!norm) return KV_ERR_INVALID_ARG;
-    return append_rotary(p, layout, rot, norm, q, q_stride, q_out, k, k_stride, v, v_stride, positions, dev_q_starts, T,
-                         dev_table, dev_ctx_lens, max_blocks, S, Hq, stream);
 }
 
 }  // extern "C"
