@@ -47,10 +47,12 @@ __device__ __forceinline__ void turn2(float2 &u, float2 &v, float2 c, float2 s)
     v = __ffma2_rn(v, c, __fmul2_rn(u, s));
     u = p;
 }
-// an adjacent pair
-__device__ __forceinline__ void turn1(float2 &u, float c, float s)
+// an adjacent pair (c, s: its cos and sin)
+__device__ __forceinline__ void turn(float &x, float &y, float c, float s)
 {
-    u = __ffma2_rn(u, make_float2(c, c), __fmul2_rn(make_float2(u.y, u.x), make_float2(-s, s)));
+    const float p = __fmaf_rn(x, c, -__fmul_rn(y, s));
+    y = __fmaf_rn(y, c, __fmul_rn(x, s));
+    x = p;
 }
 
 // the cos and sin of position `by` at a frequency of `step` turns a position, in

@@ -5,11 +5,10 @@
 // v is copied, k and v go to the paged pool.
 //
 // Bound by HBM for prompts (each row read and written once) and by latency for a
-// decode step.  A head's columns lie with 4 to 32 lanes of a warp (its items, as in
-// rotary.cu: pairs of chunks that turn together, chunks that turn, chunks that only
-// are normed), which sum its squares by shuffles, so a warp needs no other and no
-// barrier: it takes a range of (token, batch of rows) units, the same number as every
-// other, computes each token's angles among its lanes, and keeps its columns'
+// decode step.  A head's columns lie with 4 to 16 lanes of a warp, 16 columns with each
+// (two chunks; of the half layout, where it turns, those that turn together), which
+// sum its squares by shuffles, so a warp needs no other and no barrier: it takes a range of (token, batch of rows of q, k or v) units, as many as
+// every other, computes each token's angles among its lanes, and keeps its columns'
 // frequencies from token to token; the weights lie in shared memory in fp32.
 #include <algorithm>
 #include <climits>
@@ -25,7 +24,7 @@ namespace {
 using namespace kvp;
 
 constexpr int kNormThreads = 128;
-constexpr int kNormResident = 6;   // CTAs an SM
+constexpr int kNormResident = 5;   // CTAs an SM
 constexpr int kMaxNormDim = 256;   // a head's lanes are of one warp
 
 struct NormArgs {
@@ -45,28 +44,32 @@ struct NormArgs {
     float magnitude, eps, offset, inv_d;
     int32_t pages_per_block, max_blocks;
     int32_t S, Hq, Hkv, D, bs, rot;
-    int32_t items, batches;     // of a row; units of a token
+    int32_t items;                       // of a row
+    int32_t units, q_units, kv_units;    // of a token: q_units + 2 kv_units
 };
 
-// rows of a warp in a unit, times the lanes of a row
-template <bool INTERLEAVED>
-constexpr int kNormBatch = INTERLEAVED ? 4 : 2;
+constexpr int kNormBatch = 2;  // rows of a lane in a unit
 
 template <bool INTERLEAVED, int LANES>
 __global__ void __launch_bounds__(kNormThreads, kNormResident) rotary_norm_kernel(const __grid_constant__ NormArgs a)
 {
     constexpr int RPW = 32 / LANES;             // rows side by side in a warp
-    constexpr int NP = INTERLEAVED ? 4 : 8;     // pairs of an item
+    constexpr int NP = 8;                       // pairs of an item that turns
     constexpr int OWN = (NP + RPW - 1) / RPW;   // of which a lane computes
-    constexpr int BATCH = kNormBatch<INTERLEAVED>;
+    constexpr int BATCH = kNormBatch;
     constexpr unsigned ALL = 0xffffffffu;
     // weights with the offset, of q and of k: a chunk's first four columns, then its others
     __shared__ __align__(16) float4 weights[2][2][kMaxNormDim / 8];
     const int lane = threadIdx.x & 31, item = lane % LANES, grp = lane / LANES;
-    const int turned = INTERLEAVED ? a.rot / 8 : a.rot / 16;
-    const bool holds = item < a.items, turns = item < turned, pair = !INTERLEAVED && turns;
-    const int at = turns ? item : item + a.rot / 8 - turned;  // the item's (first) chunk
-    const int far = a.rot / 16;                               // chunks to a pair's other one
+    // An item is two chunks of eight columns: of the half layout two that turn together
+    // or two that do not turn; of adjacent pairs a chunk of either half of the head.
+    const int chunks = a.D / 8, turned = a.rot / 8;  // chunks; those that turn
+    const int near = INTERLEAVED || item < turned / 2 ? item : item + turned / 2;
+    const int apart = INTERLEAVED ? (chunks + 1) / 2 : item < turned / 2 ? turned / 2 : (chunks - turned + 1) / 2;
+    const bool holds = item < a.items, pair = holds && near + apart < (INTERLEAVED || item >= turned / 2 ? chunks : turned);
+    const bool turns0 = holds && near < turned, turns1 = INTERLEAVED ? pair && near + apart < turned : turns0;
+    // (a lane without columns, or with one chunk, takes any chunk along)
+    const int chunk0 = holds ? near : 0, chunk1 = pair ? near + apart : chunk0, hops = (chunk1 - chunk0) * 8;
     grid_dependency_wait();
     grid_launch_dependents();
     for (int i = threadIdx.x; i < a.D / 4; i += kNormThreads)  // (of q, then of k: four columns at a time)
@@ -83,8 +86,9 @@ __global__ void __launch_bounds__(kNormThreads, kNormResident) rotary_norm_kerne
     uint64_t step[OWN];  // of the pairs whose angles this lane computes
 #pragma unroll
     for (int e = 0; e < OWN; ++e) {
-        const int p = e * RPW + grp;
-        step[e] = turns && p < NP ? a.steps[item * NP + p] : 0;
+        const int p = e * RPW + grp;  // of adjacent pairs: four of either chunk
+        const bool any = p < NP && (INTERLEAVED && p >= 4 ? turns1 : turns0);
+        step[e] = any ? a.steps[!INTERLEAVED ? chunk0 * 8 + p : p < 4 ? chunk0 * 4 + p : chunk1 * 4 + p - 4] : 0;
     }
     __syncthreads();
 
@@ -92,28 +96,28 @@ __global__ void __launch_bounds__(kNormThreads, kNormResident) rotary_norm_kerne
     int64_t unit = warp * a.per_warp + min(warp, a.longer);
     const int64_t unit_end = unit + a.per_warp + (warp < a.longer);
     if (warp >= a.warps) return;
-    int t = (int)(unit / a.batches);
-    int first = (int)(unit - (int64_t)t * a.batches) * BATCH * RPW;  // the unit's first row
-    const int q_rows = a.q ? a.Hq : 0, kv = a.k ? a.Hkv : 0, rows = q_rows + 2 * kv;
+    int t = (int)(unit / a.units);
+    int batch = (int)(unit - (int64_t)t * a.units);      // of the token's
     const int64_t head_bytes = (int64_t)a.bs * a.D * 2;  // of one KV head in a block
     int32_t n = 0, end = INT32_MIN, s = 0;               // the token's sequence, its context, the token past it
-    float2 c[NP / 2], sn[NP / 2];                        // of the item's pairs
+    float c[NP], sn[NP];                                 // of the item's pairs
     uint8_t *slot = nullptr;
-    int now = -1;                                        // the token whose c, sn and slot these are
+    int now = -1;                                        // the token whose these are
     for (; unit < unit_end; ++unit) {
+        // the unit's rows: of q, k or v alone
+        const int of = batch < a.q_units ? 0 : batch < a.q_units + a.kv_units ? 1 : 2;
+        const int first = (batch - (of == 0 ? 0 : of == 1 ? a.q_units : a.q_units + a.kv_units)) * BATCH * RPW + grp;
+        const int rows = of == 0 ? a.Hq : a.Hkv;
+        const uint16_t *src = (of == 0 ? a.q + t * a.q_stride : of == 1 ? a.k + t * a.k_stride : a.v + t * a.v_stride) + chunk0 * 8;
         uint4 x[BATCH], y[BATCH];
         // the rows' addresses need the token alone: they are on their way before its
-        // position, angles and slot, four dependent loads away, are known
+        // position, angles and slot, four dependent loads away, are known.  (A thread
+        // without a row, or without columns, loads others': no branch.)
 #pragma unroll
         for (int b = 0; b < BATCH; ++b) {
-            const int r = first + b * RPW + grp, g = r - q_rows;
-            if (holds && r < rows) {
-                const uint16_t *src = g < 0    ? a.q + t * a.q_stride + r * a.D
-                                      : g < kv ? a.k + t * a.k_stride + g * a.D
-                                               : a.v + t * a.v_stride + (g - kv) * a.D;
-                x[b] = *reinterpret_cast<const uint4 *>(src + at * 8);
-                if (pair) y[b] = *reinterpret_cast<const uint4 *>(src + (at + far) * 8);
-            }
+            const uint16_t *row = src + min(first + b * RPW, rows - 1) * a.D;
+            x[b] = *reinterpret_cast<const uint4 *>(row);
+            y[b] = *reinterpret_cast<const uint4 *>(row + hops);
         }
         if (t != now) {
             now = t;
@@ -127,12 +131,12 @@ __global__ void __launch_bounds__(kNormThreads, kNormResident) rotary_norm_kerne
             // outside the table or a page outside the pool is reported (as is t >= end: a
             // bad array)
             slot = nullptr;
-            if (kv && n > 0) {
+            if (a.kv_units && n > 0) {
                 bool ok = t < end && pos >= 0 && pos < a.max_blocks * a.bs;
                 if (ok) {
                     const int32_t b = pos / a.bs, phys = a.table[(int64_t)s * a.max_blocks + b];
                     ok = phys >= 0 && (int64_t)phys + a.pages_per_block <= a.n_pages;
-                    if (ok) slot = a.pool + (int64_t)phys * a.page_bytes + (int64_t)(pos - b * a.bs) * a.D * 2 + at * 16;
+                    if (ok) slot = a.pool + (int64_t)phys * a.page_bytes + (int64_t)(pos - b * a.bs) * a.D * 2;
                 }
                 if (!ok && lane == 0) atomicCAS(a.err, 0, KV_ERR_DEVICE_BOUNDS);
             }
@@ -146,71 +150,73 @@ __global__ void __launch_bounds__(kNormThreads, kNormResident) rotary_norm_kerne
             }
 #pragma unroll
             for (int e = 0; e < NP; ++e) {
-                const float ce = __shfl_sync(ALL, own_c[e / RPW], (e % RPW) * LANES + item);
-                const float se = __shfl_sync(ALL, own_s[e / RPW], (e % RPW) * LANES + item);
-                if (e & 1)
-                    c[e / 2].y = ce, sn[e / 2].y = se;
-                else
-                    c[e / 2].x = ce, sn[e / 2].x = se;
+                c[e] = __shfl_sync(ALL, own_c[e / RPW], (e % RPW) * LANES + item);
+                sn[e] = __shfl_sync(ALL, own_s[e / RPW], (e % RPW) * LANES + item);
             }
         }
-        uint8_t *q_dst = reinterpret_cast<uint8_t *>(a.q_out + (int64_t)t * a.Hq * a.D) + at * 16;
+        if (of < 2) {
+            const bool normed = (of ? a.k_weight : a.q_weight) != nullptr;
 #pragma unroll
-        for (int b = 0; b < BATCH; ++b) {
-            const int r = first + b * RPW + grp, g = r - q_rows;
-            const bool mine = holds && r < rows;
-            if (first + b * RPW < q_rows + kv) {  // (the warp's rows of v alone need no more than a copy)
+            for (int b = 0; b < BATCH; ++b) {
                 float2 u[4], v[4];
                 const uint32_t *xw = reinterpret_cast<const uint32_t *>(&x[b]), *yw = reinterpret_cast<const uint32_t *>(&y[b]);
-                float2 sum2 = make_float2(0.f, 0.f);
+                float2 sum2 = make_float2(0.f, 0.f), far2 = make_float2(0.f, 0.f);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    u[e] = mine ? unpack2(xw[e]) : make_float2(0.f, 0.f);
+                    u[e] = unpack2(xw[e]);
                     sum2 = __ffma2_rn(u[e], u[e], sum2);
-                    if (!INTERLEAVED) {
-                        v[e] = mine && pair ? unpack2(yw[e]) : make_float2(0.f, 0.f);
-                        sum2 = __ffma2_rn(v[e], v[e], sum2);
-                    }
+                    v[e] = unpack2(yw[e]);
+                    far2 = __ffma2_rn(v[e], v[e], far2);
                 }
-                float sum = sum2.x + sum2.y;
+                float sum = (holds ? sum2.x + sum2.y : 0.f) + (pair ? far2.x + far2.y : 0.f);
 #pragma unroll
                 for (int off = 1; off < LANES; off <<= 1) sum += __shfl_xor_sync(ALL, sum, off);
-                if (g < kv) {
-                    const bool of_k = g >= 0;
-                    const float by = (of_k ? a.k_weight : a.q_weight) ? rsqrtf(fmaf(sum, a.inv_d, a.eps)) : 1.f;
-                    const float2 by2 = make_float2(by, by);
-                    auto scale = [&](float2 (&z)[4], int chunk) {
-                        const float4 w0 = weights[of_k][0][chunk], w1 = weights[of_k][1][chunk];
-                        z[0] = __fmul2_rn(__fmul2_rn(z[0], by2), make_float2(w0.x, w0.y));
-                        z[1] = __fmul2_rn(__fmul2_rn(z[1], by2), make_float2(w0.z, w0.w));
-                        z[2] = __fmul2_rn(__fmul2_rn(z[2], by2), make_float2(w1.x, w1.y));
-                        z[3] = __fmul2_rn(__fmul2_rn(z[3], by2), make_float2(w1.z, w1.w));
-                    };
-                    if (holds) scale(u, at);
-                    if (!INTERLEAVED && pair) scale(v, at + far);
-                    if (turns) {
+                const float by = normed ? rsqrtf(fmaf(sum, a.inv_d, a.eps)) : 1.f;
+                const float2 by2 = make_float2(by, by);
+                auto scale = [&](float2 (&z)[4], int chunk) {
+                    const float4 w0 = weights[of][0][chunk], w1 = weights[of][1][chunk];
+                    z[0] = __fmul2_rn(__fmul2_rn(z[0], by2), make_float2(w0.x, w0.y));
+                    z[1] = __fmul2_rn(__fmul2_rn(z[1], by2), make_float2(w0.z, w0.w));
+                    z[2] = __fmul2_rn(__fmul2_rn(z[2], by2), make_float2(w1.x, w1.y));
+                    z[3] = __fmul2_rn(__fmul2_rn(z[3], by2), make_float2(w1.z, w1.w));
+                };
+                scale(u, chunk0);
+                scale(v, chunk1);
+                if constexpr (INTERLEAVED) {
+                    if (turns0) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            if constexpr (INTERLEAVED)
-                                turn1(u[e], e & 1 ? c[e / 2].y : c[e / 2].x, e & 1 ? sn[e / 2].y : sn[e / 2].x);
-                            else
-                                turn2(u[e], v[e], c[e], sn[e]);
-                        }
+                        for (int e = 0; e < 4; ++e) turn(u[e].x, u[e].y, c[e], sn[e]);
                     }
-                    x[b] = make_uint4(pack2(u[0].x, u[0].y), pack2(u[1].x, u[1].y), pack2(u[2].x, u[2].y), pack2(u[3].x, u[3].y));
-                    if (!INTERLEAVED && pair)
-                        y[b] = make_uint4(pack2(v[0].x, v[0].y), pack2(v[1].x, v[1].y), pack2(v[2].x, v[2].y), pack2(v[3].x, v[3].y));
+                    if (turns1) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) turn(v[e].x, v[e].y, c[4 + e], sn[4 + e]);
+                    }
+                } else if (turns0) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        turn2(u[e], v[e], make_float2(c[2 * e], c[2 * e + 1]), make_float2(sn[2 * e], sn[2 * e + 1]));
                 }
-            }
-            if (mine && (g < 0 || slot)) {
-                uint8_t *dst = g < 0 ? q_dst + r * a.D * 2 : slot + g * head_bytes;  // v's heads follow k's
-                *reinterpret_cast<uint4 *>(dst) = x[b];
-                if (pair) *reinterpret_cast<uint4 *>(dst + far * 16) = y[b];
+                x[b] = make_uint4(pack2(u[0].x, u[0].y), pack2(u[1].x, u[1].y), pack2(u[2].x, u[2].y), pack2(u[3].x, u[3].y));
+                y[b] = make_uint4(pack2(v[0].x, v[0].y), pack2(v[1].x, v[1].y), pack2(v[2].x, v[2].y), pack2(v[3].x, v[3].y));
             }
         }
-        first += BATCH * RPW;
-        if (first >= rows) {
-            first = 0;
+        uint8_t *dst = of == 0   ? reinterpret_cast<uint8_t *>(a.q_out + (int64_t)t * a.Hq * a.D)
+                       : of == 1 ? slot
+                                 : slot + a.Hkv * head_bytes;
+        const int64_t row_bytes = of == 0 ? a.D * 2 : head_bytes;
+        if (holds && (of == 0 || slot)) {
+            dst += chunk0 * 16;
+#pragma unroll
+            for (int b = 0; b < BATCH; ++b) {
+                const int r = first + b * RPW;
+                if (r < rows) {
+                    *reinterpret_cast<uint4 *>(dst + r * row_bytes) = x[b];
+                    if (pair) *reinterpret_cast<uint4 *>(dst + r * row_bytes + hops * 2) = y[b];
+                }
+            }
+        }
+        if (++batch == a.units) {
+            batch = 0;
             ++t;
         }
     }
@@ -222,8 +228,7 @@ void (*norm_variant(int lanes))(NormArgs)
     switch (lanes) {
     case 4: return rotary_norm_kernel<INTERLEAVED, 4>;
     case 8: return rotary_norm_kernel<INTERLEAVED, 8>;
-    case 16: return rotary_norm_kernel<INTERLEAVED, 16>;
-    default: return rotary_norm_kernel<INTERLEAVED, 32>;
+    default: return rotary_norm_kernel<INTERLEAVED, 16>;  // (256 columns, and no more)
     }
 }
 
@@ -276,13 +281,14 @@ extern "C" int kv_append_rotary_norm(kv_pool *p, int layout, const kv_rotary *ro
     a.D = L.head_dim;
     a.bs = p->desc.block_size;
     a.rot = rot->rot_dim;
-    a.items = (rot->interleaved ? a.rot / 8 : a.rot / 16) + (a.D - a.rot) / 8;
+    a.items = rot->interleaved ? (a.D / 8 + 1) / 2 : a.rot / 16 + ((a.D - a.rot) / 8 + 1) / 2;
     int lanes = 4;
     while (lanes < a.items) lanes *= 2;
-    const int batch = (rot->interleaved ? kNormBatch<true> : kNormBatch<false>) * (32 / lanes);
-    const int rows = (q ? Hq : 0) + (k ? 2 * a.Hkv : 0);
-    a.batches = (rows + batch - 1) / batch;
-    const int64_t units = (int64_t)T * a.batches;
+    const int batch = kNormBatch * (32 / lanes);
+    a.q_units = q ? (Hq + batch - 1) / batch : 0;
+    a.kv_units = k ? (a.Hkv + batch - 1) / batch : 0;
+    a.units = a.q_units + 2 * a.kv_units;
+    const int64_t units = (int64_t)T * a.units;
     a.warps = std::min((int64_t)kNormResident * std::max(1, p->sm_count) * (kNormThreads / 32), units);
     a.per_warp = units / a.warps;
     a.longer = units % a.warps;
