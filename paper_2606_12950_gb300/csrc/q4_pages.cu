@@ -46,15 +46,14 @@ struct PackParams {
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// least and greatest of a chunk's values, NaN if one is
-__device__ __forceinline__ void extremes(const uint4 &x, __nv_bfloat162 &mn, __nv_bfloat162 &mx)
+// The least value and the greatest one's negative of a chunk, NaN if one is: a
+// pair, so that a step among lanes is one shuffle and one minimum.
+__device__ __forceinline__ __nv_bfloat162 extremes(const uint4 &x)
 {
     const __nv_bfloat162 *p = reinterpret_cast<const __nv_bfloat162 *>(&x);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        mn = __hmin2_nan(mn, p[e]);
-        mx = __hmax2_nan(mx, p[e]);
-    }
+    const __nv_bfloat162 mn = __hmin2_nan(__hmin2_nan(p[0], p[1]), __hmin2_nan(p[2], p[3]));
+    const __nv_bfloat162 mx = __hmax2_nan(__hmax2_nan(p[0], p[1]), __hmax2_nan(p[2], p[3]));
+    return __halves2bfloat162(__hmin_nan(mn.x, mn.y), __hneg(__hmax_nan(mx.x, mx.y)));
 }
 __device__ __forceinline__ __nv_bfloat162 shuffled(__nv_bfloat162 v, int off)
 {
@@ -62,33 +61,69 @@ __device__ __forceinline__ __nv_bfloat162 shuffled(__nv_bfloat162 v, int off)
     return *reinterpret_cast<const __nv_bfloat162 *>(&w);
 }
 
-// A group's parameters: s and z as they are stored, 1 / s.
-struct Group {
-    float s, z, inv;
-    uint32_t word;  // (s, z) bf16
-};
-__device__ __forceinline__ Group group_of(__nv_bfloat162 mn, __nv_bfloat162 mx)
+// Of N values a lane, each to be joined over N lanes (of those whose numbers differ
+// in bits N / 2 * STEP .. STEP): the one that this lane's bits name, joined.  log2 N
+// rounds of N / 2, N / 4, .. shuffles.
+template <int N, int STEP>
+__device__ __forceinline__ __nv_bfloat162 joined(__nv_bfloat162 (&e)[N], int lane)
 {
-    Group g;
-    const float lo = __bfloat162float(__hmin_nan(mn.x, mn.y)), hi = __bfloat162float(__hmax_nan(mx.x, mx.y));
-    const float span = hi - lo;
-    __nv_bfloat16 s = __float2bfloat16_rn(__fdiv_rn(span, 15.f));
-    if (!(__bfloat162float(s) >= kScaleLeast)) s = __float2bfloat16_rn(0.f);
-    if (!(span < kSpanLimit)) s = __ushort_as_bfloat16(0x7fc0);  // NaN
-    g.s = __bfloat162float(s);
-    g.z = lo;
-    g.inv = g.s > 0.f ? __frcp_rn(g.s) : 0.f;
-    g.word = (uint32_t)__bfloat16_as_ushort(s) | (__float_as_uint(lo) & 0xFFFF0000u);
-    return g;
+#pragma unroll
+    for (int n = N / 2; n > 0; n /= 2) {
+        const bool up = (lane & (n * STEP)) != 0;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const __nv_bfloat162 keep = up ? e[i + n] : e[i], give = up ? e[i] : e[i + n];
+            e[i] = __hmin2_nan(keep, shuffled(give, n * STEP));
+        }
+    }
+    return e[0];
 }
 
-// the code of a value, in the low four bits (0 where s = 0; some code in a NaN
-// group)
-__device__ __forceinline__ uint32_t code_of(float x, const Group &g)
+// A group's parameters, (s, z) as they are stored, and about 1 / s; each lane that
+// shares the group's row computes another group's.
+__device__ __forceinline__ uint32_t params_of(__nv_bfloat162 ext, float &inv)
 {
-    const float d = x - g.z, q = d * g.inv;
-    const float r = __fmaf_rn(__fmaf_rn(-q, g.s, d), g.inv, q);
-    return __float_as_uint(r + 12582912.f) & 15u;
+    const float lo = __bfloat162float(ext.x), span = -__bfloat162float(ext.y) - lo;
+    // span / 15, rounded to the nearest fp32: a quotient corrected by its residual
+    const float q = span * (1.f / 15.f);
+    __nv_bfloat16 s = __float2bfloat16_rn(__fmaf_rn(__fmaf_rn(-q, 15.f, span), 1.f / 15.f, q));
+    if (!(__bfloat162float(s) >= kScaleLeast)) s = __float2bfloat16_rn(0.f);
+    if (!(span < kSpanLimit)) s = __ushort_as_bfloat16(0x7fc0);  // NaN
+    const float f = __bfloat162float(s);
+    inv = f > 0.f ? __fdividef(1.f, f) : 0.f;
+    return (uint32_t)__bfloat16_as_ushort(s) | (__float_as_uint(lo) & 0xFFFF0000u);
+}
+
+// As the codes take them, two values at a time.
+struct Group {
+    float2 ns, nz, inv;  // -s, -z, 1 / s
+    __device__ __forceinline__ Group(uint32_t word, float i)
+    {
+        ns = make_float2(-lo_f(word), -lo_f(word));
+        nz = make_float2(-hi_f(word), -hi_f(word));
+        inv = make_float2(i, i);
+    }
+};
+
+// kCodeBase plus the codes of a word's two values (0 where s = 0; anything in a NaN
+// group), whole numbers.
+constexpr float kCodeBase = 12582912.f;  // 1.5 * 2^23
+__device__ __forceinline__ float2 based_codes(uint32_t w, const Group &g)
+{
+    const float2 d = __fadd2_rn(make_float2(lo_f(w), hi_f(w)), g.nz), q = __fmul2_rn(d, g.inv);
+    return __fadd2_rn(__ffma2_rn(__ffma2_rn(q, g.ns, d), g.inv, q), make_float2(kCodeBase, kCodeBase));
+}
+// the next word's codes, 256 times, added
+__device__ __forceinline__ float2 with_next(float2 based, float2 next)
+{
+    return __ffma2_rn(__fadd2_rn(next, make_float2(-kCodeBase, -kCodeBase)), make_float2(256.f, 256.f), based);
+}
+// Codes are joined as fp32 sums above kCodeBase, whose low 16 bits four of them are:
+// the integer units, which split and compare the bf16 pairs, have less to spare.
+__device__ __forceinline__ float four(float2 based) { return __fmaf_rn(based.y - kCodeBase, 16.f, based.x); }
+__device__ __forceinline__ uint32_t eight(float lo, float hi)
+{
+    return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x5410);
 }
 
 template <int D, int N>
@@ -117,67 +152,72 @@ __global__ void __launch_bounds__(kPackThreads) pack_blocks_kernel(const __grid_
         for (int c = 0; c < NG; ++c)
             v[r][c] = *reinterpret_cast<const uint4 *>(src + kv + (2 * tig + (r & 1) + 4 * (r & 2)) * 2 * D +
                                                        2 * (64 * c + 8 * gid));
-    const __nv_bfloat162 inf = __bfloat162bfloat162(__ushort_as_bfloat16(0x7f80)), ninf = __hneg2(inf);
-    // ---- K: four lanes hold a row ----
+    // ---- K: four lanes hold a row, and each finds the parameters of one of the
+    // tile's groups that lie with them (or of one of two, twice) ----
+    {
+        __nv_bfloat162 ext[4];
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        uint32_t codes[NW], params[NG];
-#pragma unroll
-        for (int c = 0; c < NG; ++c) {
-            __nv_bfloat162 mn = inf, mx = ninf;
-            extremes(k[r][2 * c], mn, mx);
-            extremes(k[r][2 * c + 1], mn, mx);
-#pragma unroll
-            for (int off = 1; off < 4; off <<= 1) {
-                mn = __hmin2_nan(mn, shuffled(mn, off));
-                mx = __hmax2_nan(mx, shuffled(mx, off));
-            }
-            const Group g = group_of(mn, mx);
-            params[c] = g.word;
-#pragma unroll
-            for (int j = 2 * c; j < 2 * c + 2; ++j) {
-                const uint32_t *w = reinterpret_cast<const uint32_t *>(&k[r][j]);
-                codes[j] = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    codes[j] |= code_of(lo_f(w[e]), g) << (8 * e) | code_of(hi_f(w[e]), g) << (8 * e + 4);
-            }
+        for (int i = 0; i < 4; ++i) {
+            const int r = i & 1, c = NG == 2 ? i >> 1 : 0;  // (row, group)
+            ext[i] = __hmin2_nan(extremes(k[r][2 * c]), extremes(k[r][2 * c + 1]));
         }
-        uint8_t *row = dst + (gid + 8 * r) * (D / 2) + tig * (D / 8);
-        if constexpr (NW == 4)
-            *reinterpret_cast<uint4 *>(row) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
-        else
-            *reinterpret_cast<uint2 *>(row) = make_uint2(codes[0], codes[1]);
-        uint32_t *par = reinterpret_cast<uint32_t *>(dst + 16 * D) + (gid + 8 * r) * 2 * NG;
-        if (tig == r) {
+        float inv;
+        const uint32_t mine = params_of(joined<4, 1>(ext, lane), inv);
+        if (tig < 2 * NG)
+            *(reinterpret_cast<uint32_t *>(dst + 16 * D) + (gid + 8 * (tig & 1)) * 2 * NG + (tig >> 1)) = mine;
 #pragma unroll
-            for (int c = 0; c < NG; ++c) par[c] = params[c];
+        for (int r = 0; r < 2; ++r) {
+            uint32_t codes[NW];
+#pragma unroll
+            for (int c = 0; c < NG; ++c) {
+                const int from = (lane & ~3) + 2 * c + r;
+                const Group g(__shfl_sync(0xffffffffu, mine, from), __shfl_sync(0xffffffffu, inv, from));
+#pragma unroll
+                for (int j = 2 * c; j < 2 * c + 2; ++j) {
+                    const uint32_t *w = reinterpret_cast<const uint32_t *>(&k[r][j]);
+                    codes[j] = eight(four(with_next(based_codes(w[0], g), based_codes(w[1], g))),
+                                     four(with_next(based_codes(w[2], g), based_codes(w[3], g))));
+                }
+            }
+            uint8_t *row = dst + (gid + 8 * r) * (D / 2) + tig * (D / 8);
+            if constexpr (NW == 4)
+                *reinterpret_cast<uint4 *>(row) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
+            else
+                *reinterpret_cast<uint2 *>(row) = make_uint2(codes[0], codes[1]);
         }
     }
-    // ---- V: eight lanes hold a row's group ----
+    // ---- V: eight lanes hold a row's group, four rows and NG groups each ----
+    {
+        __nv_bfloat162 ext[8];
 #pragma unroll
-    for (int c = 0; c < NG; ++c) {
-        uint32_t codes[4] = {0, 0, 0, 0};
+        for (int i = 0; i < 8; ++i) ext[i] = extremes(v[i & 3][NG == 2 ? i >> 2 : 0]);
+        float inv;
+        const uint32_t mine = params_of(joined<8, 4>(ext, lane), inv);
+        if (gid < 4 * NG)
+            *(reinterpret_cast<uint32_t *>(dst + 16 * D) + (2 * tig + (gid & 1) + 4 * (gid & 2)) * 2 * NG + NG + (gid >> 2)) = mine;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            __nv_bfloat162 mn = inf, mx = ninf;
-            extremes(v[r][c], mn, mx);
+        for (int c = 0; c < NG; ++c) {
+            // tokens a, a + 8 (r = 0, 2) are a word's low half, a + 1 and a + 9 its high one
+            float2 half[2][4];
 #pragma unroll
-            for (int off = 4; off < 32; off <<= 1) {
-                mn = __hmin2_nan(mn, shuffled(mn, off));
-                mx = __hmax2_nan(mx, shuffled(mx, off));
+            for (int r = 0; r < 4; ++r) {
+                const int from = tig + 4 * (4 * c + r);
+                uint32_t word = __shfl_sync(0xffffffffu, mine, from);
+                const float i = __shfl_sync(0xffffffffu, inv, from);
+                // (a NaN group's codes are 0: the sums are other tokens' too)
+                const bool ok = (word & 0x7fffu) < 0x7f80u;
+                word = ok ? word : 0u;
+                const Group g(word, i);
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    const float2 b = based_codes(ok ? reinterpret_cast<const uint32_t *>(&v[r][c])[m] : 0u, g);
+                    half[r & 1][m] = r < 2 ? b : with_next(half[r & 1][m], b);
+                }
             }
-            const Group g = group_of(mn, mx);
-            if (gid == r)
-                *(reinterpret_cast<uint32_t *>(dst + 16 * D) + (2 * tig + (r & 1) + 4 * (r & 2)) * 2 * NG + NG + c) = g.word;
-            // tokens a, a + 1, a + 8, a + 9: nibbles 0, 4, 2, 6 and those after
-            const int nib = 4 * (r & 1) + (r & 2);
-            const uint32_t *w = reinterpret_cast<const uint32_t *>(&v[r][c]);
-#pragma unroll
-            for (int m = 0; m < 4; ++m)
-                codes[m] |= code_of(lo_f(w[m]), g) << (4 * nib) | code_of(hi_f(w[m]), g) << (4 * nib + 4);
+            *reinterpret_cast<uint4 *>(dst + 8 * D + 512 * c + 16 * lane) =
+                make_uint4(eight(four(half[0][0]), four(half[1][0])), eight(four(half[0][1]), four(half[1][1])),
+                           eight(four(half[0][2]), four(half[1][2])), eight(four(half[0][3]), four(half[1][3])));
         }
-        *reinterpret_cast<uint4 *>(dst + 8 * D + 512 * c + 16 * lane) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
     }
 }
 
