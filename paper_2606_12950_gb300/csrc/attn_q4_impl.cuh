@@ -41,8 +41,12 @@ constexpr int kQ4Threads = kQ4Warps * 32;
 constexpr int kQ4Stages = 2;
 template <int D>
 constexpr int kQ4Unit = D == 64 ? 4 : 2;  // tiles of a stage: 4608 bytes either way
-constexpr int kQ4Cost = 9, kBf16Cost = 32, kRunCost = 24;
-constexpr int kQ4MinPart = 64;            // a part's least cost: more than any tile's, so that each has one
+constexpr int kQ4Rebalance = 32;          // tiles (see Q4State::rebalance)
+constexpr int kQ4Cost = 9, kBf16Cost = 32;
+template <int D>
+constexpr int kRunCost = D == 64 ? 56 : 18;
+constexpr int kQ4Spread = 4;              // warps of a CTA with parts, where there are few parts
+constexpr int kQ4MinPart = 96;            // a part's least cost: more than any tile's, so that each has one
 
 struct Q4Args {
     const uint16_t *q;
@@ -76,6 +80,7 @@ inline size_t q4_smem_bytes(int G)
 }
 
 // A sequence's lengths, clamped to what the tables can hold.
+template <int D>
 struct Q4Seq {
     int32_t n, p;    // tokens; of them in 4 bits
     bool append;     // a new row can be appended
@@ -85,15 +90,16 @@ struct Q4Seq {
     __device__ int32_t cost() const { return n > 0 ? cost_to(tiles()) : 0; }
     __device__ int32_t cost_to(int32_t i) const
     {
-        return i > 0 ? kRunCost + kQ4Cost * min(i, p >> 4) + kBf16Cost * max(0, i - (p >> 4)) : 0;
+        return i > 0 ? kRunCost<D> + kQ4Cost * min(i, p >> 4) + kBf16Cost * max(0, i - (p >> 4)) : 0;
     }
 };
 
-__device__ __forceinline__ Q4Seq q4_seq(const Q4Args &a, int s)
+template <int D>
+__device__ __forceinline__ Q4Seq<D> q4_seq(const Q4Args &a, int s)
 {
     const int32_t n = a.lens[s], p = a.packed[s];
     const int32_t cap = a.max_blocks * a.bs, cap4 = a.max_blocks4 * a.bs;
-    Q4Seq q;
+    Q4Seq<D> q;
     q.n = min(max(n, 0), cap);
     q.p = min(min(max(p, 0), q.n), cap4) & ~15;
     q.append = n == q.n && n > q.p;
@@ -101,11 +107,12 @@ __device__ __forceinline__ Q4Seq q4_seq(const Q4Args &a, int s)
 }
 
 // the first tile of a run with no less than cost x before it
-__device__ __forceinline__ int32_t q4_tile_at(const Q4Seq &q, int32_t x)
+template <int D>
+__device__ __forceinline__ int32_t q4_tile_at(const Q4Seq<D> &q, int32_t x)
 {
     if (x <= 0) return 0;
     if (x >= q.cost()) return q.tiles();
-    x -= kRunCost;
+    x -= kRunCost<D>;
     const int32_t c4 = kQ4Cost * q.tiles4();
     const int32_t i = x <= c4 ? (int32_t)((uint32_t)(max(x, 0) + kQ4Cost - 1) / (uint32_t)kQ4Cost)
                               : q.tiles4() + (x - c4 + kBf16Cost - 1) / kBf16Cost;
@@ -377,6 +384,32 @@ struct Q4State {
         }
     }
 
+    // The tensor cores' sums lose what falls under an fp32 digit, always toward zero,
+    // and codes are never negative: sums of thousands of tiles drift (16384 tokens of flat
+    // weights in one warp: the output 1.3e-2 off, 65536 tokens 3.6e-2), and z undoes most of
+    // such a sum.  So now and then the sums' mean over a group's columns moves to the
+    // sum of p z, exactly but for fp32 rounding: what stays is as small as the output.
+    __device__ __forceinline__ void rebalance()
+    {
+#pragma unroll
+        for (int c = 0; c < NG; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float x = 0.f;
+#pragma unroll
+                for (int i = 4 * c; i < 4 * c + 4; ++i) x += fmaf(acc[i][2 + h], 0.0625f, acc[i][h]);
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+                x *= 1.f / 64.f;
+#pragma unroll
+                for (int i = 4 * c; i < 4 * c + 4; ++i) {
+                    acc[i][h] -= x;
+                    acc[i][2 + h] = fmaf(x, -16.f, acc[i][2 + h]);
+                }
+                z[c][h] = fmaf(x, 0x1p21f, z[c][h]);  // (an eighth each: eight lanes hold parts of the sum)
+            }
+    }
+
     // A tile of bf16 rows: its K's scores (rows, their first of this lane's, and
     // the tile's tokens with a weight, a bit each), then its V.  qrow as in begin;
     // where token `fresh` is one of the tile's, its row is k_new or v_new.
@@ -518,7 +551,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
         const int lo = min(S, tid * per), hi = min(S, lo + per);
         int64_t sum = 0;
         for (int s = lo; s < hi; ++s) {
-            const Q4Seq q = q4_seq(a, s);
+            const Q4Seq<D> q = q4_seq<D>(a, s);
             sum += (int64_t)q.cost() * a.Hkv;
             if (s % a.P == bid) {
                 const int32_t n = a.lens[s], p = a.packed[s];
@@ -548,7 +581,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
     // Equal shares of the cost: CTAs, and in a CTA its warps; a warp's is at least
     // kQ4MinPart.  (64-bit divisions take 0.5 us each: there is one where W needs it.)
     const int64_t W = __shfl_sync(0xffffffffu, upto, kQ4Warps - 1);
-    const int NC = (int)min((int64_t)a.P, (W / kQ4MinPart + kQ4Warps - 1) / kQ4Warps + (W < kQ4MinPart));
+    const int NC = (int)min((int64_t)a.P, (W / kQ4MinPart + kQ4Spread - 1) / kQ4Spread + (W < kQ4MinPart));
     if (bid >= NC || W == 0) return;
     const int64_t wq = (W >> 32) == 0 ? (int64_t)((uint32_t)W / (uint32_t)NC) : W / NC;
     const uint32_t wr = (uint32_t)(W - wq * NC);
@@ -559,7 +592,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
     auto warp_begin = [&](int w) { return w * nq + (int32_t)((uint32_t)(w * nr) / (uint32_t)nw); };
 
     struct Run {
-        Q4Seq q;
+        Q4Seq<D> q;
         int32_t s, g;
         int32_t begin;       // cost before it, from the CTA's start on
         int32_t i0, i1;      // this warp's tiles of it
@@ -575,7 +608,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
                 r.g = 0;
                 do {
                     if (r.begin >= w1 || ++r.s >= S) return false;
-                    r.q = q4_seq(a, r.s);
+                    r.q = q4_seq<D>(a, r.s);
                 } while (r.q.n == 0);
             }
             if (r.begin >= w1) return false;
@@ -594,10 +627,10 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
             const int t = 31 - __clz((int)__ballot_sync(0xffffffffu, base[k * 32 + lane] <= x));
             x -= base[k * 32 + t];  // cost from the sequence's start on
             run.s = (k * 32 + t) * per;
-            run.q = q4_seq(a, run.s);
+            run.q = q4_seq<D>(a, run.s);
             while (x >= (int64_t)run.q.cost() * a.Hkv) {
                 x -= (int64_t)run.q.cost() * a.Hkv;
-                run.q = q4_seq(a, ++run.s);
+                run.q = q4_seq<D>(a, ++run.s);
             }
             run.g = (int32_t)((uint32_t)x / (uint32_t)run.q.cost());
             run.begin = w0 - (int32_t)((uint32_t)x - (uint32_t)run.g * (uint32_t)run.q.cost());
@@ -661,7 +694,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
         bool dead = false;
         uint32_t stage = 0, parity = 0;
         for (; go; go = next(run)) {
-            const Q4Seq q = run.q;
+            const Q4Seq<D> q = run.q;
             const int32_t r = run.s * a.Hkv + run.g;
             const uint16_t *qrow = a.q + (int64_t)r * G * D;
             Q4State<D> st;
@@ -677,7 +710,9 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
                 __syncwarp();
                 issue();
             };
-            for (int32_t i = run.i0; i < end4; i += U) {
+            const int32_t i0 = run.i0;
+            for (int32_t i = i0; i < end4; i += U) {
+                if ((i - i0) % kQ4Rebalance == kQ4Rebalance - U) st.rebalance();
                 wait_phase(bar0 + stage * 8, parity, a.err, dead);
                 if (i + U <= end4)
                     st.template unit4<true>(ring + stage * STAGE, U, lane);

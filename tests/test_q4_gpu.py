@@ -318,3 +318,27 @@ def test_bad_lengths_and_entries_set_the_error_word():
         want, tol = c.reference(q, 0.09)
         ref().check(out[1], want[1], tol[1])  # the other sequence is as ever
         c.close()
+
+
+@pytest.mark.parametrize("d,n", [(64, 16400), (128, 16400)])
+def test_long_runs_in_one_warp_do_not_drift(d, n):
+    """As many contexts as warps, so that a warp takes each from end to end, with
+    nearly flat weights: the output is small beside what its sums are made of.  (All
+    read the same blocks.)  Rounding moves the output by 2^-8 of its norm at most,
+    and weights off by 2^-11 each, on their own, by 2^-11 sum(p s c) / sqrt(n) a
+    column: under 2^-9 of a mean of n values about as large."""
+    c = ref().PagedQ4([n], [n // 16 * 16 - 16], 1, 1, d, 16, 5, append=False)
+    S = 2560
+    table, table4 = c.table.expand(S, -1).contiguous(), c.table4.expand(S, -1).contiguous()
+    lens, packed = c.lens.expand(S).contiguous(), c.packed.expand(S).contiguous()
+    q = (c.normal(S, 1, d).float() * 0.05).to(torch.bfloat16)
+    out = torch.empty(S, 1, d, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(K.kv_q4_workspace_bytes(c.h, 1, S, 1, c.max_blocks), dtype=torch.uint8, device="cuda")
+    K.paged_decode_attn_q4(c.h, 0, 1, q, None, None, out, table, lens, c.max_blocks, table4, packed, c.max_blocks4, S, 1,
+                           d ** -0.5, ws, ws.numel())
+    torch.cuda.synchronize()
+    k, v = torch.cat([ref().values(c.rows[0][:, :, : int(c.p[0])]), c.rows[0][:, :, int(c.p[0]) :].double()], 2)[:, 0]
+    want = torch.softmax(q[:, 0].double() @ k.T * d ** -0.5, -1) @ v
+    off = ((out[:, 0].double() - want).norm(dim=-1) / want.norm(dim=-1)).max().item()
+    assert off <= 2.0 ** -8 + 2.0 ** -9, off
+    c.close()
