@@ -1,6 +1,7 @@
-"""One attention layer of a server whose chats outgrow their window: rotary
-positions, a sliding window with sinks, forks, and a page cache that gives back
-what the window has left behind.
+"""One attention layer of a server: WindowedLayer, whose chats outgrow their
+window (rotary positions, a sliding window with sinks, forks, and a page cache
+that gives back what the window has left behind), and PackedLayer, whose chats
+keep their whole context (heads normed, the older pages in 4 bits).
 
 PyTorch supplies device memory and the stream; every step of the path runs in
 libkvpool's kernels: the rotary append, prompt and decode attention over the
@@ -89,7 +90,7 @@ class WindowedLayer:
             else:
                 st.wait_event(self.done)
             # (what torch's allocator has from another stream, it takes back after this one)
-            for x in (self.table, self.lens, self.ws, self.rotary.steps):
+            for x in self._kept():
                 x.record_stream(st)
         try:
             if st.cuda_stream == here.cuda_stream:
@@ -102,6 +103,10 @@ class WindowedLayer:
                     yield st
         finally:
             self._leave(st)
+
+    def _kept(self) -> tuple:
+        """The layer's own device tensors."""
+        return self.table, self.lens, self.ws, self.rotary.steps
 
     def _workspace(self, n: int) -> torch.Tensor:
         if n > self.ws.numel():
@@ -221,3 +226,160 @@ class WindowedLayer:
         self.tab.close()
         if self.own:
             self.pool.close()
+
+
+class PackedLayer(WindowedLayer):
+    """Slots of one layer that see their whole context, of which the older pages
+    are held in 4 bits: every full page but those that the last `keep` tokens
+    reach (at least 1) is packed at the end of the call that filled it.
+
+    n_pages: the pool's size in bf16 pages, each of which has room for three
+    packed ones (pool: a pool of the caller's whose layouts are (Hkv, d) and (Hkv,
+    d | KV_Q4)).  norm: the heads' norms (kvpool.HeadNorm), or None.  The rest, the
+    streams too, is as WindowedLayer says.  Where the pool has no page left for
+    packing, a slot's pages stay in bf16 until a later call finds one.  A prompt on a chat
+    with packed pages reads them through bf16 copies, which it needs pages for
+    while it runs.
+    """
+
+    def __init__(self, n_pages: int, Hq: int, Hkv: int, d: int, bs: int, max_seqs: int, max_tokens: int, keep: int, freqs,
+                 norm=None, interleaved: bool = False, magnitude: float = 1.0, scale: float | None = None, pool=None):
+        if keep < 1:
+            raise ValueError("keep must be at least 1")
+        own = pool is None
+        if own:
+            pool = DevicePool(32 * n_pages, Hkv * bs * d // 8, bs, [(Hkv, d), (Hkv, d | K.KV_Q4)])
+        self.norm, self.keep = norm, keep
+        self.tab4 = K.SeqTab(pool.handle, 1, max_seqs, -(-max_tokens // bs))
+        self.table4 = torch.empty((max_seqs, self.tab4.max_blocks), dtype=torch.int32, device=pool.device)
+        self.lens4 = torch.empty(max_seqs, dtype=torch.int32, device=pool.device)
+        super().__init__(n_pages, Hq, Hkv, d, bs, max_seqs, max_tokens, 0, 0, freqs, interleaved, magnitude, scale, pool)
+        self.own = own
+        n = K.kv_q4_workspace_bytes(pool.handle, 1, max_seqs, Hq, self.tab.max_blocks)
+        self._workspace(n)
+
+    def _kept(self) -> tuple:
+        weights = () if self.norm is None else tuple(w for w in self.norm.weights if w is not None)
+        return super()._kept() + (self.table4, self.lens4) + weights
+
+    def _append(self, q, k, v, starts, T, stream):
+        if self.norm is None:
+            return super()._append(q, k, v, starts, T, stream)
+        q_out = torch.empty((T, self.Hq, self.d), dtype=torch.bfloat16, device=q.device)
+        K.kv_append_rotary_norm(self.pool.handle, 0, self.rotary, self.norm, q, q.stride(0), q_out, k, k.stride(0), v,
+                                v.stride(0), None, starts, T, self.table, self.lens, self.tab.max_blocks, self.S, self.Hq,
+                                stream)
+        return q_out
+
+    def _room(self, call):
+        """call(), once more with the pages that the other kind has free where there
+        are none (a pool keeps those until kv_pool_trim)."""
+        try:
+            return call()
+        except K.KVError as e:
+            if e.code != K.KV_ERR_OUT_OF_BLOCKS:
+                raise
+        K.kv_pool_trim(self.pool.handle)
+        return call()
+
+    def _pack(self, slots, st) -> None:
+        try:
+            self._room(lambda: self.tab.pack(self.tab4, slots, self.keep, st))
+            return
+        except K.KVError as e:
+            if e.code != K.KV_ERR_OUT_OF_BLOCKS:
+                raise
+        # a few pages at a time, oldest first: those that become free make room for the next
+        lens, done = self.tab.lens(), self.tab4.lens()
+        for s in slots:
+            want, have = max(0, int(lens[s]) - self.keep) // self.bs, int(done[s]) // self.bs
+            while have < want:
+                K.kv_pool_trim(self.pool.handle)
+                st4 = K.kv_pool_stats(self.pool.handle)
+                n = min(want - have, st4["blocks_capacity"][1] - st4["blocks_used"][1])
+                if n == 0:
+                    return  # they stay as they are until there is room
+                self.tab.pack(self.tab4, [s], int(lens[s]) - (have + n) * self.bs, st)
+                have += n
+
+    def prompt(self, counts, q, k, v, stream=None) -> torch.Tensor:
+        """As WindowedLayer.prompt; KVError (KV_ERR_OUT_OF_BLOCKS) also where the
+        pool has no pages for copies of packed ones."""
+        counts = np.asarray(counts, dtype=np.int64)
+        lens, T = self.tab.lens(), int(counts.sum())
+        if counts.shape != (self.S,) or counts.min() < 0 or q.shape[0] != T:
+            raise ValueError("counts must have a number for each slot, and q a row for each new token")
+        if T == 0:
+            return torch.empty((0, self.Hq, self.d), dtype=torch.bfloat16, device=q.device)
+        self._check_rows(T, q, k, v)
+        slots = np.nonzero(counts)[0]
+        for s in slots:
+            self._room(lambda: self.tab.reserve(int(s), int(lens[s] + counts[s])))
+        table4, lens4 = self.tab4.host()
+        packed = [(s, int(lens4[s]) // self.bs) for s in slots if lens4[s]]
+        copies = self._room(lambda: K.kv_alloc_blocks(self.pool.handle, 0, sum(n for _, n in packed)))
+        try:
+            for s in slots:
+                self.tab.set_len(int(s), int(lens[s] + counts[s]))
+            with self._on(stream, q, k, v) as st:
+                out = torch.empty((T, self.Hq, self.d), dtype=torch.bfloat16, device=q.device)
+                starts = torch.from_numpy(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)).to(q.device)
+                self.tab.sync(self.table, self.lens, st)
+                table, ctx = self.table, self.lens
+                if packed:
+                    K.kv_unpack_blocks(self.pool.handle, 1, 0, np.concatenate([table4[s, :n] for s, n in packed]), copies, st)
+                    whole, at = self.tab.host()[0], 0
+                    for s, n in packed:
+                        whole[s, :n] = copies[at : at + n]
+                        at += n
+                    # (the other slots have no rows here, and what they see is not asked for)
+                    ctx = torch.from_numpy(np.where(counts > 0, lens + counts, 0).astype(np.int32)).to(q.device)
+                    table = torch.from_numpy(whole).to(q.device)
+                x = self._append(q, k, v, starts, T, st)
+                n = K.kv_prompt_workspace_bytes(self.pool.handle, 0, self.S, self.Hq, T, int(counts.max()),
+                                                self.tab.max_blocks, 0, 0)
+                K.paged_prompt_attn(self.pool.handle, 0, x, out, starts, T, int(counts.max()), table, ctx,
+                                    self.tab.max_blocks, self.S, self.Hq, self.scale, 0, 0, self._workspace(n), n, st)
+                self._pack(slots, st)
+        finally:
+            if copies.size:
+                K.kv_free_blocks(self.pool.handle, 0, copies)
+        return self._given(out, stream)
+
+    def step(self, q, k, v, stream=None) -> torch.Tensor:
+        """As WindowedLayer.step."""
+        self._check_rows(self.S, q, k, v)
+        self._room(self.tab.advance)
+        with self._on(stream, q, k, v) as st:
+            self.tab.sync(self.table, self.lens, st)
+            self.tab4.sync(self.table4, self.lens4, st)
+            x = self._append(q, k, v, None, self.S, st)
+            out = torch.empty_like(x)
+            K.paged_decode_attn_q4(self.pool.handle, 0, 1, x, None, None, out, self.table, self.lens, self.tab.max_blocks,
+                                   self.table4, self.lens4, self.tab4.max_blocks, self.S, self.Hq, self.scale, self.ws,
+                                   self.ws.numel(), st)
+            self._pack(np.nonzero(self.tab.lens())[0], st)
+        return self._given(out, stream)
+
+    def fork(self, src: int, dsts, stream=None) -> None:
+        dsts = np.asarray(dsts, dtype=np.int32)
+        self._room(lambda: super(PackedLayer, self).fork(src, dsts, stream))
+        try:
+            self.tab4.fork(src, dsts)  # whole pages, by reference
+        except K.KVError:
+            for s in dsts:
+                self.tab.release(int(s))
+            raise
+
+    def release(self, s: int) -> None:
+        self.tab.release(s)
+        self.tab4.release(s)
+
+    def packed_used(self) -> int:
+        """Pages held in 4 bits (pages_used: in bf16)."""
+        return K.kv_pool_stats(self.pool.handle)["blocks_used"][1]
+
+    def close(self) -> None:
+        torch.cuda.synchronize()
+        self.tab4.close()
+        super().close()
