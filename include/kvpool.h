@@ -240,8 +240,9 @@ int kv_copy_blocks(kv_pool *pool, int layout, int n, const int32_t *src, const i
  * of its layout, no destination appears twice.  A source may appear again.
  * Packing what was unpacked gives the same values where bf16 holds s c + z.
  * The pairs travel as kernel parameters (2040 a launch): the arrays may change
- * right after the call.  Errors also: KV_ERR_UNSUPPORTED (a layout that is
- * not of that kind), KV_ERR_CUDA.
+ * right after the call.  Errors also: KV_ERR_INVALID_ARG where the current device
+ * is not the pool's, KV_ERR_UNSUPPORTED (a layout that is not of that kind),
+ * KV_ERR_CUDA.
  */
 int kv_pack_blocks(kv_pool *pool, int layout, int q4_layout, int n, const int32_t *src, const int32_t *dst,
                    void *stream);
@@ -682,10 +683,12 @@ int kv_append_rotary(kv_pool *pool, int layout, const kv_rotary *rot, const uint
  * heads, 16-byte aligned device arrays; NULL: those heads are not normed.
  * offset: 0, or 1 where the checkpoint holds weights about 0.  Everything is
  * in fp32, the sum of squares too, with one rounding to bf16 at the end, also
- * for the columns past rot_dim.  A row of zeros with eps = 0 gives NaN; a row
- * with an infinity or a NaN gives NaN.  All else, the strides, q == q_out,
+ * for the columns past rot_dim.  A row of zeros with eps = 0 and one with a NaN
+ * give NaN; one whose sum of squares leaves fp32 (values near 2^64) gives zeros,
+ * and NaN where it holds an infinity.  All else, the strides, q == q_out,
  * ragged chunks and errors, is as there; KV_ERR_INVALID_ARG also for eps < 0
- * or not finite, KV_ERR_UNSUPPORTED for head dims above 256.
+ * or not finite and where the current device is not the pool's,
+ * KV_ERR_UNSUPPORTED for head dims above 256.
  */
 typedef struct kv_head_norm {
     const uint16_t *q_weight;
@@ -798,8 +801,8 @@ int paged_decode_attn_window(kv_pool *pool, int layout, const uint16_t *q, const
  * V groups with s below 2^-60 count as constant.
  * The result of a call does not depend on where its blocks lie.
  * Workspace: kv_q4_workspace_bytes (256-byte aligned, not initialised).
- * Errors: those of paged_decode_attn; layout and q4_layout have the same heads
- * and columns, else KV_ERR_INVALID_ARG.
+ * Errors: those of paged_decode_attn; KV_ERR_INVALID_ARG also where layout and
+ * q4_layout differ in heads or columns or the current device is not the pool's.
  */
 int kv_q4_workspace_bytes(const kv_pool *pool, int q4_layout, int S, int Hq, int max_blocks, size_t *out_bytes);
 

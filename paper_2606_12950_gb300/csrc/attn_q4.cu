@@ -31,7 +31,7 @@ int q4_shape(const kv_pool *p, int q4_layout, int S, int Hq, int max_blocks, int
     if ((int64_t)max_blocks * p->desc.block_size >= INT32_MAX - kQ4Tile) return KV_ERR_INVALID_ARG;
     const int64_t tiles = ((int64_t)max_blocks * p->desc.block_size + kQ4Tile - 1) / kQ4Tile;
     if (tiles * L.num_kv_heads * kvp::kBf16Cost >= INT32_MAX) return KV_ERR_INVALID_ARG;
-    if ((int64_t)S * L.num_kv_heads >= INT32_MAX) return KV_ERR_INVALID_ARG;
+    if (S * tiles * L.num_kv_heads >= INT32_MAX) return KV_ERR_INVALID_ARG;  // (a CTA's share of the cost, too)
     return KV_OK;
 }
 
@@ -76,6 +76,7 @@ int paged_decode_attn_q4(kv_pool *p, int layout, int q4_layout, const uint16_t *
     if (!aligned16(q) || !aligned16(out)) return KV_ERR_INVALID_ARG;
     if ((k_new || v_new) && (!k_new || !v_new || !aligned16(k_new) || !aligned16(v_new))) return KV_ERR_INVALID_ARG;
     if (p->sm_count <= 0) return KV_ERR_CUDA;
+    if (!kvp_on_device(p)) return KV_ERR_INVALID_ARG;
     rc = run(D, G, nullptr, p->sm_count, nullptr, false, &P);
     if (rc) return rc;
     size_t part_off;

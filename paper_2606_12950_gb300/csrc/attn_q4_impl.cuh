@@ -286,11 +286,11 @@ struct Q4State {
         }
     }
 
-    // a unit of `tiles` tiles in 4 bits (FULL: of kQ4Unit)
-    template <bool FULL>
-    __device__ __forceinline__ void unit4(const uint8_t *stage, int tiles, int lane)
+    // U tiles in 4 bits
+    template <int U>
+    __device__ __forceinline__ void tiles4(const uint8_t *stage, int lane)
     {
-        constexpr int U = kQ4Unit<D>, TILE = kQ4TileBytes<D>;
+        constexpr int TILE = kQ4TileBytes<D>;
         const int gid = lane >> 2, tig = lane & 3;
         float x[U][4];
         uint32_t vp[U][2][NG];
@@ -298,7 +298,7 @@ struct Q4State {
         uint32_t top = 0;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (FULL || u < tiles) {
+            {
                 const uint8_t *tile = stage + u * TILE;
                 uint32_t ka[NW], kb[NW], kp[2][NG];
                 const uint8_t *ra = tile + gid * (D / 2) + tig * (D / 8), *rb = ra + 8 * (D / 2);
@@ -357,7 +357,7 @@ struct Q4State {
         raise(fmaf(x0, factor[0], L), fmaf(x1, factor[1], L));
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (FULL || u < tiles) {
+            {
                 const uint8_t *tile = stage + u * TILE;
                 const float p0 = fast_exp2(fmaf(x[u][0], factor[0], -m[0])), p1 = fast_exp2(fmaf(x[u][1], factor[1], -m[1]));
                 const float p2 = fast_exp2(fmaf(x[u][2], factor[0], -m[0])), p3 = fast_exp2(fmaf(x[u][3], factor[1], -m[1]));
@@ -715,9 +715,9 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
                 if ((i - i0) % kQ4Rebalance == kQ4Rebalance - U) st.rebalance();
                 wait_phase(bar0 + stage * 8, parity, a.err, dead);
                 if (i + U <= end4)
-                    st.template unit4<true>(ring + stage * STAGE, U, lane);
+                    st.template tiles4<U>(ring + stage * STAGE, lane);
                 else
-                    st.template unit4<false>(ring + stage * STAGE, end4 - i, lane);
+                    for (int32_t u = i; u < end4; ++u) st.template tiles4<1>(ring + stage * STAGE + (u - i) * TILE, lane);
                 unit_done();
             }
             for (int32_t i = max(run.i0, q.tiles4()); i < run.i1; ++i) {

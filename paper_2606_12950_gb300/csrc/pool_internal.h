@@ -8,6 +8,7 @@
 #include <vector>
 
 #include <cuda.h>
+#include <cuda_runtime.h>
 
 #include "kvpool.h"
 
@@ -84,4 +85,12 @@ inline bool kvp_block_in_pool(const kv_pool *p, int layout, int64_t id)
         if (!p->vmm.mapped[(size_t)c]) return false;
     }
     return true;
+}
+
+// False where the current device is not the pool's: a launch would run beside the
+// pool's memory.  (Without a GPU nothing is launched.)
+inline bool kvp_on_device(const kv_pool *p)
+{
+    int device = -1;
+    return p->sm_count <= 0 || (cudaGetDevice(&device) == cudaSuccess && device == p->device);
 }

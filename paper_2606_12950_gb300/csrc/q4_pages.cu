@@ -357,7 +357,7 @@ int pack_call(kv_pool *p, int layout, int q4_layout, int n, const int32_t *src, 
     if (rc) return rc;
     if (n < 0) return KV_ERR_INVALID_ARG;
     if (n == 0) return KV_OK;
-    if (!src || !dst) return KV_ERR_INVALID_ARG;
+    if (!src || !dst || !kvp_on_device(p)) return KV_ERR_INVALID_ARG;
     const int from = unpack ? q4_layout : layout, to = unpack ? layout : q4_layout;
     {
         // every id a live block of its layout, no destination twice.  Marks go to
@@ -426,6 +426,7 @@ int kv_seq_pack(kv_seqtab *t, kv_seqtab *t4, int n, const int32_t *slots, int ke
             }
         }
         if (src.empty()) return KV_OK;
+        if (!kvp_on_device(t->pool)) return KV_ERR_INVALID_ARG;
         const int m = (int)src.size();
         dst.resize((size_t)m);
         rc = kv_alloc_blocks(t4->pool, t4->layout, m, dst.data());

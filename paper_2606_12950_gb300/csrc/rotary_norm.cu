@@ -250,6 +250,7 @@ extern "C" int kv_append_rotary_norm(kv_pool *p, int layout, const kv_rotary *ro
     const kv_layout &L = p->desc.layouts[layout];
     if (L.head_dim > kMaxNormDim) return KV_ERR_UNSUPPORTED;
     if (!go) return KV_OK;
+    if (!kvp_on_device(p)) return KV_ERR_INVALID_ARG;
     NormArgs a{};
     a.q = q;
     a.k = k;

@@ -342,3 +342,78 @@ def test_long_runs_in_one_warp_do_not_drift(d, n):
     off = ((out[:, 0].double() - want).norm(dim=-1) / want.norm(dim=-1)).max().item()
     assert off <= 2.0 ** -8 + 2.0 ** -9, off
     c.close()
+
+
+def test_packed_blocks_are_copied_whole_and_moved():
+    x = normal(7, 2, 2, 16, 128, seed=1).to(torch.bfloat16)
+    b = Blocks(x)
+    K.kv_pack_blocks(b.h, 0, 1, b.a, b.q)
+    raw = [b.buf[int(i) * b.block // 32 :][: b.block * 9 // 32].clone() for i in b.q]
+    before = b.buf.clone()
+    K.kv_copy_blocks(b.h, 1, [b.q[0], b.q[1], b.q[2]], [b.q[5], b.q[6], b.q[3]], [16, 0, 16])
+    torch.cuda.synchronize()
+    for i, want in ((5, 0), (6, 6), (3, 2), (4, 4)):
+        assert torch.equal(b.buf[int(b.q[i]) * b.block // 32 :][: b.block * 9 // 32], raw[want])
+    for i in (5, 3):
+        at = int(b.q[i]) * b.block // 32
+        before[at : at + b.block * 9 // 32] = b.buf[at : at + b.block * 9 // 32]
+    assert torch.equal(before, b.buf)  # not a byte beside them
+    b.close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_tables_of_packed_blocks_compacted_and_forked(d):
+    """Live packed blocks move together: the same attention afterwards, from fewer
+    superpages; forks read the same blocks."""
+    Hkv, Hq, bs, S = 2, 4, 16, 4
+    block = 2 * Hkv * bs * d * 2
+    buf = torch.zeros(64 * block, dtype=torch.uint8, device="cuda")
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    h = K.kv_pool_create(buf, buf.numel(), bs, [(Hkv, d), (Hkv, d | K.KV_Q4)], err, page_bytes=block // 32, shuffle_seed=5)
+    t, q4 = K.SeqTab(h, 0, S, 12), K.SeqTab(h, 1, S, 12)
+    n = [150, 97, 33, 0]
+    for s in range(S - 1):
+        t.reserve(s, n[s])
+        t.set_len(s, n[s])
+    page = block // 32
+    for s in range(S - 1):
+        for j, i in enumerate(t.host()[0][s, : -(-n[s] // bs)]):
+            buf[int(i) * page :][:block].view(torch.bfloat16)[:] = normal(block // 2, seed=100 * s + j).to(torch.bfloat16)
+    # three a superpage: slot 0's first lies with two of slot 1's, its last two with room for one
+    assert t.pack(q4, [2, 3], 1) == 2 and t.pack(q4, [1, 0], 1) == 15
+    t.release(2)
+    q4.release(2)
+    t.release(1)
+    q4.release(1)
+    q4.fork(0, [3])
+    t.fork(0, [3])
+    table, lens = torch.empty(S, 12, dtype=torch.int32, device="cuda"), torch.empty(S, dtype=torch.int32, device="cuda")
+    table4, lens4 = table.clone(), lens.clone()
+    ws = torch.empty(K.kv_q4_workspace_bytes(h, 1, S, Hq, 12), dtype=torch.uint8, device="cuda")
+    q = normal(S, Hq, d, seed=9).to(torch.bfloat16)
+    q[3] = q[0]
+
+    def attend():
+        out = torch.empty(S, Hq, d, dtype=torch.bfloat16, device="cuda")
+        t.sync(table, lens)
+        q4.sync(table4, lens4)
+        K.paged_decode_attn_q4(h, 0, 1, q, None, None, out, table, lens, 12, table4, lens4, 12, S, Hq, 0.1, ws, ws.numel())
+        torch.cuda.synchronize()
+        return out
+
+    a = attend()
+    # (another split over the warps: both off by 2^-8 of the value and 2^-11 of sum(p s c),
+    # which is below a span, 8 here)
+    assert ((a[0].float() - a[3].float()).abs() <= 2.0 ** -7 * a[0].float().abs() + 2.0 ** -7).all()
+    assert (a[1:3] == 0).all() and torch.isfinite(a).all() and (a[0] != 0).any()
+    ids = q4.host()[0].copy()
+    assert K.kv_pool_compact(h) > 0
+    assert (q4.host()[0] != ids).any()
+    free = K.kv_pool_stats(h)["pages_unassigned"]
+    K.kv_pool_trim(h)
+    assert K.kv_pool_stats(h)["pages_unassigned"] > free
+    assert torch.equal(attend(), a)
+    assert K.kv_pool_get_error(h, None) == 0
+    t.close()
+    q4.close()
+    K.kv_pool_destroy(h)
