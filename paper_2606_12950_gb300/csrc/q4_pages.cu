@@ -30,7 +30,7 @@
 
 namespace {
 
-constexpr int kPackThreads = 128;
+constexpr int kPackThreads = 128, kUnpackThreads = 256;
 constexpr float kSpanLimit = 0x1p80f;   // spans from here on are NaN
 constexpr float kScaleLeast = 0x1p-100f;  // scales below are 0
 
@@ -127,7 +127,7 @@ __device__ __forceinline__ uint32_t eight(float lo, float hi)
 }
 
 template <int D, int N>
-__global__ void __launch_bounds__(kPackThreads) pack_blocks_kernel(const __grid_constant__ PackParams<N> p)
+__global__ void __launch_bounds__(kPackThreads, 6) pack_blocks_kernel(const __grid_constant__ PackParams<N> p)
 {
     constexpr int NG = D / kQ4Group, NW = D / 32, TILE = kQ4TileBytes<D>;
     kvp::grid_dependency_wait();
@@ -231,12 +231,12 @@ __device__ __forceinline__ uint32_t values_of(uint32_t w, int a, int b, float s,
 }
 
 template <int D, int N>
-__global__ void __launch_bounds__(kPackThreads) unpack_blocks_kernel(const __grid_constant__ PackParams<N> p)
+__global__ void __launch_bounds__(kUnpackThreads) unpack_blocks_kernel(const __grid_constant__ PackParams<N> p)
 {
     constexpr int NG = D / kQ4Group, NW = D / 32, TILE = kQ4TileBytes<D>;
     kvp::grid_dependency_wait();
     kvp::grid_launch_dependents();
-    const int unit = blockIdx.y * (kPackThreads / 32) + (threadIdx.x >> 5);  // (head, tile)
+    const int unit = blockIdx.y * (kUnpackThreads / 32) + (threadIdx.x >> 5);  // (head, tile)
     if (unit >= p.Hkv * p.tiles) return;
     const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
     const int64_t kv = (int64_t)p.Hkv * p.tiles * 32 * D;
@@ -302,13 +302,13 @@ int pack_launch(const kv_pool *p, int layout, int n, const int32_t *src, const i
         c.at[i][0] = src[i];
         c.at[i][1] = dst[i];
     }
-    const int per_cta = kPackThreads / 32;
+    const int threads = unpack ? kUnpackThreads : kPackThreads, per_cta = threads / 32;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)n, (unsigned)((c.Hkv * c.tiles + per_cta - 1) / per_cta));
-    cfg.blockDim = dim3(kPackThreads);
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.stream = st;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
@@ -367,13 +367,10 @@ int pack_call(kv_pool *p, int layout, int q4_layout, int n, const int32_t *src, 
             return id >= 0 && id < p->n_pages && p->owner[(size_t)id] == l && p->refcnt[(size_t)id] > 0;
         };
         bool ok = true;
-        for (int i = 0; i < n && ok; ++i) ok = live(src[i], from) && live(dst[i], to);
         int marked = 0;
         for (; ok && marked < n; ++marked) {
-            if (p->tally[(size_t)dst[marked]]) {
-                ok = false;
-                break;
-            }
+            ok = live(src[marked], from) && live(dst[marked], to) && !p->tally[(size_t)dst[marked]];
+            if (!ok) break;
             p->tally[(size_t)dst[marked]] = 1;
         }
         for (int i = 0; i < marked; ++i) p->tally[(size_t)dst[i]] = 0;
