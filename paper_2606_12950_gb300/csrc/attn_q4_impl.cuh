@@ -21,12 +21,33 @@
 // of the bf16 kernel do.
 //
 // Work split: a tile is 16 tokens of a (sequence, KV head) run; it costs 9 where
-// it is in 4 bits and 32 in bf16 (its bytes).  The batch's tiles, in order, are cut
-// into parts of equal cost, one a CTA, and those into equal ones, one a warp.  A
-// run inside a CTA leaves its output, others a record a CTA for the combine (the
-// warps' states merged in shared memory).  Each warp streams its tiles
-// through its own ring of shared-memory stages, a bulk copy each (of K or V, where
-// they are in bf16).
+// it is in 4 bits and 32 in bf16 (its bytes), a run's first one kRunCost more (what
+// starts and ends a run).  The batch's tiles, in order, are cut into parts of equal
+// cost, one a CTA, and those into equal ones, one a warp.  A run inside a CTA leaves
+// its output, others a record a CTA for the combine (the warps' states merged in
+// shared memory).  Each warp streams its tiles through its own ring of two stages, a
+// bulk copy a tile (or K or V, where they are in bf16).
+//
+// Bound by HBM in the long run, by its start and end in short ones.  Steady state (the
+// slope from 240000 to 480000 tokens, 32 q / 8 KV heads of 128): 6.53 TB/s, 0.96 of the
+// measured copy; 16 single heads of 64 5.93.  Around it a call spends about 12 us:
+// the lengths' round trip and the split 2, the table's and the first tiles' 3, warps
+// that end apart 3, merges and the combine 4.  Calls (us; floor at 6.78 TB/s):
+//   250 sequences, 40 q / 8 KV heads of 128, 700 MB    119.1 (103)
+//   64 sequences, 32 / 8 of 128, 242 MB                 48.6 (35.7)
+//   one of 100000 tokens, 32 / 8 of 128, 115 MB         30.0 (17.0)
+//   40 sequences, 16 heads of 64, 140 MB                34.2 (20.7)
+// A tile of 128 columns takes 255 issue slots of the 396 that an SM quarter has while
+// HBM brings it; half of them are masks and shifts of codes, which is why the masked
+// words must be operands as they are.  (With a subtraction per pair, or codes as bf16,
+// they would be twice as many.)
+//
+// What was measured on the way, 64 / 250 sequences: a CTA of 8 warps twice on an SM 54.0
+// / 123.9 and one of 16 48.2 / 117.4, as the CTA that came first ran 25% ahead and left
+// the other half the SM; warps' records for the combine, not CTAs', 60.6 / 145.5; bf16
+// tiles read into registers, without the ring, 54.0 / 136.7; the last CTA of a run
+// merging its records, in place of the combine, 52.7 / 123.5 (counted by compare and
+// swap) and 53.9 / 124.4 (flags), as the fences at a CTA's end took 7 us.
 #pragma once
 
 #include <cuda_fp16.h>
