@@ -198,7 +198,7 @@ struct Q4State {
     static constexpr int NG = D / kQ4Group, NW = D / 32, NM = D / 16;
     uint32_t qh[NW][4];     // q, head g: words of 8 columns as the K words pair them, fp16
     uint32_t qsum[2];       // 2^-24 times the scaled q's sums over groups, head g, as the z's operand
-    float factor[2];        // of the scores, to base-2 exponents; not negative
+    float factor[2];        // of the scores, to base-2 exponents; |scale| goes here, its sign to q
     float m[2], l[2];
     float z[NG][2];         // sums of p z over this lane's tokens
     float acc[NM][4];       // sums of p s c: row pairs (e, e + 1), odd columns times 16, all times 2^-24
@@ -578,7 +578,8 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
                 const int32_t n = a.lens[s], p = a.packed[s];
                 if (n != q.n || p != q.p || (a.k_new && n > 0 && !q.append)) report(a.err, KV_ERR_DEVICE_BOUNDS);
                 if (q.n == 0) {  // no softmax: zeros
-                    for (int i = 0; i < a.Hkv * G * D; ++i) a.out[(int64_t)s * a.Hkv * G * D + i] = 0;
+                    uint4 *row = reinterpret_cast<uint4 *>(a.out + (int64_t)s * a.Hkv * G * D);
+                    for (int i = 0; i < a.Hkv * G * (D / 8); ++i) row[i] = make_uint4(0u, 0u, 0u, 0u);
                     for (int g = 0; g < a.Hkv; ++g) a.ws_run[(int64_t)s * a.Hkv + g] = make_int2(0, 0);
                 }
             }
@@ -830,7 +831,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
 
 }  // namespace kvp
 
-// one entry per head dim: the CTAs that are resident at once (launch false), or
-// both kernels
+// one entry per head dim: the CTAs that are resident at once (launch false), or the
+// kernel and its combine
 int kvp_q4_attn_d64(int G, const kvp::Q4Args *a, int sm_count, cudaStream_t st, bool launch, int *P_out);
 int kvp_q4_attn_d128(int G, const kvp::Q4Args *a, int sm_count, cudaStream_t st, bool launch, int *P_out);

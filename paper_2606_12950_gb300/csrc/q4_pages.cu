@@ -11,7 +11,7 @@
 // Bound by HBM, and close to it by instructions: a value is read in 2 bytes and written
 // in 9/16, or the other way.  2040 blocks of 64 KB (171 MB) are packed in 29.6 us (5.8
 // TB/s; 36.7 one value an instruction, every lane finding its groups' parameters) and
-// unpacked in 24; 4000 packed and read back 111.6 us (671 MB, 6.0 TB/s), 6000 read back
+// unpacked in 26; 4000 packed and read back 111.6 us (671 MB, 6.0 TB/s), 6000 read back
 // 80.5 (504 MB, 6.26 TB/s).
 // A warp takes a tile (16 tokens of a KV head, K and V): K's rows as 16-byte
 // chunks of 8 columns, four lanes a row, V's eight lanes a row, so that each lane

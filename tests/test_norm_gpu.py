@@ -69,7 +69,7 @@ def verify(n, nq, Hq, Hkv, d, bs, rot, interleaved=False, eps=1e-6, offset=0.0, 
 
 
 @pytest.mark.parametrize("interleaved", [False, True])
-@pytest.mark.parametrize("d,rot", [(64, 64), (64, 16), (128, 128), (128, 64), (128, 48), (128, 0), (80, 32), (256, 256), (8, 0)])
+@pytest.mark.parametrize("d,rot", [(64, 64), (64, 16), (128, 128), (128, 64), (128, 48), (128, 0), (80, 32), (256, 256), (8, 0), (24, 16), (40, 32)])
 @pytest.mark.parametrize("Hq,Hkv", [(4, 2), (1, 1), (40, 8)])
 def test_layouts(interleaved, d, rot, Hq, Hkv):
     verify([70, 3, 17, 16], [33, 3, 1, 16], Hq, Hkv, d, 16, rot, interleaved)

@@ -184,3 +184,43 @@ def test_attention_refusals():
     assert code(lambda: call(Hq=6)) == U  # three heads a KV head
     assert code(K.kv_q4_workspace_bytes, h, 0, 1, 4, 4) == U and code(K.kv_q4_workspace_bytes, h, 1, 1, 3, 4) == I
     K.kv_pool_destroy(h)
+
+
+def test_vmm_pools_and_layouts_of_several_models():
+    """Chunks follow superpages of three packed blocks; two models' packed and bf16
+    blocks in one pool."""
+    class Backing:
+        def __init__(self):
+            self.mapped = set()
+
+        def map(self, off, n):
+            self.mapped.add(off)
+            return 0
+
+        def unmap(self, off, n):
+            self.mapped.remove(off)
+            return 0
+
+    fb, block = Backing(), 2 * 2 * 16 * 64 * 2
+    layouts = [(2, 64), (2, 64 | K.KV_Q4), (4, 64), (4, 64 | K.KV_Q4)]
+    h = K.kv_pool_create_vmm(16 * block, 16, layouts, ERR, page_bytes=block // 32, chunk_bytes=2 * block, backend=fb,
+                             device_base=BASE)
+    # a superpage holds the largest block, 64 pages: one, two, three (18) or seven (9) blocks
+    assert K.kv_pool_stats(h)["blocks_capacity"] == [16, 8 * 7, 8, 8 * 3]
+    a = K.kv_alloc_blocks(h, 1, 8)
+    assert len(fb.mapped) == 2 and len(set(a)) == 8 and set(a % 64) <= set(range(0, 63, 9))
+    b = K.kv_alloc_blocks(h, 3, 4)
+    assert set(b % 64) <= {0, 18, 36} and len(fb.mapped) == 4
+    spans = sorted([(int(i), int(i) + 9) for i in a] + [(int(i), int(i) + 18) for i in b])
+    assert all(x[1] <= y[0] for x, y in zip(spans, spans[1:]))
+    K.kv_free_blocks(h, 1, a)
+    K.kv_free_blocks(h, 3, b[:3])
+    K.kv_pool_trim(h)
+    assert len(fb.mapped) == 1
+    c = K.kv_alloc_blocks(h, 2, 7)
+    assert len(fb.mapped) == 8 and code(K.kv_alloc_blocks, h, 0, 1) == K.KV_ERR_OUT_OF_BLOCKS
+    K.kv_free_blocks(h, 2, c)
+    K.kv_free_blocks(h, 3, b[3:])
+    K.kv_pool_trim(h)
+    assert not fb.mapped
+    K.kv_pool_destroy(h)
