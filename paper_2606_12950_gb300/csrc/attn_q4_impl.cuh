@@ -81,12 +81,13 @@ struct Q4Args {
     const int32_t *packed;   // tokens held there
     int32_t *err;
     float *ws_part;          // records (combine_kernel)
-    int2 *ws_run;            // per run: the parts of its records, [x, y)
+    int2 *ws_run;            // as in AttnArgs (kRecCtas, or kRecCtasByPart)
     int64_t page_bytes, pool_pages;
     int32_t pages_per_block, pages_per_block4;
     int32_t max_blocks, max_blocks4;
     int32_t S, Hkv, G, bs;
     int32_t P;               // CTAs
+    bool by_part;            // ws_run is per part
     float qk_scale;          // scale * log2(e)
 };
 
@@ -138,6 +139,40 @@ __device__ __forceinline__ int32_t q4_tile_at(const Q4Seq<D> &q, int32_t x)
     const int32_t i = x <= c4 ? (int32_t)((uint32_t)(max(x, 0) + kQ4Cost - 1) / (uint32_t)kQ4Cost)
                               : q.tiles4() + (x - c4 + kBf16Cost - 1) / kBf16Cost;
     return max(1, i);
+}
+
+// A run as a warp works on it, in units of its CTA's costs.
+template <int D>
+struct Q4Run {
+    Q4Seq<D> q;
+    int32_t s, g;
+    int32_t begin;       // cost before it, from the CTA's start on
+    int32_t i0, i1;      // this warp's tiles of it
+    int32_t stop;        // the cost at the end of the warp's part
+};
+
+// Runs wait in shared memory while tiles are worked on (every lane stores and loads the
+// same): the registers are needed there, and what is spilled is spilled in the loops.
+template <int D>
+__device__ __forceinline__ void put_run(uint32_t at, const Q4Run<D> &r)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(r.q.n), "r"(r.q.append ? ~r.q.p : r.q.p),
+                 "r"(r.s), "r"(r.g));
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + 16), "r"(r.begin), "r"(r.i0), "r"(r.i1),
+                 "r"(r.stop));
+}
+template <int D>
+__device__ __forceinline__ Q4Run<D> get_run(uint32_t at)
+{
+    Q4Run<D> r;
+    int32_t p;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.q.n), "=r"(p), "=r"(r.s), "=r"(r.g) : "r"(at));
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r.begin), "=r"(r.i0), "=r"(r.i1), "=r"(r.stop)
+                 : "r"(at + 16));
+    r.q.append = p < 0;
+    r.q.p = p < 0 ? ~p : p;
+    return r;
 }
 
 // D(16x8, f32) += A(16x16, f16, row) * B(16x8, f16, col)
@@ -525,11 +560,12 @@ struct Q4State {
                     *reinterpret_cast<float4 *>(slot + at) = make_float4(o[0], o[1], o[2], o[3]);
                     *reinterpret_cast<float4 *>(slot + at + 4) = make_float4(o[4], o[5], o[6], o[7]);
                 } else {
+                    const float il = 1.f / l[h];
                     uint4 w;
-                    w.x = bf16_pair(o[0] / l[h], o[1] / l[h]);
-                    w.y = bf16_pair(o[2] / l[h], o[3] / l[h]);
-                    w.z = bf16_pair(o[4] / l[h], o[5] / l[h]);
-                    w.w = bf16_pair(o[6] / l[h], o[7] / l[h]);
+                    w.x = bf16_pair(o[0] * il, o[1] * il);
+                    w.y = bf16_pair(o[2] * il, o[3] * il);
+                    w.z = bf16_pair(o[4] * il, o[5] * il);
+                    w.w = bf16_pair(o[6] * il, o[7] * il);
                     *reinterpret_cast<uint4 *>(orow + at) = w;
                 }
             }
@@ -562,7 +598,9 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
         for (int i = 0; i < kQ4Warps * kQ4Stages; ++i) mbar_init(smem_u32(&bars[i]), 1);
         fence_mbar_init();
     }
+    __shared__ int2 part;  // by_part: this CTA's entry of ws_run
     if (lane == 0) chains[warp].x = -1;
+    if (tid == 0) part = make_int2(-1, -1);
     grid_launch_dependents();
     grid_dependency_wait();
 
@@ -580,7 +618,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
                 if (q.n == 0) {  // no softmax: zeros
                     uint4 *row = reinterpret_cast<uint4 *>(a.out + (int64_t)s * a.Hkv * G * D);
                     for (int i = 0; i < a.Hkv * G * (D / 8); ++i) row[i] = make_uint4(0u, 0u, 0u, 0u);
-                    for (int g = 0; g < a.Hkv; ++g) a.ws_run[(int64_t)s * a.Hkv + g] = make_int2(0, 0);
+                    for (int g = 0; g < a.Hkv && !a.by_part; ++g) a.ws_run[(int64_t)s * a.Hkv + g] = make_int2(0, 0);
                 }
             }
         }
@@ -604,7 +642,10 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
     // kQ4MinPart.  (64-bit divisions take 0.5 us each: there is one where W needs it.)
     const int64_t W = __shfl_sync(0xffffffffu, upto, kQ4Warps - 1);
     const int NC = (int)min((int64_t)a.P, (W / kQ4MinPart + kQ4Spread - 1) / kQ4Spread + (W < kQ4MinPart));
-    if (bid >= NC || W == 0) return;
+    if (bid >= NC || W == 0) {
+        if (a.by_part && tid == 0) a.ws_run[bid] = make_int2(-1, -1);
+        return;
+    }
     const int64_t wq = (W >> 32) == 0 ? (int64_t)((uint32_t)W / (uint32_t)NC) : W / NC;
     const uint32_t wr = (uint32_t)(W - wq * NC);
     const int64_t c0 = bid * wq + (uint32_t)bid * wr / (uint32_t)NC;
@@ -613,34 +654,33 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
     const int32_t nq = (int32_t)((uint32_t)cn / (uint32_t)nw), nr = cn - nq * nw;
     auto warp_begin = [&](int w) { return w * nq + (int32_t)((uint32_t)(w * nr) / (uint32_t)nw); };
 
-    struct Run {
-        Q4Seq<D> q;
-        int32_t s, g;
-        int32_t begin;       // cost before it, from the CTA's start on
-        int32_t i0, i1;      // this warp's tiles of it
-    };
     if (warp < nw) {
-        const int32_t w0 = warp_begin(warp), w1 = warp_begin(warp + 1);
+        const int32_t w0 = warp_begin(warp);
         // a run's tiles from cost x on
-        auto tile_from = [&](const Run &r, int32_t x) { return q4_tile_at(r.q, x - r.begin); };
+        auto tile_from = [&](const Q4Run<D> &r, int32_t x) { return q4_tile_at(r.q, x - r.begin); };
         // the run after r that has tiles in this part; false if there is none
-        auto next = [&](Run &r) {
+        auto next = [&](Q4Run<D> &r) {
             r.begin += r.q.cost();
             if (++r.g == a.Hkv) {
                 r.g = 0;
                 do {
-                    if (r.begin >= w1 || ++r.s >= S) return false;
+                    if (r.begin >= r.stop || ++r.s >= S) return false;
                     r.q = q4_seq<D>(a, r.s);
                 } while (r.q.n == 0);
             }
-            if (r.begin >= w1) return false;
+            if (r.begin >= r.stop) return false;
             r.i0 = 0;
-            r.i1 = tile_from(r, w1);
+            r.i1 = tile_from(r, r.stop);
             return true;
         };
+        // the run that is worked on, and the one whose tiles are asked for
+        __shared__ alignas(16) int32_t boxes[kQ4Warps][16];
+        const uint32_t box = smem_u32(boxes[warp]);
+        int32_t at, ahead_i1, ahead_t4, head;  // of the latter: its next tile, end, tiles in 4 bits, KV head
         // ---- the run at the part's start ----
-        Run run;
+        bool go;
         {
+            Q4Run<D> run;
             // the last thread whose sequences start at or before w0 (with any cost)
             int64_t x = c0 + w0;
             const int k = __popc(__ballot_sync(0xffffffffu, lane < kQ4Warps && upto <= x));  // warps before
@@ -657,10 +697,17 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
             run.g = (int32_t)((uint32_t)x / (uint32_t)run.q.cost());
             run.begin = w0 - (int32_t)((uint32_t)x - (uint32_t)run.g * (uint32_t)run.q.cost());
             run.i0 = tile_from(run, w0);
-            run.i1 = tile_from(run, w1);
+            run.stop = warp_begin(warp + 1);
+            run.i1 = tile_from(run, run.stop);
+            // (the part may start past this run's last tile; it has one of the next then)
+            go = run.i0 < run.i1 || next(run);
+            put_run(box, run);
+            put_run(box + 32, run);
+            at = run.i0;
+            ahead_i1 = run.i1;
+            ahead_t4 = run.q.tiles4();
+            head = run.g;
         }
-        // (the part may start past this run's last tile; it has one of the next then)
-        bool go = run.i0 < run.i1 || next(run);
 
         // ---- the ring: units of this warp's tiles, piece after piece.  A unit is up
         // to kQ4Unit tiles in 4 bits, or the K or the V of one in bf16 ----
@@ -668,35 +715,41 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
         const uint32_t ring_addr = smem_u32(ring), bar0 = smem_u32(&bars[warp * kQ4Stages]);
         const uint64_t policy = l2_policy_evict_first();
         const int per_block = a.bs / kQ4Tile;
-        Run ahead = run;
-        bool more = go;          // `ahead` is a run of this part
-        int32_t at = run.i0;     // its next tile to ask for
-        int32_t from = at - 32;  // tile of lane 0's address
-        const uint8_t *src = nullptr;  // of tile from + lane
+        bool more = go;          // there is a run whose tiles are asked for
+        // The places of tiles [from, from + 32), one a lane, for head 0: a sequence's
+        // runs share them, so that short ones load them once.
+        int32_t from = at - 32;
+        const uint8_t *src = nullptr;
         uint32_t good = 0;       // lanes with one
         bool v_next = false;     // a bf16 tile's V is next
         uint32_t issue_stage = 0;
         auto issue = [&]() {     // the next unit, if there is one
             if (!more) return;
-            if (at >= ahead.i1) {
+            if (at >= ahead_i1) {
+                Q4Run<D> ahead = get_run<D>(box + 32);
+                const int32_t s = ahead.s;
                 more = next(ahead);
                 if (!more) return;
-                at = ahead.i0;
-                from = at - 32;
+                put_run(box + 32, ahead);
+                at = 0;
+                ahead_i1 = ahead.i1;
+                ahead_t4 = ahead.q.tiles4();
+                head = ahead.g;
+                if (from != 0 || s != ahead.s) from = -32;
             }
-            const int32_t tiles4 = ahead.q.tiles4();
-            const bool packed = at < tiles4;
-            const int32_t end = packed ? min(at + U, min(ahead.i1, tiles4)) : at + 1;
+            const bool packed = at < ahead_t4;
+            const int32_t end = packed ? min(at + U, min(ahead_i1, ahead_t4)) : at + 1;
             if (end > from + 32) {  // the next 32 tiles' places
                 from = at;
+                const Q4Run<D> ahead = get_run<D>(box + 32);
                 const int32_t i = at + lane, b = (int32_t)((uint32_t)i / (uint32_t)per_block), t = i - b * per_block;
-                const bool in4 = i < tiles4;
+                const bool in4 = i < ahead_t4;
                 int32_t id = -1;
-                if (i < ahead.i1)
+                if (i < ahead.q.tiles())
                     id = in4 ? a.table4[(int64_t)ahead.s * a.max_blocks4 + b] : a.table[(int64_t)ahead.s * a.max_blocks + b];
                 const bool ok = id >= 0 && (int64_t)id + (in4 ? a.pages_per_block4 : a.pages_per_block) <= a.pool_pages;
-                if (i < ahead.i1 && !ok) report(a.err, KV_ERR_DEVICE_BOUNDS);
-                src = a.pool + (int64_t)id * a.page_bytes + ((int64_t)ahead.g * per_block + t) * (in4 ? TILE : TILE16);
+                if (i < ahead_i1 && !ok) report(a.err, KV_ERR_DEVICE_BOUNDS);
+                src = a.pool + (int64_t)id * a.page_bytes + t * (in4 ? TILE : TILE16);
                 good = __ballot_sync(0xffffffffu, ok);
             }
             const int off = at - from, n = end - at;
@@ -706,22 +759,35 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
             __syncwarp();
             if ((uint32_t)(lane - off) < (uint32_t)n && ((good >> lane) & 1u))
                 bulk_load(ring_addr + issue_stage * STAGE + (lane - off) * TILE,
-                          src + (v_next ? (int64_t)a.Hkv * per_block * TILE16 : 0), bytes, bar, policy);
+                          src + (int64_t)(((v_next ? a.Hkv : 0) + head) * per_block) * bytes, bytes, bar, policy);
             if (packed || v_next) at = end;
             v_next = !packed && !v_next;
             issue_stage = issue_stage + 1 == kQ4Stages ? 0 : issue_stage + 1;
         };
         for (int st = 0; st < kQ4Stages; ++st) issue();
 
+        // run r's entry of ws_run: it starts, ends in this CTA
+        auto note = [&](int32_t r, bool first, bool last) {
+            if (a.by_part) {
+                if (first && !last) part.x = r;
+                if (last && !first) part.y = r;
+                return;
+            }
+            if (first) a.ws_run[r].x = bid;
+            if (last) a.ws_run[r].y = first ? bid : bid + 1;
+        };
+
         bool dead = false;
         uint32_t stage = 0, parity = 0;
-        for (; go; go = next(run)) {
-            const Q4Seq<D> q = run.q;
-            const int32_t r = run.s * a.Hkv + run.g;
-            const uint16_t *qrow = a.q + (int64_t)r * G * D;
+        while (go) {
             Q4State<D> st;
-            st.begin(qrow, G, a.qk_scale, lane);
-            const int32_t end4 = min(run.i1, q.tiles4());
+            int32_t i0, end4;
+            {
+                const Q4Run<D> run = get_run<D>(box);
+                st.begin(a.q + ((int64_t)run.s * a.Hkv + run.g) * G * D, G, a.qk_scale, lane);
+                i0 = run.i0;
+                end4 = min(run.i1, run.q.tiles4());
+            }
             auto unit_done = [&]() {
                 if (++stage == kQ4Stages) {
                     stage = 0;
@@ -732,7 +798,6 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
                 __syncwarp();
                 issue();
             };
-            const int32_t i0 = run.i0;
             for (int32_t i = i0; i < end4; i += U) {
                 if ((i - i0) % kQ4Rebalance == kQ4Rebalance - U) st.rebalance();
                 wait_phase(bar0 + stage * 8, parity, a.err, dead);
@@ -742,7 +807,11 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
                     for (int32_t u = i; u < end4; ++u) st.template tiles4<1>(ring + stage * STAGE + (u - i) * TILE, lane);
                 unit_done();
             }
-            for (int32_t i = max(run.i0, q.tiles4()); i < run.i1; ++i) {
+            Q4Run<D> run = get_run<D>(box);
+            const Q4Seq<D> q = run.q;
+            const int32_t r = run.s * a.Hkv + run.g;
+            const uint16_t *qrow = a.q + (int64_t)r * G * D;
+            for (int32_t i = max(i0, q.tiles4()); i < run.i1; ++i) {
                 const int32_t tok0 = i * kQ4Tile;
                 const int fresh = a.k_new && q.append ? q.n - 1 - tok0 : -1, valid = q.n - tok0;
                 float y[4];
@@ -773,10 +842,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
             const bool first = t0 == 0, last = t1 == q.tiles(), split = !(first && last);
             if (run.i0 == t0 && run.i1 == t1) {
                 st.store(a.out + (int64_t)r * G * D, a.ws_part + ((int64_t)r + bid) * MF, split, G, lane);
-                if (lane == 0) {
-                    if (first) a.ws_run[r].x = bid;
-                    if (last) a.ws_run[r].y = split ? bid + 1 : bid;
-                }
+                if (lane == 0) note(r, first, last);
             } else if (run.i0 != t0) {  // goes on from an earlier warp, which merges it
                 st.store(nullptr, recs + warp * MF, true, G, lane);
             } else {  // goes on in the next warp: the last piece here, so the ring is free
@@ -784,8 +850,13 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
                 const int32_t last_tile = run.begin + q.cost_to(t1 - 1);
                 int e = warp;
                 while (e + 1 < nw && warp_begin(e + 1) <= last_tile) ++e;
-                if (lane == 0) chains[warp] = make_int4(r, e - warp, (first ? 1 : 0) | (last ? 2 : 0), split ? 1 : 0);
+                if (lane == 0) {
+                    chains[warp] = make_int4(r, e - warp, split ? 1 : 0, 0);
+                    note(r, first, last);
+                }
             }
+            go = next(run);
+            put_run(box, run);
         }
     }
     __syncthreads();
@@ -814,7 +885,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
             O.z = __fmaf_rn(o.z, e, O.z);
             O.w = __fmaf_rn(o.w, e, O.w);
         }
-        if (ch.w == 0) {
+        if (ch.z == 0) {
             store_column(a.out + (int64_t)ch.x * (G * D) + c * 4, O, L);
         } else {
             float *slot = a.ws_part + ((int64_t)ch.x + bid) * MF;
@@ -824,9 +895,8 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
                 slot[G * D + G + h] = L;
             }
         }
-        if (c == 0 && (ch.z & 1)) a.ws_run[ch.x].x = bid;
-        if (c == 0 && (ch.z & 2)) a.ws_run[ch.x].y = bid + ch.w;
     }
+    if (a.by_part && tid == 0) a.ws_run[bid] = part;
 }
 
 }  // namespace kvp

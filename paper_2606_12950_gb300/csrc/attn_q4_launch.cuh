@@ -12,6 +12,8 @@ int q4_combine(const Q4Args &a, int sm_count, const cudaLaunchConfig_t &cfg)
 {
     const CombineArgs c{a.out, a.ws_run, a.ws_part, a.S, a.Hkv, nullptr, nullptr, 0};
     const double per_run = (double)a.P / std::max(1, a.S * a.Hkv) + 1.0;
+    if (a.by_part)
+        return combine_launch<D, G, 1, 1, kRecCtasByPart>(c, combine_groups<D, G, 1>(per_run), cfg, a.P);
     return combine_run<D, G, kRecCtas>(c, per_run, sm_count, cfg);
 }
 
@@ -35,6 +37,9 @@ int q4_attn_run(int G, const Q4Args *args, int sm_count, cudaStream_t st, bool l
     if (!launch) return KV_OK;
     Q4Args a = *args;
     a.P = *P_out;
+    // with several waves of runs, a combine CTA per part (as in attn_launch.cuh)
+    const int64_t runs = (int64_t)a.S * a.Hkv;
+    a.by_part = runs >= 8 * (int64_t)a.P && 4 * runs > (int64_t)kSlicedCtas * sm_count;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;

@@ -182,6 +182,27 @@ def test_long_and_short_together():
     attend([20000, 3, 65, 9000, 16], [19968, 0, 48, 0, 0], 16, 4, 128, 16)[0].close()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kind", ["two", "among short ones", "none", "one token"])
+def test_many_runs(kind, d):
+    """So many runs that the merge goes by parts, not by runs: all but two empty
+    (fewer parts than there are CTAs, a run over most of them), a long one among
+    short ones, none with a token."""
+    n, p = np.zeros(320, np.int64), np.zeros(320, np.int64)
+    if kind == "two":
+        n[100], p[100], n[319], p[319] = 20007, 19984, 5, 0
+    elif kind == "among short ones":
+        n[:] = np.arange(320) % 45
+        p[:] = (n - 1).clip(0) // 16 * 16
+        n[160], p[160] = 30011, 29984
+    elif kind == "one token":
+        n[7] = 1
+    c, q, out = attend(n, p, 8, 4, d, 16)
+    assert (out[torch.from_numpy(n == 0).cuda()] == 0).all()
+    assert torch.equal(c.run(q, d ** -0.5), out)
+    c.close()
+
+
 @pytest.mark.parametrize("append", [True, False])
 def test_scales_far_apart(append):
     """Rows of V whose scales differ by many powers of two, within a tile, from
