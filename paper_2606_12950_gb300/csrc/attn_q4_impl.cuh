@@ -241,13 +241,12 @@ struct Q4State {
     // qrow: q rows of the run's G heads
     __device__ __forceinline__ void begin(const uint16_t *qrow, int G, float qk_scale, int lane)
     {
-        const int gid = lane >> 2, tig = lane & 3;
+        const int tig = lane & 3;
         uint4 w[NW];
+        load_q(w, qrow, G, lane);
         float mx = 0.f;
 #pragma unroll
         for (int j = 0; j < NW; ++j) {
-            w[j] = gid < G ? *reinterpret_cast<const uint4 *>(qrow + gid * D + 64 * (j >> 1) + 32 * (j & 1) + 8 * tig)
-                           : make_uint4(0u, 0u, 0u, 0u);
             const uint32_t *x = reinterpret_cast<const uint32_t *>(&w[j]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fmaxf(fabsf(bf_lo(x[e])), fabsf(bf_hi(x[e]))));
@@ -466,23 +465,28 @@ struct Q4State {
             }
     }
 
-    // A tile of bf16 rows: its K's scores (rows, their first of this lane's, and
-    // the tile's tokens with a weight, a bit each), then its V.  qrow as in begin;
-    // where token `fresh` is one of the tile's, its row is k_new or v_new.
-    __device__ __forceinline__ void scores16(float (&y)[4], const uint16_t *rows, int valid, int fresh, const uint16_t *k_new,
-                                             const uint16_t *qrow, int G, float qk_scale, int lane)
+    // A tile of bf16 rows, of which the first `valid` are tokens: its K's scores (qw
+    // as load_q gives it), then its V.
+    static __device__ __forceinline__ void load_q(uint4 (&qw)[NW], const uint16_t *qrow, int G, int lane)
     {
         const int gid = lane >> 2, tig = lane & 3;
-        const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-        const uint16_t *k0 = gid == fresh ? k_new : rows + gid * D, *k1 = gid + 8 == fresh ? k_new : rows + (gid + 8) * D;
+#pragma unroll
+        for (int j = 0; j < NW; ++j)
+            qw[j] = gid < G ? *reinterpret_cast<const uint4 *>(qrow + gid * D + 64 * (j >> 1) + 32 * (j & 1) + 8 * tig)
+                            : make_uint4(0u, 0u, 0u, 0u);
+    }
+    __device__ __forceinline__ void scores16(float (&y)[4], const uint16_t *rows, int valid, const uint4 (&qw)[NW],
+                                             float qk_scale, int lane)
+    {
+        const int gid = lane >> 2, tig = lane & 3;
+        const uint16_t *k0 = rows + gid * D, *k1 = k0 + 8 * D;
         float x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NW; ++j) {
             const int at = 64 * (j >> 1) + 32 * (j & 1) + 8 * tig;
             const uint4 a = *reinterpret_cast<const uint4 *>(k0 + at), b = *reinterpret_cast<const uint4 *>(k1 + at);
-            const uint4 q = gid < G ? *reinterpret_cast<const uint4 *>(qrow + gid * D + at) : none;
-            mma_bf16_16816(x, a.x, b.x, a.y, b.y, q.x, q.y);
-            mma_bf16_16816(x, a.z, b.z, a.w, b.w, q.z, q.w);
+            mma_bf16_16816(x, a.x, b.x, a.y, b.y, qw[j].x, qw[j].y);
+            mma_bf16_16816(x, a.z, b.z, a.w, b.w, qw[j].z, qw[j].w);
         }
         const float no = -INFINITY;
         y[0] = gid < valid ? x[0] * qk_scale : no;
@@ -491,15 +495,14 @@ struct Q4State {
         y[3] = gid + 8 < valid ? x[3] * qk_scale : no;
         raise(fmaxf(y[0], y[2]), fmaxf(y[1], y[3]));
     }
-    __device__ __forceinline__ void values16(const float (&y)[4], const uint16_t *rows, int valid, int fresh,
-                                             const uint16_t *v_new, int lane)
+    __device__ __forceinline__ void values16(const float (&y)[4], const uint16_t *rows, int valid, int lane)
     {
         const int gid = lane >> 2, tig = lane & 3;
         uint4 vw[4][NG];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {  // (what lies past the context may be anything)
             const int t = 2 * tig + (r & 1) + 4 * (r & 2);
-            const uint16_t *v = t == fresh ? v_new : rows + t * D;
+            const uint16_t *v = rows + t * D;
 #pragma unroll
             for (int c = 0; c < NG; ++c)
                 vw[r][c] = t < valid ? *reinterpret_cast<const uint4 *>(v + 64 * c + 8 * gid) : make_uint4(0u, 0u, 0u, 0u);
@@ -811,29 +814,39 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
             const Q4Seq<D> q = run.q;
             const int32_t r = run.s * a.Hkv + run.g;
             const uint16_t *qrow = a.q + (int64_t)r * G * D;
+            // The new row, lanes [0, D / 8) its K and the next D / 8 its V: it goes to
+            // its tile's copy in shared memory and, once that has landed, to the pool
+            // (no other unit holds that row).
+            int32_t fresh = a.k_new && q.append && run.i1 == q.tiles() ? q.n - 1 : -1, place = -1;
+            uint4 row = make_uint4(0u, 0u, 0u, 0u);
+            if (fresh >= 0 && lane < D / 4) {
+                place = a.table[(int64_t)run.s * a.max_blocks + fresh / a.bs];
+                row = *reinterpret_cast<const uint4 *>((lane < D / 8 ? a.k_new : a.v_new) + (int64_t)r * D + lane % (D / 8) * 8);
+            }
             for (int32_t i = max(i0, q.tiles4()); i < run.i1; ++i) {
-                const int32_t tok0 = i * kQ4Tile;
-                const int fresh = a.k_new && q.append ? q.n - 1 - tok0 : -1, valid = q.n - tok0;
+                const int32_t tok0 = i * kQ4Tile, valid = q.n - tok0;
+                const bool here = (uint32_t)(fresh - tok0) < (uint32_t)kQ4Tile;
+                auto put_row = [&](int kv) {
+                    if (!here) return;
+                    if (lane / (D / 8) == kv)
+                        *reinterpret_cast<uint4 *>(ring + stage * STAGE + ((fresh - tok0) * D + lane % (D / 8) * 8) * 2) = row;
+                    __syncwarp();
+                };
                 float y[4];
+                uint4 qw[D / 32];
+                Q4State<D>::load_q(qw, qrow, G, lane);
                 wait_phase(bar0 + stage * 8, parity, a.err, dead);
-                st.scores16(y, reinterpret_cast<const uint16_t *>(ring + stage * STAGE), valid, fresh, a.k_new + (int64_t)r * D,
-                            qrow, G, a.qk_scale, lane);
+                put_row(0);
+                st.scores16(y, reinterpret_cast<const uint16_t *>(ring + stage * STAGE), valid, qw, a.qk_scale, lane);
                 unit_done();
                 wait_phase(bar0 + stage * 8, parity, a.err, dead);
-                st.values16(y, reinterpret_cast<const uint16_t *>(ring + stage * STAGE), valid, fresh, a.v_new + (int64_t)r * D,
-                            lane);
-                if ((uint32_t)fresh < (uint32_t)kQ4Tile && lane < D / 4) {
-                    // the new row's place: this warp's copies of the tile have landed, and
-                    // no other unit holds that row
-                    const int32_t j = q.n - 1, b = j / a.bs;
-                    const int32_t id = a.table[(int64_t)run.s * a.max_blocks + b];
-                    if (id >= 0 && (int64_t)id + a.pages_per_block <= a.pool_pages) {
-                        const int kv = lane / (D / 8), c = lane % (D / 8);
-                        uint16_t *dst = reinterpret_cast<uint16_t *>(a.pool + (int64_t)id * a.page_bytes) +
-                                        ((int64_t)(kv * a.Hkv + run.g) * a.bs + (j - b * a.bs)) * D;
-                        *reinterpret_cast<uint4 *>(dst + c * 8) =
-                            *reinterpret_cast<const uint4 *>((kv ? a.v_new : a.k_new) + (int64_t)r * D + c * 8);
-                    }
+                put_row(1);
+                st.values16(y, reinterpret_cast<const uint16_t *>(ring + stage * STAGE), valid, lane);
+                if (here && place >= 0 && (int64_t)place + a.pages_per_block <= a.pool_pages) {
+                    const int kv = lane / (D / 8), c = lane % (D / 8);
+                    uint16_t *dst = reinterpret_cast<uint16_t *>(a.pool + (int64_t)place * a.page_bytes) +
+                                    ((int64_t)(kv * a.Hkv + run.g) * a.bs + fresh % a.bs) * D;
+                    *reinterpret_cast<uint4 *>(dst + c * 8) = row;
                 }
                 unit_done();
             }
