@@ -341,9 +341,11 @@ struct Q4State {
         }
     }
 
-    // U tiles in 4 bits
+    // The first `count` (or more) of a stage's U tiles in 4 bits.  In place of those that
+    // are missing the last one is read once more, without weight: one tile by itself
+    // takes nearly as long as two.
     template <int U>
-    __device__ __forceinline__ void tiles4(const uint8_t *stage, int lane)
+    __device__ __forceinline__ void tiles4(const uint8_t *stage, int count, int lane)
     {
         constexpr int TILE = kQ4TileBytes<D>;
         const int gid = lane >> 2, tig = lane & 3;
@@ -354,7 +356,7 @@ struct Q4State {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             {
-                const uint8_t *tile = stage + u * TILE;
+                const uint8_t *tile = stage + min(u, count - 1) * TILE;
                 uint32_t ka[NW], kb[NW], kp[2][NG];
                 const uint8_t *ra = tile + gid * (D / 2) + tig * (D / 8), *rb = ra + 8 * (D / 2);
                 const uint8_t *pa = tile + 16 * D + gid * 8 * NG, *pb = pa + 64 * NG;
@@ -413,9 +415,11 @@ struct Q4State {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             {
-                const uint8_t *tile = stage + u * TILE;
-                const float p0 = fast_exp2(fmaf(x[u][0], factor[0], -m[0])), p1 = fast_exp2(fmaf(x[u][1], factor[1], -m[1]));
-                const float p2 = fast_exp2(fmaf(x[u][2], factor[0], -m[0])), p3 = fast_exp2(fmaf(x[u][3], factor[1], -m[1]));
+                const uint8_t *tile = stage + min(u, count - 1) * TILE;
+                const bool in = u == 0 || u < count;
+                const float m0 = in ? -m[0] : -INFINITY, m1 = in ? -m[1] : -INFINITY;
+                const float p0 = fast_exp2(fmaf(x[u][0], factor[0], m0)), p1 = fast_exp2(fmaf(x[u][1], factor[1], m1));
+                const float p2 = fast_exp2(fmaf(x[u][2], factor[0], m0)), p3 = fast_exp2(fmaf(x[u][3], factor[1], m1));
                 l[0] += p0 + p2;
                 l[1] += p1 + p3;
 #pragma unroll
@@ -767,6 +771,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
             v_next = !packed && !v_next;
             issue_stage = issue_stage + 1 == kQ4Stages ? 0 : issue_stage + 1;
         };
+#pragma unroll 1
         for (int st = 0; st < kQ4Stages; ++st) issue();
 
         // run r's entry of ws_run: it starts, ends in this CTA
@@ -784,88 +789,98 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
         uint32_t stage = 0, parity = 0;
         while (go) {
             Q4State<D> st;
-            int32_t i0, end4;
+            int32_t i, i0, i1, end4;
             {
                 const Q4Run<D> run = get_run<D>(box);
                 st.begin(a.q + ((int64_t)run.s * a.Hkv + run.g) * G * D, G, a.qk_scale, lane);
-                i0 = run.i0;
+                i = i0 = run.i0;
+                i1 = run.i1;
                 end4 = min(run.i1, run.q.tiles4());
             }
-            auto unit_done = [&]() {
+            auto tile_in = [&]() { return ring + stage * STAGE; };
+            auto stage_done = [&]() {
                 if (++stage == kQ4Stages) {
                     stage = 0;
                     parity ^= 1u;
                 }
-                // the stage is refilled by bulk copies next: after this warp's reads
+            };
+            auto unit_done = [&](int again) {
+                stage_done();
+                // the stages are refilled by bulk copies next: after this warp's reads
                 fence_proxy_async_smem();
                 __syncwarp();
-                issue();
+#pragma unroll 1
+                for (; again > 0; --again) issue();
             };
-            for (int32_t i = i0; i < end4; i += U) {
-                if ((i - i0) % kQ4Rebalance == kQ4Rebalance - U) st.rebalance();
+            for (; i < end4; i += U) {
                 wait_phase(bar0 + stage * 8, parity, a.err, dead);
-                if (i + U <= end4)
-                    st.template tiles4<U>(ring + stage * STAGE, lane);
+                if ((i - i0) % kQ4Rebalance == kQ4Rebalance - U) st.rebalance();
+                // (a lone tile takes its warp nearly as long as two, but of d = 64's four one
+                // is often enough alone; and where there are many short runs the kernel waits
+                // for its instructions, so that less code counts)
+                if (D == 128 || i + U <= end4)
+                    st.template tiles4<U>(tile_in(), end4 - i, lane);
                 else
-                    for (int32_t u = i; u < end4; ++u) st.template tiles4<1>(ring + stage * STAGE + (u - i) * TILE, lane);
-                unit_done();
+#pragma unroll 1
+                    for (int32_t u = i; u < end4; ++u) st.template tiles4<1>(tile_in() + (u - i) * TILE, 1, lane);
+                unit_done(1);
+            }
+            for (i = max(i0, end4); i < i1; ++i) {
+                const Q4Run<D> run = get_run<D>(box);
+                const int32_t r = run.s * a.Hkv + run.g, tok0 = i * kQ4Tile, valid = run.q.n - tok0;
+                // The new row, lanes [0, D / 8) its K and the next D / 8 its V: it goes
+                // to its tile's copy in shared memory and, once that has landed, to the
+                // pool (no other unit holds that row).
+                const int32_t fresh = a.k_new && run.q.append && valid <= kQ4Tile ? valid - 1 : -1;
+                int32_t place = -1;
+                uint4 row = make_uint4(0u, 0u, 0u, 0u), qw[D / 32];
+                if (fresh >= 0 && lane < D / 4) {
+                    place = a.table[(int64_t)run.s * a.max_blocks + (run.q.n - 1) / a.bs];
+                    row = *reinterpret_cast<const uint4 *>((lane < D / 8 ? a.k_new : a.v_new) + (int64_t)r * D +
+                                                           lane % (D / 8) * 8);
+                }
+                Q4State<D>::load_q(qw, a.q + (int64_t)r * G * D, G, lane);
+                auto put_row = [&](int kv) {
+                    if (fresh < 0) return;
+                    if (lane / (D / 8) == kv)
+                        *reinterpret_cast<uint4 *>(tile_in() + (fresh * D + lane % (D / 8) * 8) * 2) = row;
+                    __syncwarp();
+                };
+                float y[4];
+                wait_phase(bar0 + stage * 8, parity, a.err, dead);
+                put_row(0);
+                st.scores16(y, reinterpret_cast<const uint16_t *>(tile_in()), valid, qw, a.qk_scale, lane);
+                stage_done();
+                wait_phase(bar0 + stage * 8, parity, a.err, dead);
+                put_row(1);
+                st.values16(y, reinterpret_cast<const uint16_t *>(tile_in()), valid, lane);
+                if (place >= 0 && (int64_t)place + a.pages_per_block <= a.pool_pages) {
+                    const int kv = lane / (D / 8), c = lane % (D / 8);
+                    uint16_t *dst = reinterpret_cast<uint16_t *>(a.pool + (int64_t)place * a.page_bytes) +
+                                    ((int64_t)(kv * a.Hkv + run.g) * a.bs + (run.q.n - 1) % a.bs) * D;
+                    *reinterpret_cast<uint4 *>(dst + c * 8) = row;
+                }
+                unit_done(2);
             }
             Q4Run<D> run = get_run<D>(box);
             const Q4Seq<D> q = run.q;
             const int32_t r = run.s * a.Hkv + run.g;
-            const uint16_t *qrow = a.q + (int64_t)r * G * D;
-            // The new row, lanes [0, D / 8) its K and the next D / 8 its V: it goes to
-            // its tile's copy in shared memory and, once that has landed, to the pool
-            // (no other unit holds that row).
-            int32_t fresh = a.k_new && q.append && run.i1 == q.tiles() ? q.n - 1 : -1, place = -1;
-            uint4 row = make_uint4(0u, 0u, 0u, 0u);
-            if (fresh >= 0 && lane < D / 4) {
-                place = a.table[(int64_t)run.s * a.max_blocks + fresh / a.bs];
-                row = *reinterpret_cast<const uint4 *>((lane < D / 8 ? a.k_new : a.v_new) + (int64_t)r * D + lane % (D / 8) * 8);
-            }
-            for (int32_t i = max(i0, q.tiles4()); i < run.i1; ++i) {
-                const int32_t tok0 = i * kQ4Tile, valid = q.n - tok0;
-                const bool here = (uint32_t)(fresh - tok0) < (uint32_t)kQ4Tile;
-                auto put_row = [&](int kv) {
-                    if (!here) return;
-                    if (lane / (D / 8) == kv)
-                        *reinterpret_cast<uint4 *>(ring + stage * STAGE + ((fresh - tok0) * D + lane % (D / 8) * 8) * 2) = row;
-                    __syncwarp();
-                };
-                float y[4];
-                uint4 qw[D / 32];
-                Q4State<D>::load_q(qw, qrow, G, lane);
-                wait_phase(bar0 + stage * 8, parity, a.err, dead);
-                put_row(0);
-                st.scores16(y, reinterpret_cast<const uint16_t *>(ring + stage * STAGE), valid, qw, a.qk_scale, lane);
-                unit_done();
-                wait_phase(bar0 + stage * 8, parity, a.err, dead);
-                put_row(1);
-                st.values16(y, reinterpret_cast<const uint16_t *>(ring + stage * STAGE), valid, lane);
-                if (here && place >= 0 && (int64_t)place + a.pages_per_block <= a.pool_pages) {
-                    const int kv = lane / (D / 8), c = lane % (D / 8);
-                    uint16_t *dst = reinterpret_cast<uint16_t *>(a.pool + (int64_t)place * a.page_bytes) +
-                                    ((int64_t)(kv * a.Hkv + run.g) * a.bs + fresh % a.bs) * D;
-                    *reinterpret_cast<uint4 *>(dst + c * 8) = row;
-                }
-                unit_done();
-            }
             // ---- end of a piece: t0, t1 are the CTA's tiles of the run ----
             const int32_t t0 = tile_from(run, 0), t1 = tile_from(run, cn);
             const bool first = t0 == 0, last = t1 == q.tiles(), split = !(first && last);
-            if (run.i0 == t0 && run.i1 == t1) {
+            const bool alone = run.i0 == t0 && run.i1 == t1;
+            // (a run that goes on in the next warp is the last here: the ring is free)
+            if (alone)
                 st.store(a.out + (int64_t)r * G * D, a.ws_part + ((int64_t)r + bid) * MF, split, G, lane);
-                if (lane == 0) note(r, first, last);
-            } else if (run.i0 != t0) {  // goes on from an earlier warp, which merges it
-                st.store(nullptr, recs + warp * MF, true, G, lane);
-            } else {  // goes on in the next warp: the last piece here, so the ring is free
-                st.store(nullptr, reinterpret_cast<float *>(ring), true, G, lane);
-                const int32_t last_tile = run.begin + q.cost_to(t1 - 1);
-                int e = warp;
-                while (e + 1 < nw && warp_begin(e + 1) <= last_tile) ++e;
-                if (lane == 0) {
+            else
+                st.store(nullptr, run.i0 != t0 ? recs + warp * MF : reinterpret_cast<float *>(ring), true, G, lane);
+            if (lane == 0 && run.i0 == t0) {  // (one that goes on from an earlier warp is merged there)
+                note(r, first, last);
+                if (!alone) {
+                    const int32_t last_tile = run.begin + q.cost_to(t1 - 1);
+                    int e = warp;
+                    while (e + 1 < nw && warp_begin(e + 1) <= last_tile) ++e;
                     chains[warp] = make_int4(r, e - warp, split ? 1 : 0, 0);
-                    note(r, first, last);
                 }
             }
             go = next(run);
