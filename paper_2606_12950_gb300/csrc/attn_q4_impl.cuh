@@ -141,6 +141,8 @@ __device__ __forceinline__ int32_t q4_tile_at(const Q4Seq<D> &q, int32_t x)
     return max(1, i);
 }
 
+__device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
 // A run as a warp works on it, in units of its CTA's costs.
 template <int D>
 struct Q4Run {
@@ -680,10 +682,13 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
             r.i1 = tile_from(r, r.stop);
             return true;
         };
-        // the run that is worked on, and the one whose tiles are asked for
-        __shared__ alignas(16) int32_t boxes[kQ4Warps][16];
-        const uint32_t box = smem_u32(boxes[warp]);
-        int32_t at, ahead_i1, ahead_t4, head;  // of the latter: its next tile, end, tiles in 4 bits, KV head
+        // The runs from the one that is worked on to the one whose tiles are asked for
+        // (three at most: the units of the ring are of two).
+        __shared__ alignas(16) int32_t boxes[kQ4Warps][4][8];
+        static_assert(kQ4Stages + 1 <= 4, "boxes");
+        auto box = [&](int k) { return smem_u32(boxes[warp][k & 3]); };
+        int asked = 0;                         // the latter's box
+        int32_t at, ahead_i1, ahead_t4, head;  // its next tile, end, tiles in 4 bits, KV head
         // ---- the run at the part's start ----
         bool go;
         {
@@ -708,8 +713,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
             run.i1 = tile_from(run, run.stop);
             // (the part may start past this run's last tile; it has one of the next then)
             go = run.i0 < run.i1 || next(run);
-            put_run(box, run);
-            put_run(box + 32, run);
+            put_run(box(0), run);
             at = run.i0;
             ahead_i1 = run.i1;
             ahead_t4 = run.q.tiles4();
@@ -733,11 +737,13 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
         auto issue = [&]() {     // the next unit, if there is one
             if (!more) return;
             if (at >= ahead_i1) {
-                Q4Run<D> ahead = get_run<D>(box + 32);
+                Q4Run<D> ahead = get_run<D>(box(asked));
                 const int32_t s = ahead.s;
                 more = next(ahead);
                 if (!more) return;
-                put_run(box + 32, ahead);
+                put_run(box(++asked), ahead);
+                if (lane < (G * D * 2 + 127) / 128)  // its q is needed next
+                    prefetch_l2(a.q + ((int64_t)ahead.s * a.Hkv + ahead.g) * G * D + lane * 64);
                 at = 0;
                 ahead_i1 = ahead.i1;
                 ahead_t4 = ahead.q.tiles4();
@@ -748,7 +754,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
             const int32_t end = packed ? min(at + U, min(ahead_i1, ahead_t4)) : at + 1;
             if (end > from + 32) {  // the next 32 tiles' places
                 from = at;
-                const Q4Run<D> ahead = get_run<D>(box + 32);
+                const Q4Run<D> ahead = get_run<D>(box(asked));
                 const int32_t i = at + lane, b = (int32_t)((uint32_t)i / (uint32_t)per_block), t = i - b * per_block;
                 const bool in4 = i < ahead_t4;
                 int32_t id = -1;
@@ -787,11 +793,11 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
 
         bool dead = false;
         uint32_t stage = 0, parity = 0;
-        while (go) {
+        for (int k = 0; go && k <= asked; ++k) {
             Q4State<D> st;
             int32_t i, i0, i1, end4;
             {
-                const Q4Run<D> run = get_run<D>(box);
+                const Q4Run<D> run = get_run<D>(box(k));
                 st.begin(a.q + ((int64_t)run.s * a.Hkv + run.g) * G * D, G, a.qk_scale, lane);
                 i = i0 = run.i0;
                 i1 = run.i1;
@@ -826,7 +832,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
                 unit_done(1);
             }
             for (i = max(i0, end4); i < i1; ++i) {
-                const Q4Run<D> run = get_run<D>(box);
+                const Q4Run<D> run = get_run<D>(box(k));
                 const int32_t r = run.s * a.Hkv + run.g, tok0 = i * kQ4Tile, valid = run.q.n - tok0;
                 // The new row, lanes [0, D / 8) its K and the next D / 8 its V: it goes
                 // to its tile's copy in shared memory and, once that has landed, to the
@@ -862,7 +868,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
                 }
                 unit_done(2);
             }
-            Q4Run<D> run = get_run<D>(box);
+            const Q4Run<D> run = get_run<D>(box(k));
             const Q4Seq<D> q = run.q;
             const int32_t r = run.s * a.Hkv + run.g;
             // ---- end of a piece: t0, t1 are the CTA's tiles of the run ----
@@ -883,8 +889,6 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
                     chains[warp] = make_int4(r, e - warp, split ? 1 : 0, 0);
                 }
             }
-            go = next(run);
-            put_run(box, run);
         }
     }
     __syncthreads();
