@@ -29,25 +29,34 @@
 // bulk copy a tile (or K or V, where they are in bf16).
 //
 // Bound by HBM in the long run, by its start and end in short ones.  Steady state (the
-// slope from 240000 to 480000 tokens, 32 q / 8 KV heads of 128): 6.53 TB/s, 0.96 of the
-// measured copy; 16 single heads of 64 5.93.  Around it a call spends about 12 us:
-// the lengths' round trip and the split 2, the table's and the first tiles' 3, warps
-// that end apart 3, merges and the combine 4.  Calls (us; floor at 6.78 TB/s):
-//   250 sequences, 40 q / 8 KV heads of 128, 700 MB    119.1 (103)
-//   64 sequences, 32 / 8 of 128, 242 MB                 48.6 (35.7)
-//   one of 100000 tokens, 32 / 8 of 128, 115 MB         30.0 (17.0)
+// slope from 240000 to 480000 tokens, 32 q / 8 KV heads of 128): 7.08 TB/s read, 1.04
+// of the measured copy; 16 single heads of 64 6.41.  Around it a call spends about 12
+// us: the lengths' round trip and the split 3, the table's and the first tiles' 3, warps
+// that end apart 2, merges and the combine 4.  Calls (us; floor at 6.78 TB/s):
+//   250 sequences, 40 q / 8 KV heads of 128, 700 MB    113.5 (103)
+//   64 sequences, 32 / 8 of 128, 242 MB                 46.8 (35.7)
+//   one of 100000 tokens, 32 / 8 of 128, 115 MB         29.4 (17.0)
 //   40 sequences, 16 heads of 64, 140 MB                34.2 (20.7)
-// A tile of 128 columns takes 255 issue slots of the 396 that an SM quarter has while
+//   400 of 100 to 500 tokens, 32 / 8 of 128, 174 MB     41.2 (25.7)
+//   1000 of 20 to 200 tokens, 32 / 8 of 128, 217 MB     55.5 (32.0)
+// A tile of 128 columns takes 252 issue slots of the 396 that an SM quarter has while
 // HBM brings it; half of them are masks and shifts of codes, which is why the masked
 // words must be operands as they are.  (With a subtraction per pair, or codes as bf16,
-// they would be twice as many.)
+// they would be twice as many.)  Short runs add what begins and ends them; there the
+// kernel waits for instructions more than for data, and its size counts.
 //
 // What was measured on the way, 64 / 250 sequences: a CTA of 8 warps twice on an SM 54.0
 // / 123.9 and one of 16 48.2 / 117.4, as the CTA that came first ran 25% ahead and left
 // the other half the SM; warps' records for the combine, not CTAs', 60.6 / 145.5; bf16
 // tiles read into registers, without the ring, 54.0 / 136.7; the last CTA of a run
 // merging its records, in place of the combine, 52.7 / 123.5 (counted by compare and
-// swap) and 53.9 / 124.4 (flags), as the fences at a CTA's end took 7 us.
+// swap) and 53.9 / 124.4 (flags), as the fences at a CTA's end took 7 us.  Later, 47.1 /
+// 112.9 now: shifts as high products, off the busiest pipe, 51.8 / 126.7; the way to the
+// first tiles gone once before the grids ahead are done, for its instructions, 48.3 /
+// 114.9.  And 1000 short / 400 / 250 sequences: 92.4 / 58.3 / 118.6 with the runs' fields in
+// registers, spilled in the loops (66.4 / 48.8 / 113.5 in shared memory); 64.8 / 48.2 with
+// three loops that ask for tiles and lone tiles on their own (57.4 / 42.8); runs found
+// twice, by the loader and the consumer, 57.3 / 42.8 (55.5 / 41.2).
 #pragma once
 
 #include <cuda_fp16.h>
