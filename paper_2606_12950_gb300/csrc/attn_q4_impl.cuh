@@ -76,7 +76,9 @@ constexpr int kQ4Cost = 9, kBf16Cost = 32;
 template <int D>
 constexpr int kRunCost = D == 64 ? 56 : 18;
 constexpr int kQ4Spread = 4;              // warps of a CTA with parts, where there are few parts
-constexpr int kQ4MinPart = 96;            // a part's least cost: more than any tile's, so that each has one
+// A part costs no less than any tile, so that each has one: this much before rounding.
+template <int D>
+constexpr int kQ4MinPart = kRunCost<D> + kBf16Cost + kQ4Warps;
 
 struct Q4Args {
     const uint16_t *q;
@@ -656,21 +658,23 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
         const int64_t v = __shfl_up_sync(0xffffffffu, upto, off);
         if (lane >= off) upto += v;
     }
-    // Equal shares of the cost: CTAs, and in a CTA its warps; a warp's is at least
-    // kQ4MinPart.  (64-bit divisions take 0.5 us each: there is one where W needs it.)
+    // Equal shares of the cost, rounded up, but for the last: CTAs, and in a CTA its warps.
+    // The last one's roundings leave it a tile's cost: a warp's 15 of kQ4MinPart, a CTA's
+    // 151 at the most, and then it has four times as much.
+    // (Divisions take 0.1 us each in this chain, those of 64 bits 0.5.)
     const int64_t W = __shfl_sync(0xffffffffu, upto, kQ4Warps - 1);
-    const int NC = (int)min((int64_t)a.P, (W / kQ4MinPart + kQ4Spread - 1) / kQ4Spread + (W < kQ4MinPart));
+    const uint32_t least = (uint32_t)min(W, (int64_t)UINT32_MAX);
+    const int NC = (int)min((uint32_t)a.P, (least / kQ4MinPart<D> + kQ4Spread - 1) / kQ4Spread + (least < kQ4MinPart<D>));
     if (bid >= NC || W == 0) {
         if (a.by_part && tid == 0) a.ws_run[bid] = make_int2(-1, -1);
         return;
     }
-    const int64_t wq = (W >> 32) == 0 ? (int64_t)((uint32_t)W / (uint32_t)NC) : W / NC;
-    const uint32_t wr = (uint32_t)(W - wq * NC);
-    const int64_t c0 = bid * wq + (uint32_t)bid * wr / (uint32_t)NC;
-    const int32_t cn = (int32_t)(wq + (uint32_t)(bid + 1) * wr / (uint32_t)NC - (uint32_t)bid * wr / (uint32_t)NC);  // this CTA's
-    const int nw = max(1, min(kQ4Warps, cn / kQ4MinPart));
-    const int32_t nq = (int32_t)((uint32_t)cn / (uint32_t)nw), nr = cn - nq * nw;
-    auto warp_begin = [&](int w) { return w * nq + (int32_t)((uint32_t)(w * nr) / (uint32_t)nw); };
+    const int64_t wq = (W >> 32) == 0 ? (int64_t)((uint32_t)(W - 1) / (uint32_t)NC + 1u) : (W - 1) / NC + 1;
+    const int64_t c0 = bid * wq;
+    const int32_t cn = (int32_t)min(wq, W - c0);  // this CTA's
+    const int nw = max(1, min(kQ4Warps, cn / kQ4MinPart<D>));
+    const int32_t nq = (int32_t)((uint32_t)(cn - 1) / (uint32_t)nw + 1u);
+    auto warp_begin = [&](int w) { return min(w * nq, cn); };
 
     if (warp < nw) {
         const int32_t w0 = warp_begin(warp);
