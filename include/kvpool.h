@@ -88,6 +88,10 @@ typedef enum kv_status {
  * [Hkv][bs / 16] tiles of 16 tokens, K and V side by side (csrc/q4_format.h).
  * In a pool of bf16 and 4-bit blocks of one geometry, page_bytes is a 32nd of
  * the bf16 block; a superpage then holds one bf16 block or three 4-bit ones.
+ * The bf16 attention calls (and their workspace queries) need page_bytes to be a
+ * multiple of 2 head_dim, a row: pages of 128 bytes, or of 384, serve bf16 layouts
+ * of head_dim 64 there and no others (KV_ERR_UNSUPPORTED); the appends, copies,
+ * packing and paged_decode_attn_q4 take any.
  */
 #define KV_Q4 0x10000
 typedef struct kv_layout {

@@ -185,6 +185,9 @@ int attn_shape(const kv_pool *p, int layout, int S, int Hq, int max_blocks, int 
     const int G = Hq / L.num_kv_heads;
     if (L.head_dim != 64 && L.head_dim != 128) return KV_ERR_UNSUPPORTED;
     if (p->desc.block_size % kvp::kTile) return KV_ERR_UNSUPPORTED;
+    // a block is found by its row of the pool (beside a 4-bit layout, pages may be
+    // of 128 bytes; without one they are of whole rows)
+    if (p->page_bytes % (2ull * L.head_dim)) return KV_ERR_UNSUPPORTED;
     if (!(G == 1 || G == 2 || G == 4 || G == 5 || G == 8)) return KV_ERR_UNSUPPORTED;
     // unit ids and pool rows are 32-bit on the device
     const int64_t tiles = ((int64_t)max_blocks * p->desc.block_size + kvp::kTile - 1) / kvp::kTile;
