@@ -802,7 +802,9 @@ int paged_decode_attn_window(kv_pool *pool, int layout, const uint16_t *q, const
  * to the weights, which are rounded to fp16 with the scale (to bf16 before
  * rows in bf16); sums and softmax statistics in fp32.  Where |scale * q . K|
  * is near fp32's range, or q holds an infinity or a NaN, the output is NaN.
- * V groups with s below 2^-60 count as constant.
+ * Weights below 2^-86 of a head's largest count as 0.  A product of weight and V's
+ * scale is rounded to 2^-11 of itself, or to 2^-32 of the largest of its head and
+ * group of columns where that is more; scales below 2^-72 lose bits.
  * The result of a call does not depend on where its blocks lie.
  * Workspace: kv_q4_workspace_bytes (256-byte aligned, not initialised).
  * Errors: those of paged_decode_attn; KV_ERR_INVALID_ARG also where layout and

@@ -14,11 +14,16 @@
 //
 // Ranges.  q is scaled by a power of two (its largest column in [2^14, 2^15)),
 // so that fp16 holds all bits of its bf16 columns down to 2^-28 of the largest.
-// A weight meets V's scale before it is rounded to fp16: the running maximum M is
-// that of score + L, L the power of two above the unit's largest V scale, so
-// p s <= 2^15 (M moves only when it would be passed, by 2^8 at once).  The sums of
-// p and p z are fp32 and need no such range, and records (M, l, o) merge as those
-// of the bf16 kernel do.
+// Weights p = 2^(score - M) are held under 2^-32 (M moves only when that would be
+// passed, by 2^8 at once): the fp32 sums of p, p z and p v stay in range for any
+// bf16 z and v.  A weight meets V's scale before it is rounded to fp16, and a power
+// of two of its head and group, the gain, before that: the largest p s gain so far
+// lies in [2^7, 2^15], and the gain moves only when 2^15 is passed.  So a group keeps
+// its digits whatever the other's scales are, and whatever those of tokens of little
+// weight.  Gains leave the sums where the tiles in 4 bits end; records (M, l, o) merge
+// as those of the bf16 kernel do.  (One range for both groups, V's largest scale in M:
+// 2 to 4 % faster, 10 % with short contexts, but a V group of scales 2^24 under
+// the other's was lost, as was one beside a NaN.)
 //
 // Work split: a tile is 16 tokens of a (sequence, KV head) run; it costs 9 where
 // it is in 4 bits and 32 in bf16 (its bytes), a run's first one kRunCost more (what
@@ -74,6 +79,9 @@ constexpr int kQ4Stages = 2;
 template <int D>
 constexpr int kQ4Unit = D == 64 ? 4 : 2;  // tiles of a stage: 4608 bytes either way
 constexpr int kQ4Rebalance = 32;          // tiles (see Q4State::rebalance)
+constexpr float kWeightTop = -32.f;       // weights are below 2 to this,
+constexpr float kWeightRest = 40.f;       // and the largest 2^-40 where M has moved
+constexpr int kMostGain = 120;            // a scale of 2^-72 and a weight of 2^-40 make 2^8
 constexpr int kQ4Cost = 9, kBf16Cost = 32;
 template <int D>
 constexpr int kRunCost = D == 64 ? 56 : 18;
@@ -231,6 +239,11 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
+// 2^e, e from -126 to 127, and 0 below
+__device__ __forceinline__ float pow2_of(int e) { return __uint_as_float((uint32_t)max(e + 127, 0) << 23); }
+// the exponent of a power of two, or of the one below x
+__device__ __forceinline__ int exponent_of(float x) { return (int)(__float_as_uint(x) >> 23) - 127; }
+
 // `bytes` from global to shared memory, completing on `bar`
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar, uint64_t policy)
 {
@@ -251,7 +264,10 @@ struct Q4State {
     float factor[2];        // of the scores, to base-2 exponents; |scale| goes here, its sign to q
     float m[2], l[2];
     float z[NG][2];         // sums of p z over this lane's tokens
-    float acc[NM][4];       // sums of p s c: row pairs (e, e + 1), odd columns times 16, all times 2^-24
+    float gain[NG][2];      // powers of two (see the head of this file)
+    // sums of p s c: row pairs (e, e + 1), odd columns times 16, all times 2^-24 gain
+    // (from release on without that factor, and of p v too)
+    float acc[NM][4];
 
     // qrow: q rows of the run's G heads
     __device__ __forceinline__ void begin(const uint16_t *qrow, int G, float qk_scale, int lane)
@@ -307,6 +323,7 @@ struct Q4State {
                 part[c][i] = (uint32_t)__bfloat16_as_ushort(b) << 16;
             }
             z[c][0] = z[c][1] = 0.f;
+            gain[c][0] = gain[c][1] = pow2_of(kMostGain);
         }
         if constexpr (NG == 2) {  // t: group t % 2, its first (t < 2) or second term; then the third
             qsum[0] = tig == 0 ? part[0][0] : tig == 1 ? part[1][0] : tig == 2 ? part[0][1] : part[1][1];
@@ -326,33 +343,63 @@ struct Q4State {
             for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
     }
 
-    // The maximum's new place where a score passes it: y0, y1 the lane's largest
-    // scores plus L.
-    __device__ __forceinline__ void raise(float y0, float y1)
+    // M's new place where a score passes it: y0, y1 the lane's largest scores.  M
+    // moves by whole numbers; down[h]: 2 to the less of that, by which the sums acc are
+    // the caller's to scale.
+    __device__ __forceinline__ bool raise(float y0, float y1, float (&down)[2])
     {
-        if (!__any_sync(0xffffffffu, y0 > m[0] + 15.f || y1 > m[1] + 15.f)) return;
+        if (!__any_sync(0xffffffffu, y0 > m[0] + kWeightTop || y1 > m[1] + kWeightTop)) return false;
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) {
             y0 = fmaxf(y0, __shfl_xor_sync(0xffffffffu, y0, off));
             y1 = fmaxf(y1, __shfl_xor_sync(0xffffffffu, y1, off));
         }
-        const float m0 = y0 > m[0] + 15.f ? y0 - 7.f : m[0], m1 = y1 > m[1] + 15.f ? y1 - 7.f : m[1];
-        const float f0 = fast_exp2(m[0] - m0), f1 = fast_exp2(m[1] - m1);
-        m[0] = m0;
-        m[1] = m1;
-        l[0] *= f0;
-        l[1] *= f1;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float y = h ? y1 : y0, to = y > m[h] + kWeightTop ? rintf(y) + kWeightRest : m[h];
+            // (before the first score there is nothing to scale)
+            down[h] = m[h] == kMaxStart ? 1.f : pow2_of(-(int)fminf(to - m[h], 1000.f));
+            m[h] = to;
+            l[h] *= down[h];
+#pragma unroll
+            for (int c = 0; c < NG; ++c) z[c][h] *= down[h];
+        }
+        return true;
+    }
+
+    // The gains after M moved, or where the unit's weights p, with V's parameters vp,
+    // pass 2^15: a gain takes the move up, so that what was the largest p s gain stays
+    // it, and falls where something passes that, to 2^7 of it.  (A NaN is no maximum:
+    // it is on its way to its own columns.)
+    template <int U>
+    __device__ __forceinline__ void regain(const float (&p)[U][4], const uint32_t (&vp)[U][2][NG], const float (&down)[2])
+    {
+        constexpr uint32_t EXP = 0x7f800000u;
 #pragma unroll
         for (int c = 0; c < NG; ++c) {
-            z[c][0] *= f0;
-            z[c][1] *= f1;
-        }
+            uint32_t top = 0;  // of the heads' p s, as bf16 pairs
 #pragma unroll
-        for (int i = 0; i < NM; ++i) {
-            acc[i][0] *= f0;
-            acc[i][1] *= f1;
-            acc[i][2] *= f0;
-            acc[i][3] *= f1;
+            for (int u = 0; u < U; ++u) {
+                const float sa = bf_lo(vp[u][0][c]), sb = bf_lo(vp[u][1][c]);
+                const float t0 = fmaxf(0.f, fmaxf(p[u][0] * sa, p[u][2] * sb)), t1 = fmaxf(0.f, fmaxf(p[u][1] * sa, p[u][3] * sb));
+                top = __vmaxu2(top, __byte_perm(__float_as_uint(t0), __float_as_uint(t1), 0x7632));
+            }
+#pragma unroll
+            for (int off = 4; off < 32; off <<= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, off));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float t = h ? bf_hi(top) : bf_lo(top), old = gain[c][h];
+                // (1 / x of a power of two: its exponent, 127 too high, from 254)
+                float g = fminf(old * __uint_as_float(2 * (127u << 23) - __float_as_uint(down[h])), pow2_of(kMostGain));
+                if (t * g >= 0x1p15f) g = __uint_as_float(((2 * 127u + 7u) << 23) - (__float_as_uint(t) & EXP));
+                const float r = g * down[h] * __uint_as_float(2 * (127u << 23) - __float_as_uint(old));
+                gain[c][h] = g;
+#pragma unroll
+                for (int i = 4 * c; i < 4 * c + 4; ++i) {
+                    acc[i][h] *= r;
+                    acc[i][2 + h] *= r;
+                }
+            }
         }
     }
 
@@ -367,7 +414,6 @@ struct Q4State {
         float x[U][4];
         uint32_t vp[U][2][NG];
         float x0 = -INFINITY, x1 = -INFINITY;
-        uint32_t top = 0;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             {
@@ -417,42 +463,63 @@ struct Q4State {
                     x[u][1] = fmaf(dot[1], sa, x[u][1]);
                     x[u][2] = fmaf(dot[2], sb, x[u][2]);
                     x[u][3] = fmaf(dot[3], sb, x[u][3]);
-                    top = __vmaxu2(top, __vmaxu2(vp[u][0][c], vp[u][1][c]));
                 }
                 x0 = fmaxf(x0, fmaxf(x[u][0], x[u][2]));
                 x1 = fmaxf(x1, fmaxf(x[u][1], x[u][3]));
             }
         }
-        // L: a power of two above every V scale of the unit, from 2^-40 to 2^80
-        top = __reduce_max_sync(0xffffffffu, top << 16);
-        const float L = (float)min(max((int)(top >> 23) - 126, -40), 80);
-        raise(fmaf(x0, factor[0], L), fmaf(x1, factor[1], L));
+        float down[2] = {1.f, 1.f};
+        bool moved = raise(x0 * factor[0], x1 * factor[1], down);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            {
-                const uint8_t *tile = stage + min(u, count - 1) * TILE;
-                const bool in = u == 0 || u < count;
-                const float m0 = in ? -m[0] : -INFINITY, m1 = in ? -m[1] : -INFINITY;
-                const float p0 = fast_exp2(fmaf(x[u][0], factor[0], m0)), p1 = fast_exp2(fmaf(x[u][1], factor[1], m1));
-                const float p2 = fast_exp2(fmaf(x[u][2], factor[0], m0)), p3 = fast_exp2(fmaf(x[u][3], factor[1], m1));
-                l[0] += p0 + p2;
-                l[1] += p1 + p3;
+            const bool in = u == 0 || u < count;
+            const float m0 = in ? -m[0] : -INFINITY, m1 = in ? -m[1] : -INFINITY;
+            x[u][0] = fast_exp2(fmaf(x[u][0], factor[0], m0));
+            x[u][1] = fast_exp2(fmaf(x[u][1], factor[1], m1));
+            x[u][2] = fast_exp2(fmaf(x[u][2], factor[0], m0));
+            x[u][3] = fast_exp2(fmaf(x[u][3], factor[1], m1));
+            l[0] += x[u][0] + x[u][2];
+            l[1] += x[u][1] + x[u][3];
+        }
+        uint32_t b[U][NG][2];
+        auto weights = [&]() {  // rounded; the largest, as fp16 numbers
+            uint32_t top = 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int c = 0; c < NG; ++c) {
-                    const float sa = bf_lo(vp[u][0][c]), za = bf_hi(vp[u][0][c]);
-                    const float sb = bf_lo(vp[u][1][c]), zb = bf_hi(vp[u][1][c]);
-                    z[c][0] = fmaf(p0, za, fmaf(p2, zb, z[c][0]));
-                    z[c][1] = fmaf(p1, za, fmaf(p3, zb, z[c][1]));
-                    const uint32_t b0 = movmatrix_trans(f16_pair(p0 * sa, p1 * sa));
-                    const uint32_t b1 = movmatrix_trans(f16_pair(p2 * sb, p3 * sb));
-                    const uint4 v = *reinterpret_cast<const uint4 *>(tile + 8 * D + 512 * c + 16 * lane);
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                    const float2 g = make_float2(gain[c][0], gain[c][1]);
+                    const float sa = bf_lo(vp[u][0][c]), sb = bf_lo(vp[u][1][c]);
+                    const float2 pa = __fmul2_rn(make_float2(x[u][0], x[u][1]), g);
+                    const float2 pb = __fmul2_rn(make_float2(x[u][2], x[u][3]), g);
+                    b[u][c][0] = f16_pair(pa.x * sa, pa.y * sa);
+                    b[u][c][1] = f16_pair(pb.x * sb, pb.y * sb);
+                    top = __vmaxu2(top, __vmaxu2(b[u][c][0], b[u][c][1]));
+                }
+            return top;
+        };
+        // (2^15 and what is above, infinity and NaN too, carries into the sign)
+        if (!moved) moved = __any_sync(0xffffffffu, ((weights() + 0x08000800u) & 0x80008000u) != 0);
+        if (moved) {
+            regain<U>(x, vp, down);
+            weights();
+        }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t h = w[i] >> 8;
-                        mma_f16_16816(acc[4 * c + i], w[i] & 0x000f000fu, w[i] & 0x00f000f0u, h & 0x000f000fu,
-                                      h & 0x00f000f0u, b0, b1);
-                    }
+        for (int u = 0; u < U; ++u) {
+            const uint8_t *tile = stage + min(u, count - 1) * TILE;
+#pragma unroll
+            for (int c = 0; c < NG; ++c) {
+                const float za = bf_hi(vp[u][0][c]), zb = bf_hi(vp[u][1][c]);
+                z[c][0] = fmaf(x[u][0], za, fmaf(x[u][2], zb, z[c][0]));
+                z[c][1] = fmaf(x[u][1], za, fmaf(x[u][3], zb, z[c][1]));
+                const uint32_t b0 = movmatrix_trans(b[u][c][0]), b1 = movmatrix_trans(b[u][c][1]);
+                const uint4 v = *reinterpret_cast<const uint4 *>(tile + 8 * D + 512 * c + 16 * lane);
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t h = w[i] >> 8;
+                    mma_f16_16816(acc[4 * c + i], w[i] & 0x000f000fu, w[i] & 0x00f000f0u, h & 0x000f000fu, h & 0x00f000f0u,
+                                  b0, b1);
                 }
             }
         }
@@ -480,7 +547,24 @@ struct Q4State {
                     acc[i][h] -= x;
                     acc[i][2 + h] = fmaf(x, -16.f, acc[i][2 + h]);
                 }
-                z[c][h] = fmaf(x, 0x1p21f, z[c][h]);  // (an eighth each: eight lanes hold parts of the sum)
+                // (an eighth each: eight lanes hold parts of the sum)
+                z[c][h] = fmaf(x, pow2_of(21 - exponent_of(gain[c][h])), z[c][h]);
+            }
+    }
+
+    // The tiles in 4 bits are done: the sums without their gains.
+    __device__ __forceinline__ void release()
+    {
+#pragma unroll
+        for (int c = 0; c < NG; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float f = pow2_of(24 - exponent_of(gain[c][h]));
+#pragma unroll
+                for (int i = 4 * c; i < 4 * c + 4; ++i) {
+                    acc[i][h] *= f;
+                    acc[i][2 + h] *= f;
+                }
             }
     }
 
@@ -512,7 +596,17 @@ struct Q4State {
         y[1] = gid < valid ? x[1] * qk_scale : no;
         y[2] = gid + 8 < valid ? x[2] * qk_scale : no;
         y[3] = gid + 8 < valid ? x[3] * qk_scale : no;
-        raise(fmaxf(y[0], y[2]), fmaxf(y[1], y[3]));
+        float down[2];
+        if (raise(fmaxf(y[0], y[2]), fmaxf(y[1], y[3]), down)) {
+            const float f0 = down[0], f1 = down[1];
+#pragma unroll
+            for (int i = 0; i < NM; ++i) {
+                acc[i][0] *= f0;
+                acc[i][1] *= f1;
+                acc[i][2] *= f0;
+                acc[i][3] *= f1;
+            }
+        }
     }
     __device__ __forceinline__ void values16(const float (&y)[4], const uint16_t *rows, int valid, int lane)
     {
@@ -530,10 +624,8 @@ struct Q4State {
         const float p2 = fast_exp2(y[2] - m[0]), p3 = fast_exp2(y[3] - m[1]);
         l[0] += p0 + p2;
         l[1] += p1 + p3;
-        // the accumulators' units: weights times 2^-24, odd columns times 16
-        const float down = 0x1p-24f;
-        const uint32_t b0 = movmatrix_trans(bf16_pair(p0 * down, p1 * down));
-        const uint32_t b1 = movmatrix_trans(bf16_pair(p2 * down, p3 * down));
+        const uint32_t b0 = movmatrix_trans(bf16_pair(p0, p1)), b1 = movmatrix_trans(bf16_pair(p2, p3));
+        // (odd columns times 16, as the accumulators have them)
         const __nv_bfloat162 up = __float2bfloat162_rn(16.f);
 #pragma unroll
         for (int c = 0; c < NG; ++c)
@@ -574,8 +666,8 @@ struct Q4State {
                 float o[8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    o[2 * i] = fmaf(acc[4 * c + i][h], 0x1p24f, z[c][h]);
-                    o[2 * i + 1] = fmaf(acc[4 * c + i][2 + h], 0x1p20f, z[c][h]);
+                    o[2 * i] = acc[4 * c + i][h] + z[c][h];
+                    o[2 * i + 1] = fmaf(acc[4 * c + i][2 + h], 0.0625f, z[c][h]);
                 }
                 const int at = head * D + 64 * c + 8 * gid;
                 if (split) {
@@ -846,6 +938,7 @@ __global__ void __launch_bounds__(kQ4Threads, 1) q4_attn_kernel(const __grid_con
                     for (int32_t u = i; u < end4; ++u) st.template tiles4<1>(tile_in() + (u - i) * TILE, 1, lane);
                 unit_done(1);
             }
+            if (i0 < end4) st.release();
             for (i = max(i0, end4); i < i1; ++i) {
                 const Q4Run<D> run = get_run<D>(box(k));
                 const int32_t r = run.s * a.Hkv + run.g, tok0 = i * kQ4Tile, valid = run.q.n - tok0;
