@@ -266,7 +266,7 @@ struct Q4State {
     float z[NG][2];         // sums of p z over this lane's tokens
     float gain[NG][2];      // powers of two (see the head of this file)
     // sums of p s c: row pairs (e, e + 1), odd columns times 16, all times 2^-24 gain
-    // (from release on without that factor, and of p v too)
+    // (from release on without those factors, and of p v too)
     float acc[NM][4];
 
     // qrow: q rows of the run's G heads
@@ -552,18 +552,20 @@ struct Q4State {
             }
     }
 
-    // The tiles in 4 bits are done: the sums without their gains.
+    // The tiles in 4 bits are done: the sums themselves.  (bf16 values take no factor of
+    // 16: it would carry an odd column's from 2^124 on past their range.)
     __device__ __forceinline__ void release()
     {
 #pragma unroll
         for (int c = 0; c < NG; ++c)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const float f = pow2_of(24 - exponent_of(gain[c][h]));
+                const int e = exponent_of(gain[c][h]);
+                const float f = pow2_of(24 - e), odd = pow2_of(20 - e);
 #pragma unroll
                 for (int i = 4 * c; i < 4 * c + 4; ++i) {
                     acc[i][h] *= f;
-                    acc[i][2 + h] *= f;
+                    acc[i][2 + h] *= odd;
                 }
             }
     }
@@ -625,8 +627,6 @@ struct Q4State {
         l[0] += p0 + p2;
         l[1] += p1 + p3;
         const uint32_t b0 = movmatrix_trans(bf16_pair(p0, p1)), b1 = movmatrix_trans(bf16_pair(p2, p3));
-        // (odd columns times 16, as the accumulators have them)
-        const __nv_bfloat162 up = __float2bfloat162_rn(16.f);
 #pragma unroll
         for (int c = 0; c < NG; ++c)
 #pragma unroll
@@ -637,9 +637,7 @@ struct Q4State {
                     const uint32_t w0 = reinterpret_cast<const uint32_t *>(&vw[2 * r][c])[i];
                     const uint32_t w1 = reinterpret_cast<const uint32_t *>(&vw[2 * r + 1][c])[i];
                     a[2 * r] = __byte_perm(w0, w1, 0x5410);
-                    const uint32_t odd = __byte_perm(w0, w1, 0x7632);
-                    const __nv_bfloat162 o = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&odd), up);
-                    a[2 * r + 1] = *reinterpret_cast<const uint32_t *>(&o);
+                    a[2 * r + 1] = __byte_perm(w0, w1, 0x7632);
                 }
                 mma_bf16_16816(acc[4 * c + i], a[0], a[1], a[2], a[3], b0, b1);
             }
@@ -667,7 +665,7 @@ struct Q4State {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     o[2 * i] = acc[4 * c + i][h] + z[c][h];
-                    o[2 * i + 1] = fmaf(acc[4 * c + i][2 + h], 0.0625f, z[c][h]);
+                    o[2 * i + 1] = acc[4 * c + i][2 + h] + z[c][h];
                 }
                 const int at = head * D + 64 * c + 8 * gid;
                 if (split) {

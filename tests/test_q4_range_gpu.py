@@ -191,3 +191,28 @@ def test_scales_that_change_along_a_run(d):
     want, tol = c.reference(q, SCALE)
     q4_ref.check(out, want.expand(S, 1, d), (tol + grain(c, q)).expand(S, 1, d))
     c.close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("value", [2.0 ** 123, -(2.0 ** 124), 2.0 ** 126, 3.0e38])
+@pytest.mark.parametrize("column", [6, 7, 63])
+def test_large_values_in_bf16_rows(column, value, d):
+    """One bf16 row holds a value near fp32's last, in an even or odd column: the
+    output is finite and right, in contexts with tokens in 4 bits and without."""
+    from tests import q4_ref
+
+    def change(x, s):
+        m = x.shape[1]
+        for t in (m - 1, m - 5, SPECIAL):
+            if P[s] <= t < m:
+                x[:, t, column] = value * 2.0 ** (-3 * (t != SPECIAL))
+
+    q = queries(d)
+    c = cache(d, change, True, q)
+    out = c.run(q, SCALE)
+    torch.cuda.synchronize()
+    want, tol = c.reference(q, SCALE)
+    assert torch.isfinite(out).all()
+    q4_ref.check(out, want, tol + grain(c, q))
+    assert c.error() == 0
+    c.close()
