@@ -297,10 +297,22 @@ class PackedLayer(WindowedLayer):
                 K.kv_pool_trim(self.pool.handle)
                 st4 = K.kv_pool_stats(self.pool.handle)
                 n = min(want - have, st4["blocks_capacity"][1] - st4["blocks_used"][1])
+                # (a VMM pool's capacity counts what its limit or budget may not let be mapped)
+                while n and not self._packs(s, int(lens[s]) - (have + n) * self.bs, st):
+                    n //= 2
                 if n == 0:
                     return  # they stay as they are until there is room
-                self.tab.pack(self.tab4, [s], int(lens[s]) - (have + n) * self.bs, st)
                 have += n
+
+    def _packs(self, s: int, keep: int, st) -> bool:
+        """Packs slot s but for its last `keep` tokens; False where there is no room."""
+        try:
+            self.tab.pack(self.tab4, [s], keep, st)
+        except K.KVError as e:
+            if e.code != K.KV_ERR_OUT_OF_BLOCKS:
+                raise
+            return False
+        return True
 
     def prompt(self, counts, q, k, v, stream=None) -> torch.Tensor:
         """As WindowedLayer.prompt; KVError (KV_ERR_OUT_OF_BLOCKS) also where the
