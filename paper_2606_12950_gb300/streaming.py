@@ -316,7 +316,7 @@ class PackedLayer(WindowedLayer):
 
     def prompt(self, counts, q, k, v, stream=None) -> torch.Tensor:
         """As WindowedLayer.prompt; KVError (KV_ERR_OUT_OF_BLOCKS) also where the
-        pool has no pages for copies of packed ones."""
+        pool has no pages for copies of packed ones (nothing has changed then)."""
         counts = np.asarray(counts, dtype=np.int64)
         lens, T = self.tab.lens(), int(counts.sum())
         if counts.shape != (self.S,) or counts.min() < 0 or q.shape[0] != T:
@@ -325,12 +325,13 @@ class PackedLayer(WindowedLayer):
             return torch.empty((0, self.Hq, self.d), dtype=torch.bfloat16, device=q.device)
         self._check_rows(T, q, k, v)
         slots = np.nonzero(counts)[0]
-        for s in slots:
-            self._room(lambda: self.tab.reserve(int(s), int(lens[s] + counts[s])))
         table4, lens4 = self.tab4.host()
         packed = [(s, int(lens4[s]) // self.bs) for s in slots if lens4[s]]
+        # (first: without them nothing is reserved)
         copies = self._room(lambda: K.kv_alloc_blocks(self.pool.handle, 0, sum(n for _, n in packed)))
         try:
+            for s in slots:
+                self._room(lambda: self.tab.reserve(int(s), int(lens[s] + counts[s])))
             for s in slots:
                 self.tab.set_len(int(s), int(lens[s] + counts[s]))
             with self._on(stream, q, k, v) as st:

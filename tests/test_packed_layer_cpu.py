@@ -126,3 +126,42 @@ def test_a_few_pages_at_a_time_under_a_limit(make):
     x = make(ElasticPool(100, 22))
     x.prompt([21 * BS, 0], *rows(21 * BS))
     assert x.tab4.lens()[0] == 20 * BS and x.pages_used() == 1 and x.packed_used() == 20
+
+
+def test_a_refused_prompt_reserves_nothing(make):
+    """The copies of packed pages are asked for before the new tokens' own pages: a
+    prompt refused for want of them leaves tables and pool as they were."""
+    x = make(FixedPool(8))
+    x.prompt([100, 0], *rows(100))
+    assert x.packed_used() == 6 and x.pages_used() == 1     # three superpages of eight
+    hog = K.kv_alloc_blocks(x.pool.handle, 0, 3)
+    before = state(x)
+    with pytest.raises(K.KVError) as e:
+        x.prompt([20, 0], *rows(20))                        # a page, and six for copies, of two
+    assert e.value.code == K.KV_ERR_OUT_OF_BLOCKS
+    assert state(x) == before
+    K.kv_free_blocks(x.pool.handle, 0, hog)
+    before = state(x)
+    with pytest.raises(K.KVError):
+        x.prompt([20, 30], *rows(50))
+    assert state(x) == before
+    x.release(0)
+    x.prompt([60, 0], *rows(60))
+    x.prompt([20, 0], *rows(20))                            # three copies, given back
+    assert x.tab.lens()[0] == 80 and x.packed_used() == 4 and x.pages_used() == 1
+
+
+def test_a_prompt_without_pages_of_its_own_gives_its_copies_back(make):
+    x = make(FixedPool(8))
+    x.prompt([100, 0], *rows(100))
+    used = K.kv_pool_stats(x.pool.handle)["blocks_used"]
+    with pytest.raises(K.KVError) as e:
+        x.prompt([0, 400], *rows(400))                      # 25 pages
+    assert e.value.code == K.KV_ERR_OUT_OF_BLOCKS
+    assert K.kv_pool_stats(x.pool.handle)["blocks_used"] == used and x.tab.lens().tolist() == [100, 0]
+    x.release(0)
+    x.prompt([33, 0], *rows(33))
+    used = K.kv_pool_stats(x.pool.handle)["blocks_used"]
+    with pytest.raises(K.KVError):
+        x.prompt([200, 0], *rows(200))                      # two copies, then 13 pages more
+    assert K.kv_pool_stats(x.pool.handle)["blocks_used"] == used and x.tab.lens().tolist() == [33, 0]
