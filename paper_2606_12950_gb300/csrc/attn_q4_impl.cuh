@@ -18,7 +18,7 @@
 // passed, by 2^8 at once): the fp32 sums of p, p z and p v stay in range for any
 // bf16 z and v.  A weight meets V's scale before it is rounded to fp16, and a power
 // of two of its head and group, the gain, before that: the largest p s gain so far
-// lies in [2^7, 2^15], and the gain moves only when 2^15 is passed.  So a group keeps
+// lies in [2^7, 2^16), and the gain moves only when 2^15 is passed.  So a group keeps
 // its digits whatever the other's scales are, and whatever those of tokens of little
 // weight.  Gains leave the sums where the tiles in 4 bits end; records (M, l, o) merge
 // as those of the bf16 kernel do.  (One range for both groups, V's largest scale in M:
@@ -343,9 +343,9 @@ struct Q4State {
             for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
     }
 
-    // M's new place where a score passes it: y0, y1 the lane's largest scores.  M
-    // moves by whole numbers; down[h]: 2 to the less of that, by which the sums acc are
-    // the caller's to scale.
+    // M's new place where a score passes it: y0, y1 the lane's largest scores.  Their
+    // weights are powers of two then, and lose nothing where weights are rounded.
+    // down[h]: what the sums acc are the caller's to scale by.
     __device__ __forceinline__ bool raise(float y0, float y1, float (&down)[2])
     {
         if (!__any_sync(0xffffffffu, y0 > m[0] + kWeightTop || y1 > m[1] + kWeightTop)) return false;
@@ -356,9 +356,8 @@ struct Q4State {
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const float y = h ? y1 : y0, to = y > m[h] + kWeightTop ? rintf(y) + kWeightRest : m[h];
-            // (before the first score there is nothing to scale)
-            down[h] = m[h] == kMaxStart ? 1.f : pow2_of(-(int)fminf(to - m[h], 1000.f));
+            const float y = h ? y1 : y0, to = y > m[h] + kWeightTop ? y + kWeightRest : m[h];
+            down[h] = fast_exp2(m[h] - to);
             m[h] = to;
             l[h] *= down[h];
 #pragma unroll
@@ -368,9 +367,9 @@ struct Q4State {
     }
 
     // The gains after M moved, or where the unit's weights p, with V's parameters vp,
-    // pass 2^15: a gain takes the move up, so that what was the largest p s gain stays
-    // it, and falls where something passes that, to 2^7 of it.  (A NaN is no maximum:
-    // it is on its way to its own columns.)
+    // pass 2^15: a gain takes the move's power of two up, so that what was the largest
+    // p s gain stays it, and falls where something passes that, to 2^7 of it.  (A NaN is
+    // no maximum: it is on its way to its own columns.)
     template <int U>
     __device__ __forceinline__ void regain(const float (&p)[U][4], const uint32_t (&vp)[U][2][NG], const float (&down)[2])
     {
@@ -390,7 +389,7 @@ struct Q4State {
             for (int h = 0; h < 2; ++h) {
                 const float t = h ? bf_hi(top) : bf_lo(top), old = gain[c][h];
                 // (1 / x of a power of two: its exponent, 127 too high, from 254)
-                float g = fminf(old * __uint_as_float(2 * (127u << 23) - __float_as_uint(down[h])), pow2_of(kMostGain));
+                float g = fminf(old * __uint_as_float(2 * (127u << 23) - (__float_as_uint(down[h]) & EXP)), pow2_of(kMostGain));
                 if (t * g >= 0x1p15f) g = __uint_as_float(((2 * 127u + 7u) << 23) - (__float_as_uint(t) & EXP));
                 const float r = g * down[h] * __uint_as_float(2 * (127u << 23) - __float_as_uint(old));
                 gain[c][h] = g;

@@ -216,3 +216,40 @@ def test_large_values_in_bf16_rows(column, value, d):
     q4_ref.check(out, want, tol + grain(c, q))
     assert c.error() == 0
     c.close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_token_with_all_the_weight_gives_its_row(d):
+    """The largest weight loses nothing where weights are rounded: a context of one
+    token gives its V row bit for bit, one whose other tokens weigh under 2^-40 the
+    row of the token that is left, rounded once (2^-8 of the value).  Besides, s c is
+    weighed with the rounded weight and z with the fp32 one, whose exponent, a
+    difference of numbers in [64, 128) with a spacing of 2^-17, is off by 2^-18: the
+    weight by ln 2 of that, z by as much of V's largest, and the fp32 sums by 2^-20 of it:
+    under 2^-17 together."""
+    from tests import q4_ref
+
+    S, at = 40, 37  # the token: in 4 bits in half of the sequences, the others in bf16
+    g = generator(5, 5)
+    q = torch.randn(2 * S, 8, d, device="cuda", generator=g).to(torch.bfloat16)
+    q[:, 1:4], q[:, 5:] = q[:, :1], q[:, 4:5]  # (a KV head's queries alike)
+
+    def make(kv, s, m):
+        x = torch.randn(2, m, d, device="cuda", generator=g)
+        if kv == 0 and m > at:
+            h = q[s, ::4].float()
+            x[:, at] = h * ((55 + 0.3 * s) * d ** 0.5 / h.square().sum(-1, keepdim=True))
+        return x.to(torch.bfloat16)
+
+    c = q4_ref.PagedQ4([1] * S + [60] * S, [0] * S + [48 * (s % 2) for s in range(S)], 8, 2, d, 16, 4, append=False, make=make)
+    out = c.run(q, d ** -0.5)
+    torch.cuda.synchronize()
+    for s in range(2 * S):
+        x = c.rows[s][1]
+        if s < S:
+            assert torch.equal(out[s].view(2, 4, d), x[:, :1].expand(2, 4, d))
+            continue
+        row = (q4_ref.values(x) if c.p[s] else x.double())[:, at : at + 1]
+        assert ((out[s].view(2, 4, d).double() - row).abs() <= 2.0 ** -8 * row.abs() + 2.0 ** -17 * x.double().abs().max()).all()
+    assert c.error() == 0
+    c.close()
