@@ -423,6 +423,8 @@ int kv_seq_fork(kv_seqtab *t, int src, int n, const int32_t *dsts, void *stream)
  * *n_packed (may be null) receives the number of blocks.  Sync both tables
  * afterwards.  A block given up here is free at once: work on other streams
  * that reads it has to be ordered before `stream`, and later writers after it.
+ * Calls that end or replace a chat (kv_seq_release, kv_seq_replace) act on one
+ * table: they are to be made on both.
  * All-or-nothing: KV_ERR_OUT_OF_BLOCKS (4-bit blocks, or no host memory),
  * KV_ERR_INVALID_ARG (tables of different pools or slot counts, keep < 1, a
  * slot out of range or given twice, t4 shorter than a slot needs, a packed
@@ -689,7 +691,7 @@ int kv_append_rotary(kv_pool *pool, int layout, const kv_rotary *rot, const uint
  * in fp32, the sum of squares too, with one rounding to bf16 at the end, also
  * for the columns past rot_dim.  A row of zeros with eps = 0 and one with a NaN
  * give NaN; one whose sum of squares leaves fp32 (values near 2^64) gives zeros,
- * and NaN where it holds an infinity.  All else, the strides, q == q_out,
+ * and NaN where it holds an infinity; with eps = 0, rows under 2^-60 lose digits.  All else, the strides, q == q_out,
  * ragged chunks and errors, is as there; KV_ERR_INVALID_ARG also for eps < 0
  * or not finite and where the current device is not the pool's,
  * KV_ERR_UNSUPPORTED for head dims above 256.

@@ -22,8 +22,8 @@
 // its digits whatever the other's scales are, and whatever those of tokens of little
 // weight.  Gains leave the sums where the tiles in 4 bits end; records (M, l, o) merge
 // as those of the bf16 kernel do.  (One range for both groups, V's largest scale in M:
-// 2 to 4 % faster, 10 % with short contexts, but a V group of scales 2^24 under
-// the other's was lost, as was one beside a NaN.)
+// 4 % faster, 10 % with short contexts, but a V group of scales 2^24 under the other's
+// was lost, as was one beside a NaN.)
 //
 // Work split: a tile is 16 tokens of a (sequence, KV head) run; it costs 9 where
 // it is in 4 bits and 32 in bf16 (its bytes), a run's first one kRunCost more (what
@@ -34,36 +34,30 @@
 // bulk copy a tile (or K or V, where they are in bf16).
 //
 // Bound by HBM in the long run, by its start and end in short ones.  Steady state (the
-// slope from 240000 to 480000 tokens, 32 q / 8 KV heads of 128): 7.13 TB/s read, 1.05
-// of the measured copy; 16 single heads of 64 6.44.  Around it a call spends about 12
+// slope from 240000 to 480000 tokens, 32 q / 8 KV heads of 128): 6.68 TB/s read, 0.99
+// of the measured copy; 16 single heads of 64 6.35.  Around it a call spends about 13
 // us: the lengths' round trip and the split 3, the table's and the first tiles' 3, warps
 // that end apart 2, merges and the combine 4.  Calls (us; floor at 6.78 TB/s):
-//   250 sequences, 40 q / 8 KV heads of 128, 700 MB    112.9 (103)
-//   64 sequences, 32 / 8 of 128, 242 MB                 46.3 (35.7)
-//   one of 100000 tokens, 32 / 8 of 128, 115 MB         28.8 (17.0)
-//   40 sequences, 16 heads of 64, 140 MB                33.6 (20.7)
-//   400 of 100 to 500 tokens, 32 / 8 of 128, 174 MB     41.1 (25.7)
-//   1000 of 20 to 200 tokens, 32 / 8 of 128, 217 MB     54.7 (32.0)
-//   8 of 600 to 3500 tokens, 32 / 8 of 128, 20 MB      14.1 (2.9)
-// A tile of 128 columns takes 252 issue slots of the 396 that an SM quarter has while
+//   250 sequences, 40 q / 8 KV heads of 128, 700 MB    117.6 (103)
+//   64 sequences, 32 / 8 of 128, 242 MB                 48.4 (35.7)
+//   one of 100000 tokens, 32 / 8 of 128, 115 MB         30.2 (17.0)
+//   40 sequences, 16 heads of 64, 140 MB                34.6 (20.7)
+//   400 of 100 to 500 tokens, 32 / 8 of 128, 174 MB     45.3 (25.7)
+//   1000 of 20 to 200 tokens, 32 / 8 of 128, 217 MB     60.2 (32.0)
+//   8 of 600 to 3500 tokens, 32 / 8 of 128, 20 MB      14.4 (2.9)
+// A tile of 128 columns takes 265 issue slots of the 396 that an SM quarter has while
 // HBM brings it; half of them are masks and shifts of codes, which is why the masked
 // words must be operands as they are.  (With a subtraction per pair, or codes as bf16,
 // they would be twice as many.)  Short runs add what begins and ends them; there the
 // kernel waits for instructions more than for data, and its size counts.
 //
-// What was measured on the way, 64 / 250 sequences: a CTA of 8 warps twice on an SM 54.0
-// / 123.9 and one of 16 48.2 / 117.4, as the CTA that came first ran 25% ahead and left
-// the other half the SM; warps' records for the combine, not CTAs', 60.6 / 145.5; bf16
-// tiles read into registers, without the ring, 54.0 / 136.7; the last CTA of a run
-// merging its records, in place of the combine, 52.7 / 123.5 (counted by compare and
-// swap) and 53.9 / 124.4 (flags), as the fences at a CTA's end took 7 us.  Later, 47.1 /
-// 112.9 then: shifts as high products, off the busiest pipe, 51.8 / 126.7; the way to the
-// first tiles gone once before the grids ahead are done, for its instructions, 48.3 /
-// 114.9.  And 1000 short / 400 / 250 sequences: 92.4 / 58.3 / 118.6 with the runs' fields in
-// registers, spilled in the loops (66.4 / 48.8 / 113.5 in shared memory); 64.8 / 48.2 with
-// three loops that ask for tiles and lone tiles on their own (57.4 / 42.8); runs found
-// twice, by the loader and the consumer, 57.3 / 42.8 (55.5 / 41.2).  Least parts of 112 and
-// 160, not 66, with 8 contexts: 15.5 and 17.0 (14.1).
+// Why this shape (64 / 250 sequences, us, with the rest of the code as it then was): a CTA
+// of 16 warps an SM, not two of 8, of which the first ran 25% ahead and left the other
+// half the SM: 54.0 / 123.9 to 48.2 / 117.4.  CTAs' records for the combine, not warps':
+// 60.6 / 145.5 to 54.0 / 136.7.  bf16 tiles through the ring, not into registers: 54.0 /
+// 136.7 to 51.0 / 123.9.  Runs' fields in shared memory, not registers, spilled in the
+// loops (1000 short / 400): 92.4 / 58.3 to 66.4 / 48.8; one loop that asks for tiles and
+// finds each run once: 64.8 / 48.2 to 55.5 / 41.2.
 #pragma once
 
 #include <cuda_fp16.h>
